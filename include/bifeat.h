@@ -87,7 +87,8 @@ typedef enum {
     BIFEAT_VQ = 2
 } bifeat_kind;
 
-typedef enum { BIFEAT_F32 = 0, BIFEAT_F16 = 1 } bifeat_dtype;
+/* BIFEAT_BF16: the calls of the paged cache only (bifeat_cache_*) */
+typedef enum { BIFEAT_F32 = 0, BIFEAT_F16 = 1, BIFEAT_BF16 = 2 } bifeat_dtype;
 
 /* Sec. 3.2 allows two rules for the nearest codebook entry: Euclidean distance
  * or cosine similarity.  Cosine: the entry with the largest (x . C_c)/|C_c| (the
@@ -368,6 +369,113 @@ int bifeat_check_lists(const int64_t *indptr, const int64_t *indices, int64_t V,
 int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *indptr,
                          const int64_t *indices, int64_t E, int32_t layers, float *work,
                          double *scale, void *stream);
+
+/* ---- a paged cache of keys and values in few bits
+ * The table above is encoded once and read ever after; a model that answers token by
+ * token has one that grows by a row per token and head, which every new token reads
+ * as a whole, weighted: attention.  The cache keeps it as uniform scalar codes (the
+ * evenly spaced levels of Sec. 3.1) whose range is each row's own, so that rows need
+ * no fit and are written as they come.
+ *
+ * A sequence's tokens lie in pages of page_size tokens.  Pages are the caller's
+ * memory: DEVICE uint8 [num_pages][bifeat_cache_page_bytes()], 16-byte aligned.  A page
+ * holds, head after head,
+ *     codes of the keys    [page_size][rb]        rb = head_dim * bits / 8 rounded up to 16
+ *     codes of the values  [page_size][rb]
+ *     fp32 key scale, key minimum, value scale, value minimum   [page_size] each
+ * with column j's code at bit (j*bits) mod 8 of byte floor(j*bits/8) of its row, pad 0.
+ *
+ * write: with mn, mx the least and largest of a token's head_dim columns of one head
+ *   and L = 2^bits - 1, each step rounded to fp32 once: range = mx - mn, scale =
+ *   range / L, inv = L / range, code = min(rne((x - mn) * inv), L).  Where inv is not
+ *   finite (columns all alike, or closer than L / FLT_MAX) scale = inv = 0.  A row that
+ *   holds an infinity or a NaN, or whose range is not finite, gets scale = mn = NaN: it
+ *   reads back as NaN and spoils the tokens that attend to it, but no others.
+ * read: x' = mn + code * scale.
+ * attend: query token i of sequence b is at position p = lengths[b] - n_b + i, query head
+ *   h reads cached head h / (query_heads / heads).  It sees position j < lengths[b] if
+ *   j <= p and (window == 0 or j > p - window), or if j < prefix[b].  With
+ *     y = scale * q . k_j,   x = softcap > 0 ? softcap * tanh(y / softcap) : y,
+ *     x += slopes[h] * (j - p)
+ *   the output is sum_j softmax(x)_j v_j; a query that sees nothing gets zeros.
+ *
+ * Queries of BIFEAT_F16 and BIFEAT_BF16 enter the matrix cores as fp16 (scaled by a
+ * power of two per tile of rows: exact but for bf16 columns 2^-29 of a tile's largest),
+ * codes as they are; products are summed in fp32, softmax and its sums are fp32, weights
+ * are rounded to fp16 before they meet the values' codes.  BIFEAT_F32: queries and
+ * weights enter as two fp16 pieces each (22 bits). */
+typedef struct {
+    int32_t bits;      /* 4 or 8 */
+    int32_t heads;     /* cached heads, 1..1024 */
+    int32_t head_dim;  /* columns a head, 1..256 */
+    int32_t page_size; /* tokens a page: 16, 32, 64, ... 1024 */
+} bifeat_cache_spec;
+
+/* Opaque: the spec, options, and the workspace of bifeat_cache_attend (device memory,
+ * allocated by the first call that needs it, on the device current then). */
+typedef struct bifeat_cache bifeat_cache;
+
+/* The sequences of one call and which of their tokens it is about: the last n_b of
+ * lengths[b] (those the call writes, reads back or that ask).  n_b = indptr[b+1] -
+ * indptr[b], or tokens / sequences for all if indptr is NULL.  Token t of the call's
+ * [tokens x ...] arrays is sequence b's number t - indptr[b].  Position j of sequence b
+ * lies in page tables[b * table_width + j / page_size], slot j % page_size.
+ * Where n_b > lengths[b], the first n_b - lengths[b] tokens lie before the sequence's
+ * beginning: they are not written, read as zeros, and see nothing.
+ * Contract (checked with option "validate" or by bifeat_cache_check): indptr begins with
+ * 0, does not decrease and ends with `tokens`; 0 <= lengths[b] <= table_width *
+ * page_size; table entries of pages below lengths[b] lie in [0, num_pages).  Others are
+ * not read.  For write, no two tokens of a call share a place. */
+typedef struct {
+    const int32_t *tables;  /* DEVICE [sequences][table_width] */
+    int64_t table_width;
+    const int64_t *lengths; /* DEVICE [sequences], the call's own tokens among them */
+    const int64_t *indptr;  /* DEVICE [sequences + 1] or NULL */
+    int64_t sequences;
+    int64_t tokens;
+} bifeat_cache_batch;
+
+/* A [tokens][heads][head_dim] array whose columns lie next to each other: slices of a
+ * joint projection have token strides of their own.  Strides in elements, >= 0. */
+typedef struct {
+    const void *data; /* DEVICE */
+    int64_t token_stride, head_stride;
+} bifeat_head_rows;
+
+typedef struct {
+    float scale;           /* of q . k; usually 1 / sqrt(head_dim) */
+    float softcap;         /* > 0: scores capped by softcap * tanh(y / softcap); 0: not */
+    int64_t window;        /* > 0: positions seen back from the query's own, itself among them; 0: all */
+    const int64_t *prefix; /* DEVICE [sequences]: positions below it are seen by all queries; or NULL */
+    const float *slopes;   /* DEVICE [query_heads]: bias by distance; or NULL */
+} bifeat_attend_options;
+
+int bifeat_cache_create(const bifeat_cache_spec *spec, bifeat_cache **out);
+void bifeat_cache_destroy(bifeat_cache *c);
+/* Bytes of a page (a multiple of 16), or BIFEAT_EINVAL. */
+int64_t bifeat_cache_page_bytes(const bifeat_cache *c);
+/* "validate" = 1: every call first checks its batch on the GPU, synchronises `stream` and
+ * returns BIFEAT_EINVAL without launching anything else when the contract is broken. */
+int bifeat_cache_set_option(bifeat_cache *c, const char *name, int value);
+/* Allocates the workspace of bifeat_cache_attend ahead of time.  While a stream is
+ * captured nothing is allocated: a call that finds no workspace then does not split
+ * contexts over workgroups. */
+int bifeat_cache_reserve(bifeat_cache *c, void *stream);
+/* The batch contract on its own: BIFEAT_OK or BIFEAT_EINVAL; synchronises `stream`. */
+int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_cache_batch *batch, void *stream);
+
+/* The three calls only enqueue kernels on `stream`.  tokens = 0 is a no-op.  `dtype`
+ * (BIFEAT_F32, _F16, _BF16) is the type of k and v, of the arrays read into, of q and out.
+ * k, v outputs of read: DEVICE [tokens][heads][head_dim]; out: DEVICE
+ * [tokens][query_heads][head_dim]; query_heads a multiple of heads.  Calls on one handle
+ * that overlap in time share attend's workspace and must not. */
+int bifeat_cache_write(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
+                       const bifeat_head_rows *k, const bifeat_head_rows *v, int32_t dtype, void *stream);
+int bifeat_cache_read(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
+                      void *k, void *v, int32_t dtype, void *stream);
+int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
+                        const bifeat_head_rows *q, int32_t query_heads, int32_t dtype,
+                        const bifeat_attend_options *options, void *out, void *stream);
 
 const char *bifeat_strerror(int status);
 

@@ -16,7 +16,7 @@ _LIB_PATH = os.environ.get("BIFEAT_LIB") or os.path.join(_HERE, "libbifeat.so")
 
 UNIFORM, LOG, VQ = 0, 1, 2
 VQ_L2, VQ_COSINE = 0, 1
-F32, F16 = 0, 1
+F32, F16, BF16 = 0, 1, 2
 OK, EINVAL, ENOTFIT, EHIP, ENOTSUP, ELIMIT = 0, -1, -2, -3, -4, -5
 FIT_AGAIN = 1
 
@@ -30,6 +30,24 @@ class BifeatError(RuntimeError):
 class _CScheme(C.Structure):
     _fields_ = [("kind", C.c_int32), ("bits", C.c_int32),
                 ("vq_width", C.c_int32), ("vq_length", C.c_int32), ("vq_metric", C.c_int32)]
+
+
+class _CCacheSpec(C.Structure):
+    _fields_ = [("bits", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32)]
+
+
+class _CCacheBatch(C.Structure):
+    _fields_ = [("tables", C.c_void_p), ("table_width", C.c_int64), ("lengths", C.c_void_p),
+                ("indptr", C.c_void_p), ("sequences", C.c_int64), ("tokens", C.c_int64)]
+
+
+class _CHeadRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _CAttendOptions(C.Structure):
+    _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int64),
+                ("prefix", C.c_void_p), ("slopes", C.c_void_p)]
 
 
 @dataclass(frozen=True)
@@ -89,6 +107,18 @@ _SIGNATURES = {
     "bifeat_check_lists": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_void_p]),
     "bifeat_scale_profile": (C.c_int, [C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_void_p,
                                        C.c_int64, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bifeat_cache_create": (C.c_int, [C.POINTER(_CCacheSpec), C.POINTER(C.c_void_p)]),
+    "bifeat_cache_destroy": (None, [C.c_void_p]),
+    "bifeat_cache_page_bytes": (C.c_int64, [C.c_void_p]),
+    "bifeat_cache_set_option": (C.c_int, [C.c_void_p, C.c_char_p, C.c_int]),
+    "bifeat_cache_reserve": (C.c_int, [C.c_void_p, C.c_void_p]),
+    "bifeat_cache_check": (C.c_int, [C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.c_void_p]),
+    "bifeat_cache_write": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.POINTER(_CHeadRows),
+                                     C.POINTER(_CHeadRows), C.c_int32, C.c_void_p]),
+    "bifeat_cache_read": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.c_void_p, C.c_void_p,
+                                    C.c_int32, C.c_void_p]),
+    "bifeat_cache_attend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.POINTER(_CHeadRows),
+                                      C.c_int32, C.c_int32, C.POINTER(_CAttendOptions), C.c_void_p, C.c_void_p]),
     "bifeat_strerror": (C.c_char_p, [C.c_int]),
     "bifeat_set_option": (C.c_int, [C.c_void_p, C.c_char_p, C.c_int]),
 }

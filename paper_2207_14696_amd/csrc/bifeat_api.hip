@@ -322,6 +322,13 @@ bool dtype_ok(int32_t d) { return d == BIFEAT_F32 || d == BIFEAT_F16; }
 
 }  // namespace
 
+// for the other translation units with entry points
+namespace bf {
+int record_hip_error(hipError_t e, const char *what) { return hip_fail(e, what); }
+int take_block(void **out) { return pool_take(out); }
+void give_block(void *blk) { pool_give(blk); }
+}  // namespace bf
+
 extern "C" {
 
 int bifeat_params_create(const bifeat_scheme *scheme, int64_t D, bifeat_params **out) {

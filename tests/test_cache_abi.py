@@ -1,0 +1,119 @@
+"""The paged cache without a GPU: sizes, the refusals that come before any GPU call, and the reference that the GPU
+tests compare with (against a second evaluation of the definition)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+import cache_reference as ref
+
+
+@pytest.fixture(scope="module")
+def bf():
+    import os
+    import paper_2207_14696_amd as m
+    if not os.path.exists(m.library_path()):
+        from paper_2207_14696_amd.build import build
+        build()
+    m.load_library()
+    return m
+
+
+def test_sizes_and_specs(bf):
+    assert bf.PagedCache(8, 8, 128, 64).page_bytes == 8 * 64 * (2 * 128 + 16)
+    assert bf.PagedCache(4, 2, 100, 16).page_bytes == 2 * 16 * (2 * 64 + 16)
+    assert bf.PagedCache(4, 1, 1, 1024).page_bytes == 1024 * (2 * 16 + 16)
+    for bad in [(2, 1, 64, 16), (16, 1, 64, 16), (8, 0, 64, 16), (8, 1025, 64, 16), (8, 1, 0, 16), (8, 1, 257, 16), (8, 1, 64, 8),
+                (8, 1, 64, 48), (8, 1, 64, 2048)]:
+        with pytest.raises(bf.BifeatError) as e:
+            bf.PagedCache(*bad)
+        assert e.value.status == bf.EINVAL
+
+
+def test_argument_errors_come_before_any_gpu_call(bf):
+    from paper_2207_14696_amd.binding import _CAttendOptions, _CCacheBatch, _CHeadRows
+    lib = bf.load_library()
+    c = bf.PagedCache(8, 2, 64, 16)
+    h = c._h
+
+    def batch(**kw):
+        d = dict(tables=16, table_width=4, lengths=16, indptr=None, sequences=2, tokens=2)
+        d.update(kw)
+        return C.byref(_CCacheBatch(**d))
+
+    def rows(data=16, t=128, s=64):
+        return C.byref(_CHeadRows(data, t, s))
+
+    def options(scale=1.0, softcap=0.0, window=0, prefix=None, slopes=None):
+        return C.byref(_CAttendOptions(scale, softcap, window, prefix, slopes))
+
+    def write(h=h, pages=16, n=9, b=None, k=None, v=None, t=0):
+        return lib.bifeat_cache_write(h, pages, n, b or batch(), k or rows(), v or rows(), t, None)
+
+    def read(h=h, pages=16, n=9, b=None, k=16, v=16, t=0):
+        return lib.bifeat_cache_read(h, pages, n, b or batch(), k, v, t, None)
+
+    def attend(h=h, pages=16, n=9, b=None, q=None, heads=4, t=0, o=None, out=16):
+        return lib.bifeat_cache_attend(h, pages, n, b or batch(), q or rows(), heads, t, o or options(), out, None)
+
+    for call in (write, read, attend):
+        assert call(h=None) == -1
+        assert call(t=3) == -1 and call(t=-1) == -1
+        assert call(pages=8) == -1 and call(pages=None) == -1 and call(n=-1) == -1 and call(n=1 << 31) == -1
+        for b in (batch(tokens=-1), batch(sequences=-1), batch(table_width=-1), batch(tokens=3), batch(sequences=0), batch(lengths=None),
+                  batch(tables=None), batch(lengths=4), batch(indptr=4), batch(tables=2), batch(tokens=1 << 31)):
+            assert call(b=b) == -1
+        assert call(b=batch(tokens=0, tables=None, lengths=None)) == 0
+    for r in (rows(data=None), rows(data=2), rows(t=-1), rows(s=-1)):
+        assert write(k=r) == -1 and write(v=r) == -1 and attend(q=r) == -1
+    assert read(k=None) == -1 and read(v=None) == -1 and read(k=2) == -1
+    assert attend(out=None) == -1 and attend(out=1, t=1) == -1
+    assert attend(heads=0) == -1 and attend(heads=3) == -1 and attend(heads=-2) == -1
+    for o in (options(scale=float("inf")), options(softcap=-1.0), options(softcap=float("nan")), options(softcap=float("inf")),
+              options(window=-1), options(prefix=4), options(slopes=2)):
+        assert attend(o=o) == -1
+    assert lib.bifeat_cache_attend(h, 16, 9, batch(), rows(), 4, 0, None, 16, None) == -1
+    assert lib.bifeat_cache_check(None, 1, batch(), None) == -1 and lib.bifeat_cache_check(h, -1, batch(), None) == -1
+    assert lib.bifeat_cache_check(h, 1, None, None) == -1
+    assert lib.bifeat_cache_set_option(h, b"validate", 2) == -1 and lib.bifeat_cache_set_option(h, b"other", 1) == -1
+    assert lib.bifeat_cache_set_option(h, b"validate", 1) == 0 and lib.bifeat_cache_set_option(h, b"validate", 0) == 0
+    assert lib.bifeat_cache_page_bytes(None) == -1 and lib.bifeat_cache_create(None, None) == -1
+    assert lib.bifeat_cache_reserve(None, None) == -1
+    lib.bifeat_cache_destroy(None)
+
+
+def test_a_destroyed_cache_is_refused(bf):
+    c = bf.PagedCache(8, 2, 64, 16)
+    c.__del__()
+    assert c._h is None
+    with pytest.raises(bf.BifeatError) as e:
+        c.set_option("validate", 0)
+    assert e.value.status == bf.EINVAL
+
+
+@pytest.mark.parametrize("bits", [4, 8])
+def test_reference_quantiser(bits):
+    rng = np.random.default_rng(bits)
+    x = rng.standard_normal((200, 50)).astype(np.float32)
+    q, scale, mn = ref.quantise(x, bits)
+    top = (1 << bits) - 1
+    back = mn[:, None].astype(np.float64) + q * scale[:, None].astype(np.float64)
+    assert (np.abs(back - x) <= 0.5001 * (np.ptp(x, axis=1) / top)[:, None]).all()
+    assert (q.min(1) == 0).all() and (q.max(1) == top).all()      # the range's ends are levels
+    p = ref.pack(q, bits)
+    j = np.arange(50)
+    assert np.array_equal(p[:, j * bits // 8] >> (j * bits % 8).astype(np.uint8) & top, q)
+    assert p.shape[1] % 16 == 0
+
+
+def test_reference_attention_is_softmax_attention():
+    torch = pytest.importorskip("torch")
+    rng = np.random.default_rng(0)
+    n, m, H, G, d = 5, 9, 2, 3, 8
+    q, k, v = rng.standard_normal((n, H * G, d)), rng.standard_normal((m, H, d)), rng.standard_normal((m, H, d))
+    tq, tk, tv = (torch.from_numpy(x).transpose(0, 1) for x in (q, np.repeat(k, G, 1), np.repeat(v, G, 1)))
+    mask = torch.ones(n, m, dtype=torch.bool).tril(m - n)
+    want = torch.softmax((tq @ tk.transpose(1, 2) * 0.4).masked_fill(~mask, -torch.inf), -1) @ tv
+    assert np.allclose(ref.attend(q, k, v, n, m, 0.4), want.transpose(0, 1).numpy(), atol=1e-12)
+    assert not ref.attend(q, k[:3], v[:3], n, 3, 0.4)[:2].any()
+    assert np.allclose(ref.attend(q, k, v, n, m, 0.4, window=1), np.repeat(v[m - n:], G, 1))
