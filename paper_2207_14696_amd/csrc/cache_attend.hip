@@ -1,92 +1,130 @@
-// Attention of new tokens over the paged cache.
-#include "cache.hpp"
+// Attention over the paged cache: which kernel, how many workgroups, and the join of what several of them did of one item.
+#include <algorithm>
+
+#include "cache_attend.hpp"
 
 namespace bf {
 namespace {
 
-// A wave a query row: 64 positions a step, one a lane; then a lane 4 of the values' columns.
-template <typename T, int BITS>
-__global__ __launch_bounds__(64) void cache_attend_kernel(AttendCall a) {
-    __shared__ float qs[256];
-    const CachePages &c = a.c;
-    const int Hq = c.heads * a.group, lane = threadIdx.x;
-    const int64_t t = blockIdx.x / Hq;
-    const int hq = (int)(blockIdx.x % Hq), head = hq / a.group;
-    const int seq = sequence_of(a.b, t);
-    const int64_t len = a.b.length(seq, c.ps_log2), pos = len - a.b.count(seq) + (t - a.b.first(seq));
-    const T *q = static_cast<const T *>(a.q.data) + t * a.q.token_stride + hq * a.q.head_stride;
-    float qsum = 0.f;
-    for (int j = lane; j < c.d; j += 64) {
-        qs[j] = to_float(q[j]);
-        qsum += qs[j];
+constexpr int kCUs = 256;
+constexpr int kRowsWorkgroups = 3 * kCUs;  // as many as run at a time
+
+// One workgroup a query row of an item that was shared: its parts are those of the workgroups [w0, w1], each with sums about a
+// maximum of its own.
+template <int R, int TOK>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPlan plan, int dp) {
+    __shared__ float weight[1024], red[8];
+    __shared__ float part[4][256];
+    __shared__ int sh[8];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r = blockIdx.x % R, item = (int)(blockIdx.x / R % plan.items), head = (int)(blockIdx.x / R / plan.items);
+    // the item's sequence, and the units of the head's items before it
+    const int seq = sequence_of_item<R>(a, item);
+    const int rt = item - first_item<R>(a, seq);
+    const View v = view_of<R, TOK>(a, seq, rt);
+    const int rows = v.n * a.group;
+    if (v.units == 0 || rt * R + r >= rows) return;
+    const int per = (plan.items + 255) / 256, i0 = tid * per, i1 = i0 + per < plan.items ? i0 + per : plan.items;
+    int sum = 0, before = 0;
+    if (i0 < i1) {
+        int s = sequence_of_item<R>(a, i0);
+        int next = first_item<R>(a, s + 1);
+        for (int i = i0; i < i1; i++) {
+            while (i >= next && s + 1 < a.b.B) next = first_item<R>(a, ++s + 1);
+            const int u = view_of<R, TOK>(a, s, i - first_item<R>(a, s)).units;
+            sum += u;
+            if (i < item) before += u;
+        }
     }
-    for (int m = 1; m < 64; m *= 2) qsum += __shfl_xor(qsum, m);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m), before += __shfl_xor(before, m);
+    if (lane == 0) sh[wave] = sum, sh[4 + wave] = before;
     __syncthreads();
-    float top = -INFINITY, sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    const int64_t prefix = a.prefix ? a.prefix[seq] : 0;
-    int64_t end = pos + 1 > prefix ? pos + 1 : prefix;
-    if (end > len) end = len;
-    if (pos < 0) end = 0;
-    const float slope = a.slopes ? a.slopes[hq] : 0.f;
-    for (int64_t j0 = 0; j0 < end; j0 += 64) {
-        const int64_t j = j0 + lane;
-        const bool seen = j < end && ((j <= pos && (a.window == 0 || j > pos - a.window)) || j < prefix);
-        float x = -INFINITY;
-        if (seen) {
-            const uint8_t *block = c.block(a.b.tables[seq * a.b.width + (j >> c.ps_log2)], head);
-            const int slot = (int)(j & (c.ps() - 1));
-            const uint8_t *codes = block + c.codes(0) + (int64_t)slot * c.rb;
-            const float *f = reinterpret_cast<const float *>(block + c.floats(0)) + slot;
-            float dot = 0.f;
-            for (int i = 0; i < c.d; i++) dot += qs[i] * (float)(codes[i * BITS / 8] >> (i * BITS % 8) & ((1 << BITS) - 1));
-            x = a.scale * (f[0] * dot + f[c.ps()] * qsum);
-            if (a.softcap > 0.f) x = a.softcap * tanhf(x / a.softcap);
-            x += slope * (float)(j - pos);
+    const int64_t total = (int64_t)sh[0] + sh[1] + sh[2] + sh[3];
+    const int64_t u0 = total * head + sh[4] + sh[5] + sh[6] + sh[7], u1 = u0 + v.units - 1, all = total * a.c.heads;
+    const int64_t nw = all < plan.nw ? all : plan.nw;
+    const int w0 = (int)(((u0 + 1) * nw - 1) / all), w1 = (int)(((u1 + 1) * nw - 1) / all);
+    if (w0 == w1) return;  // one workgroup had it all
+    const int64_t stride = R * (dp + 2);
+    auto at = [&](int w) { return plan.partial + ((int64_t)w * 2 + (w == w0)) * stride + (int64_t)r * (dp + 2); };
+    float top = kNothing;
+    for (int w = w0 + tid; w <= w1; w += 256) top = fmaxf(top, at(w)[dp]);
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+    if (lane == 0) red[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    // weights of 1024 parts at a time; each wave every fourth part, a lane 4 columns (d <= 256)
+    float acc[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
+    for (int from = w0; from <= w1; from += 1024) {
+        const int to = from + 1024 <= w1 ? from + 1024 : w1 + 1;
+        __syncthreads();
+        for (int w = from + tid; w < to; w += 256) {
+            const float e = __builtin_amdgcn_exp2f(at(w)[dp] - top);
+            weight[w - from] = e;
+            den += e * at(w)[dp + 1];
         }
-        float m = x;
-        for (int o = 1; o < 64; o *= 2) m = fmaxf(m, __shfl_xor(m, o));
-        if (!__any(seen)) continue;
-        const float now = fmaxf(fmaxf(top, m), -1e30f), keep = expf(top - now), p = seen ? expf(x - now) : 0.f;
-        top = now;
-        float s = p;
-        for (int o = 1; o < 64; o *= 2) s += __shfl_xor(s, o);
-        sum = sum * keep + s;
-        for (int k = 0; k < 4; k++) acc[k] *= keep;
-        for (int i = 0; i < 64; i++) {
-            const float w = __shfl(p, i);
-            if (!__shfl((int)seen, i)) continue;
-            const int64_t ji = j0 + i;
-            const uint8_t *block = c.block(a.b.tables[seq * a.b.width + (ji >> c.ps_log2)], head);
-            const int slot = (int)(ji & (c.ps() - 1));
-            const uint8_t *codes = block + c.codes(1) + (int64_t)slot * c.rb;
-            const float *f = reinterpret_cast<const float *>(block + c.floats(1)) + slot;
-            for (int k = 0; k < 4; k++) {
-                const int col = lane + 64 * k;
-                if (col < c.d) acc[k] += w * fmaf((float)(codes[col * BITS / 8] >> (col * BITS % 8) & ((1 << BITS) - 1)), f[0], f[c.ps()]);
-            }
+        __syncthreads();
+        for (int w = from + wave; w < to; w += 4) {
+            const float e = weight[w - from];
+            const float *x = at(w);
+#pragma unroll
+            for (int k = 0; k < 4; k++)
+                if (lane + 64 * k < a.c.d) acc[k] += e * x[lane + 64 * k];
         }
     }
-    T *out = static_cast<T *>(a.out) + (t * Hq + hq) * c.d;
-    for (int k = 0; k < 4; k++) {
-        const int col = lane + 64 * k;
-        if (col < c.d) out[col] = from_float<T>(sum != 0.f ? acc[k] / sum : 0.f);
-    }
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) den += __shfl_xor(den, m);
+    if (lane == 0) red[4 + wave] = den;
+#pragma unroll
+    for (int k = 0; k < 4; k++) part[wave][lane + 64 * k] = acc[k];
+    __syncthreads();
+    den = red[4] + red[5] + red[6] + red[7];
+    const int row = rt * R + r;
+    const int64_t dst = ((a.b.first(seq) + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
+    if (tid < a.c.d) store_result(a, dst + tid, den != 0.f ? (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / den : 0.f);
 }
+
+template <int R, int TOK>
+void launch_join(const AttendCall &a, const AttendPlan &p, int dp) {
+    attend_join_kernel<R, TOK><<<(unsigned)((int64_t)p.items * a.c.heads * R), 256, 0, a.s>>>(a, p, dp);
+}
+
+// numbers of a head's items, an upper bound where the batch is ragged
+int items_of(const AttendCall &a, int R) {
+    if (a.b.indptr) return (int)(a.b.tokens * a.group / R) + a.b.B;
+    return a.b.B * ((a.b.n * a.group + R - 1) / R);
+}
+
+size_t partial_floats() { return (size_t)kRowsWorkgroups * 2 * kRowsR * (256 + 2); }
 
 }  // namespace
 
-hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
-    const unsigned grid = (unsigned)(a.b.tokens * a.c.heads * a.group);
-#define BF_GO(T)                                                                    \
-    if (h->spec.bits == 8) cache_attend_kernel<T, 8><<<grid, 64, 0, a.s>>>(a);      \
-    else cache_attend_kernel<T, 4><<<grid, 64, 0, a.s>>>(a)
-    if (a.dtype == BIFEAT_F32) { BF_GO(float); }
-    else if (a.dtype == BIFEAT_F16) { BF_GO(Half16); }
-    else { BF_GO(Brain16); }
-#undef BF_GO
-    return hipGetLastError();
+bool ensure_partial(bifeat_cache *h, hipStream_t s) {
+    if (h->d_partial) return true;
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone) return false;
+    void *p = nullptr;
+    if (hipMalloc(&p, sizeof(float) * partial_floats()) != hipSuccess) {
+        (void)hipGetLastError();
+        return false;
+    }
+    h->d_partial = (float *)p;
+    return true;
 }
 
-bool ensure_partial(bifeat_cache *, hipStream_t) { return true; }
+hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
+    const int dp = a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256, bits = h->spec.bits;
+    AttendPlan p;
+    p.items = items_of(a, kRowsR);
+    const int64_t most = ((a.b.width << a.c.ps_log2) + kRowsTok - 1) / kRowsTok, all = (int64_t)p.items * a.c.heads;
+    // contexts of a few units, and calls that find no workspace: an item a workgroup, nothing to join
+    const bool split = most > 4 && ensure_partial(h, a.s);
+    p.partial = split ? h->d_partial : nullptr;
+    p.nw = (int)(split ? std::min<int64_t>(all * most, kRowsWorkgroups) : all);
+    launch_attend_rows(a, p, bits, dp);
+    if (split) launch_join<kRowsR, kRowsTok>(a, p, dp);
+    return hipGetLastError();
+}
 
 }  // namespace bf

@@ -1,0 +1,265 @@
+// Attention over the paged cache: how the work is dealt to workgroups, and what the kernels share.
+//
+// Mathematics.  A cached row is x = mn + code * s.  Products with the keys and sums of the values are taken on the codes:
+//     q . k_t = s_t (q . code_t) + mn_t sum(q)            sum_t p_t v_t = sum_t (p_t s_t) code_t + sum_t p_t mn_t
+// so that the matrix cores see whole numbers, which fp16 holds exactly, and nothing is decoded.  A code's bits are read as
+// an fp16 number as they stand: a subnormal, code * 2^-24, which the matrix cores of gfx950 multiply as it is (the factor is
+// taken out in 32 bits).  One byte permutation makes two operands of two 8-bit codes; of 4-bit codes a mask makes two, or
+// two times 16, which is taken out of the other factor or of the sum.
+// The values' codes are weighted about the middle of their range (c = mn + 2^(bits-1) s): what a weight's rounding to fp16
+// is off by then meets at most half a row's range.
+#pragma once
+
+#include "cache.hpp"
+
+namespace bf {
+
+constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel for few rows
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kNothing = -1e30f;  // running maximum where nothing was seen: below any score, and finite
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float4v __attribute__((ext_vector_type(4)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+// Work: an item is R query rows of a sequence and a cached head (row r: new token r / group, query head r % group of the
+// head's), a unit is TOK positions of the cache that an item looks at.  The units of all items, in the order of heads,
+// then sequences, then rows, are dealt evenly to `nw` workgroups, each a run of them; contexts of any mixture of
+// lengths so keep all of them busy.  An item that several workgroups share is joined by a second kernel.
+struct AttendPlan {
+    int items;       // per head; of a ragged batch with numbers left free (see first_item)
+    int nw;
+    // null: a workgroup has one item, all of it (contexts are short, or there is no workspace)
+    float *partial;  // [nw][2][R][DP + 2]: sums, running maximum, sum of weights of an item begun before / not ended by a workgroup
+};
+
+// Sequence b's items have numbers from first_item(b) on.  In a ragged batch floor(rows before it / R) + b leaves every
+// sequence room for its own, rounded up, without a sum over the batch.
+template <int R>
+__device__ inline int first_item(const AttendCall &a, int b) {
+    if (!a.b.indptr) return b * ((a.b.n * a.group + R - 1) / R);
+    return (int)(a.b.indptr[b] * a.group / R) + b;
+}
+
+// What an item's rows see.
+struct View {
+    int len, n;          // the sequence's
+    int first, last;     // positions of the item's first and last query
+    int prefix;
+    int skip_at, skip;   // units: from the skip_at-th on, `skip` are left out
+    int units;
+};
+
+template <int R, int TOK>
+__device__ inline View view_of(const AttendCall &a, int b, int rt) {
+    View v;
+    v.len = (int)a.b.length(b, a.c.ps_log2);
+    v.n = (int)a.b.count(b);
+    const int rows = v.n * a.group;
+    if (rt * R >= rows) {
+        v.units = 0;
+        return v;
+    }
+    const int end_row = rt * R + R < rows ? rt * R + R : rows;
+    v.first = v.len - v.n + rt * R / a.group;
+    v.last = v.len - v.n + (end_row - 1) / a.group;
+    int64_t pre = a.prefix ? a.prefix[b] : 0;
+    v.prefix = pre < 0 ? 0 : pre > v.len ? v.len : (int)pre;
+    int end = v.last + 1 > v.prefix ? v.last + 1 : v.prefix;
+    if (v.last < 0) end = 0;
+    const int64_t low = a.window ? (int64_t)v.first - a.window + 1 : 0;
+    const int total = (end + TOK - 1) / TOK, from = low > 0 ? (int)(low / TOK) : 0;
+    v.skip_at = (v.prefix + TOK - 1) / TOK;
+    v.skip = from < total ? from - v.skip_at : total - v.skip_at;
+    if (v.skip < 0) v.skip = 0;
+    v.units = total - v.skip > 1 ? total - v.skip : 1;  // an item that sees nothing still has its zeros to write
+    return v;
+}
+
+struct Place {
+    int item, seq, rt;  // the item, its sequence, its number in it
+    int unit;           // of the item
+};
+
+// The sequence that item `i` of a head belongs to.
+template <int R>
+__device__ inline int sequence_of_item(const AttendCall &a, int i) {
+    if (!a.b.indptr) return i / ((a.b.n * a.group + R - 1) / R);
+    int lo = 0, hi = a.b.B;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (first_item<R>(a, mid) <= i) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+// Sums the units of a head's items: the total, and the place of unit `want` modulo it.  All threads of a workgroup.
+// sh: 16 ints.
+template <int R, int TOK>
+__device__ inline int64_t locate(const AttendCall &a, const AttendPlan &p, int64_t w, int64_t *start, int64_t *end, int *head, Place *at,
+                                 int *sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+    if (!p.partial) {
+        at->item = (int)(w % p.items);
+        at->seq = sequence_of_item<R>(a, at->item);
+        at->rt = at->item - first_item<R>(a, at->seq);
+        at->unit = 0;
+        *head = (int)(w / p.items);
+        *start = 0;
+        *end = view_of<R, TOK>(a, at->seq, at->rt).units;
+        return *end;
+    }
+    const int per = (p.items + (int)blockDim.x - 1) / (int)blockDim.x;
+    const int i0 = tid * per, i1 = i0 + per < p.items ? i0 + per : p.items;
+    int sum = 0;
+    const int seq = i0 < i1 ? sequence_of_item<R>(a, i0) : 0;
+    int s = seq, next = i0 < i1 ? first_item<R>(a, s + 1) : 0;
+    for (int i = i0; i < i1; i++) {
+        while (i >= next && s + 1 < a.b.B) next = first_item<R>(a, ++s + 1);
+        sum += view_of<R, TOK>(a, s, i - first_item<R>(a, s)).units;
+    }
+    int upto = sum;
+#pragma unroll
+    for (int m = 1; m < 64; m *= 2) {
+        const int x = __shfl_up(upto, m);
+        if (lane >= m) upto += x;
+    }
+    if (lane == 63) sh[wave] = upto;
+    __syncthreads();
+    int64_t total = 0, before = upto - sum;
+    for (int k = 0; k < waves; k++) {
+        if (k < wave) before += sh[k];
+        total += sh[k];
+    }
+    const int64_t all = total * a.c.heads, nw = all < p.nw ? all : p.nw;  // (none has nothing between two that have)
+    *start = w < nw ? w * all / nw : all;
+    *end = w < nw ? (w + 1) * all / nw : all;
+    *head = total ? (int)(*start / total) : 0;
+    const int64_t want = total && *start < all ? *start % total : -1;
+    if (want >= before && want < before + sum) {
+        int left = (int)(want - before);
+        s = seq, next = first_item<R>(a, s + 1);
+        for (int i = i0; i < i1; i++) {
+            while (i >= next && s + 1 < a.b.B) next = first_item<R>(a, ++s + 1);
+            const int rt = i - first_item<R>(a, s), u = view_of<R, TOK>(a, s, rt).units;
+            if (left < u) {
+                sh[8] = i, sh[9] = s, sh[10] = rt, sh[11] = left;
+                break;
+            }
+            left -= u;
+        }
+    }
+    __syncthreads();
+    if (want < 0) return total;
+    at->item = __builtin_amdgcn_readfirstlane(sh[8]);
+    at->seq = __builtin_amdgcn_readfirstlane(sh[9]);
+    at->rt = __builtin_amdgcn_readfirstlane(sh[10]);
+    at->unit = __builtin_amdgcn_readfirstlane(sh[11]);
+    return total;
+}
+
+// The next item that has units, of this head or the next.
+template <int R>
+__device__ inline void next_item(const AttendCall &a, int *head, Place *at) {
+    at->unit = 0;
+    at->rt++;
+    while (at->rt * R >= (int)a.b.count(at->seq) * a.group) {
+        at->rt = 0;
+        if (++at->seq == a.b.B) {
+            at->seq = 0;
+            ++*head;
+        }
+    }
+}
+
+// Power of two that brings `top` to [2^to, 2^(to+1)).
+__device__ inline float power_to(float top, int to) {
+    int e = top > 0.f ? ilogbf(top) : to;
+    e = e < -80 ? -80 : e > 80 ? 80 : e;
+    return ldexpf(1.f, to - e);
+}
+
+// codes -> fp16 operands ----------------------------------------------------------------------------------------------
+
+// the bytes lo and hi of a as two halves
+__device__ inline uint32_t bytes_of(uint32_t a, int lo) { return __builtin_amdgcn_perm(0u, a, 0x0c000c00u | lo | (lo + 1) << 16); }
+// byte i of a, byte i of b as two halves
+__device__ inline uint32_t pair_of(uint32_t a, uint32_t b, int i) { return __builtin_amdgcn_perm(b, a, 0x0c000c00u | i | (4 + i) << 16); }
+
+struct Words4 { uint32_t w[4]; };
+__device__ inline half8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __builtin_bit_cast(half8, Words4{{a, b, c, d}});
+}
+
+// The same as whole numbers less their middle (4-bit codes' times 16 where they come so), for 32-bit queries: 1024 + code is
+// the code's bits beside 1024's, and 1024 + middle is taken off exactly.  Of subnormal operands the matrix cores lose the bits
+// that a normal number would have in place of their leading zeros (4-bit codes: 7 of 24), and sums of products of codes that
+// are all positive leave 2^-24 of the codes' common part.
+__device__ inline half8 centred(half8 bits, half8 top) {
+    Words4 w = __builtin_bit_cast(Words4, bits);
+#pragma unroll
+    for (int i = 0; i < 4; i++) w.w[i] |= 0x64006400u;
+    return __builtin_bit_cast(half8, w) - top;
+}
+// what `top` is for codes of BITS bits in a row, and for eight 4-bit codes as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16
+__device__ inline half8 all_of(float x) {
+    const _Float16 m = (_Float16)x;
+    return half8{m, m, m, m, m, m, m, m};
+}
+__device__ inline half8 centre4() {
+    const _Float16 m = (_Float16)1032.f, n = (_Float16)1152.f;
+    return half8{m, m, n, n, m, m, n, n};
+}
+// the unit of a product with a code: codes are subnormals, or (NP = 2) whole numbers
+template <int NP> constexpr float kUnit = NP == 2 ? 1.f : 16777216.f;
+
+template <int N>
+__device__ inline void load_bytes(const uint8_t *p, uint32_t *w) {
+    if constexpr (N == 16) {
+        const uint4 q = *reinterpret_cast<const uint4 *>(p);
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+    } else if constexpr (N == 8) {
+        const uint2 q = *reinterpret_cast<const uint2 *>(p);
+        w[0] = q.x, w[1] = q.y;
+    } else if constexpr (N == 4) {
+        w[0] = *reinterpret_cast<const uint32_t *>(p);
+    } else if constexpr (N == 2) {
+        w[0] = *reinterpret_cast<const uint16_t *>(p);
+    } else {
+        w[0] = *p;
+    }
+}
+
+// one query's elements as floats, zeros from column a.c.d on
+template <int N>
+__device__ inline void load_query(const AttendCall &a, int64_t token, int head, int col, float (&x)[N]) {
+    const int64_t at = token * a.q.token_stride + head * a.q.head_stride + col;
+#pragma unroll
+    for (int k = 0; k < N; k += 8) {
+        float e[8];
+        const int left = a.c.d - col - k;
+        if (a.dtype == BIFEAT_F32) load8_any(static_cast<const float *>(a.q.data) + at + k, left, e);
+        else if (a.dtype == BIFEAT_F16) load8_any(static_cast<const Half16 *>(a.q.data) + at + k, left, e);
+        else load8_any(static_cast<const Brain16 *>(a.q.data) + at + k, left, e);
+#pragma unroll
+        for (int i = 0; i < 8; i++) x[k + i] = e[i];
+    }
+}
+
+__device__ inline void store_result(const AttendCall &a, int64_t at, float x) {
+    if (a.dtype == BIFEAT_F32) static_cast<float *>(a.out)[at] = x;
+    else if (a.dtype == BIFEAT_F16) static_cast<Half16 *>(a.out)[at] = from_float<Half16>(x);
+    else static_cast<Brain16 *>(a.out)[at] = from_float<Brain16>(x);
+}
+
+// y * f in units of log2, with the cap and the bias by distance (slope in the same units)
+__device__ inline float capped(float x, float cap) {  // cap * tanh(x / cap), both in units of log2
+    const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e / cap));
+    return cap - 2.f * cap * __builtin_amdgcn_rcpf(e + 1.f);
+}
+
+void launch_attend_rows(const AttendCall &a, const AttendPlan &p, int bits, int dp);
+
+}  // namespace bf

@@ -1,0 +1,335 @@
+// Attention over the paged cache for few query rows a cached head (single tokens, a few drafted ones): 16 rows an item.
+//
+// Bound by the cache's bytes: a cached row is fetched once for all query heads that share it.  Everything stays in
+// registers.  A wave takes 32 positions a step, the four waves of a workgroup every fourth step; a step's keys make room
+// for the next one's as soon as the scores are there, its values when the sums are, so that one or the other is always on
+// its way.  Scores are keys x queries (positions the rows of the 16 x 16 product), so that a lane ends up with
+// four positions of one query, which is how the second product wants its weights: nothing is moved between lanes.
+#pragma once
+
+#include "cache_attend.hpp"
+
+namespace bf {
+
+
+
+template <int BITS, int DP>
+struct RowLanes {
+    static constexpr int KB = DP / 4 * BITS / 8;   // bytes of a key that a lane reads (its quarter of the columns)
+    static constexpr int KL = KB < 16 ? KB : 16;   // in loads of so many
+    static constexpr int VB = DP / 16 * BITS / 8;  // bytes of a value (its sixteenth)
+    static constexpr int KS = DP / 32;             // products over the columns
+    static constexpr int VT = DP / 16;             // tiles of the values' columns
+    static constexpr int VW = VB < 4 ? 1 : VB / 4;
+};
+
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries)
+template <int BITS, int DP, int NP>
+__global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
+    using L = RowLanes<BITS, DP>;
+    constexpr int R = kRowsR, TOK = kRowsTok;
+    constexpr float kMiddle = 1 << (BITS - 1);
+    __shared__ float sums[4][R][DP + 4];
+    __shared__ float tops[4][R], totals[4][R];
+    __shared__ float params[4][4][32];  // a wave's step: key scale, key minimum, value scale, value minimum
+    __shared__ int sh[16];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
+    int64_t cur, end;
+    int head;
+    Place at;
+    locate<R, TOK>(a, plan, blockIdx.x, &cur, &end, &head, &at, sh);
+
+    // byte offsets in a row; past its end (columns the row is too short for) any byte will do: the queries have zeros there,
+    // and the sums of such columns are not written
+    const int rb = a.c.rb;
+    uint32_t koff[L::KB / L::KL];
+#pragma unroll
+    for (int i = 0; i < L::KB / L::KL; i++) {
+        const int o = g * L::KB + i * L::KL;
+        koff[i] = n16 * rb + (o < rb ? o : 0);
+    }
+    const uint32_t voff = 4 * g * rb + (n16 * L::VB < rb ? n16 * L::VB : 0);
+    // lane l < 32 brings four positions' worth of one of the four floats
+    const uint32_t foff = ((lane >> 3 & 3) * 4u << a.c.ps_log2) + 16 * (lane & 3);
+
+    while (cur < end) {
+        const View v = view_of<R, TOK>(a, at.seq, at.rt);
+        const int units = v.units - at.unit < end - cur ? v.units - at.unit : (int)(end - cur);
+        const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
+        const int64_t token0 = a.b.first(at.seq);
+
+        // ---- the queries: lane (n16, g) has columns [g DP/4, (g+1) DP/4) of row n16, in the order of the keys' codes
+        const int row = row0 + n16;
+        const bool real = n16 < nrows;
+        const int qi = row / a.group, qh = head * a.group + row % a.group;
+        const int pos = real ? v.len - v.n + qi : -1;
+        half8 q[NP][L::KS];
+        float qsum = 0.f, f;
+        {
+            float x[DP / 4];
+#pragma unroll
+            for (int i = 0; i < DP / 4; i++) x[i] = 0.f;
+            if (real) load_query(a, token0 + qi, qh, g * (DP / 4), x);
+            float top = 0.f;
+#pragma unroll
+            for (int i = 0; i < DP / 4; i++) top = fmaxf(top, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+            const float up = power_to(top, 14);
+            f = a.scale * kLog2e * (kUnit<NP> / up);
+#pragma unroll
+            for (int i = 0; i < DP / 4; i++) {
+                const float y = x[i] * up;
+                const _Float16 hi = (_Float16)y;
+                const _Float16 lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
+                qsum += (float)hi + (float)lo;
+                // 4-bit codes come as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16 of eight
+                const int e = i % 8, slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
+                const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
+                q[0][i / 8][slot] = hi * down;
+                if constexpr (NP == 2) q[NP - 1][i / 8][slot] = lo * down;
+            }
+            qsum += __shfl_xor(qsum, 16);
+            qsum += __shfl_xor(qsum, 32);
+            qsum *= 1.f / kUnit<NP>;
+        }
+        const float slope = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+        const float cap = a.softcap * kLog2e;
+        const bool shaped = a.softcap > 0.f || a.slopes;
+        const int low = a.window && pos - a.window >= 0 ? (int)(pos - a.window) : -1;  // positions above it are in the window
+
+        float top = kNothing, total = 0.f, mins = 0.f, weights = 0.f, unit_of_s = 0.f;
+        float4v o[L::VT];
+#pragma unroll
+        for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
+
+        // ---- pages: lane 2 i + j has the page of the wave's i-th step from `paged` on, half j
+        int pages = 0, paged = -64;
+        const int32_t *table = a.b.tables + (int64_t)at.seq * a.b.width;
+        auto base_of = [&](int u) {  // first position of the wave's step in unit u of the item
+            u += at.unit;
+            return (u < v.skip_at ? u : u + v.skip) * TOK + 32 * wave;
+        };
+        uint32_t kw[2][L::KB / 4], vw[8][L::VW];
+        float4 fw;
+        auto block_of = [&](int u, int j) -> const uint8_t * {
+            return a.c.block(__builtin_amdgcn_readlane(pages, 2 * (u - paged) + j), head);
+        };
+        auto slot_of = [&](int u, int j) { return (base_of(u) + 16 * j) & (a.c.ps() - 1); };
+        auto load_keys = [&](int u) {
+            if (u - paged >= 32) {
+                paged = u;
+                int j = base_of(u + (lane >> 1)) + 16 * (lane & 1);
+                j = j < v.len ? j : v.len - 1;
+                pages = table[j >> a.c.ps_log2];
+            }
+            const uint8_t *fp[2];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int slot = slot_of(u, j);
+                const uint8_t *block = block_of(u, j), *kp = block + (int64_t)slot * rb;
+#pragma unroll
+                for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(kp + koff[i], &kw[j][i * L::KL / 4]);
+                fp[j] = block + a.c.floats(0) + 4 * slot;
+            }
+            fw = *reinterpret_cast<const float4 *>((lane & 4 ? fp[1] : fp[0]) + foff);
+        };
+        auto load_values = [&](int u) {
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const uint8_t *vp = block_of(u, j) + a.c.codes(1) + (int64_t)slot_of(u, j) * rb;
+#pragma unroll
+                for (int i = 0; i < 4; i++) load_bytes<L::VB>(vp + voff + i * rb, vw[4 * j + i]);
+            }
+        };
+
+        auto step = [&](int u) {
+            const int base = base_of(u);
+            // all rows see all 32 positions?
+            const bool whole = base + 32 <= v.len && v.first >= 0 &&
+                               ((base + 31 <= v.first && (!a.window || base > v.last - a.window)) || base + 32 <= v.prefix);
+            wave_sync();
+            if (lane < 32) *reinterpret_cast<float4 *>(&params[wave][lane >> 3][4 * (lane & 7)]) = fw;
+            wave_sync();
+            float ks[8], km[8], vs[8], vm[8];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                float4 p[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) p[i] = *reinterpret_cast<const float4 *>(&params[wave][i][16 * j + 4 * g]);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int e = 4 * j + i;
+                    ks[e] = (&p[0].x)[i];
+                    km[e] = NP == 2 ? fmaf(ks[e], kMiddle, (&p[1].x)[i]) : (&p[1].x)[i];
+                    vs[e] = (&p[2].x)[i];
+                    vm[e] = fmaf(vs[e], kMiddle, (&p[3].x)[i]);
+                }
+            }
+            uint32_t seen = 0xffu;
+            if (!whole) {
+                seen = 0;
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    const int t = base + 16 * (e / 4) + 4 * g + e % 4;
+                    const bool is = t < v.len && pos >= 0 && ((t <= pos && t > low) || t < v.prefix);
+                    seen |= (uint32_t)is << e;
+                    vs[e] = is ? vs[e] : 0.f;  // (the unit of the weights is not that of what the row does not see)
+                }
+            }
+            // ---- scores
+            float x[8];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                float4v acc{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < L::KS; c++) {
+                    half8 key;
+                    if constexpr (BITS == 8) {
+                        const uint32_t w0 = kw[j][2 * c], w1 = kw[j][2 * c + 1];
+                        key = operand(bytes_of(w0, 0), bytes_of(w0, 2), bytes_of(w1, 0), bytes_of(w1, 2));
+                    } else {
+                        const uint32_t w = kw[j][c], w8 = w >> 8;
+                        key = operand(w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u);
+                    }
+                    if constexpr (NP == 2) key = centred(key, BITS == 8 ? all_of(1152.f) : centre4());
+#pragma unroll
+                    for (int p = 0; p < NP; p++) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc, 0, 0, 0);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) x[4 * j + i] = f * fmaf(ks[4 * j + i], acc[i], km[4 * j + i] * qsum);
+            }
+            if (u + 1 < units) load_keys(u + 1);
+            if (shaped) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    if (a.softcap > 0.f) x[e] = capped(x[e], cap);
+                    x[e] = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x[e]);
+                }
+            }
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = seen >> e & 1 ? x[e] : -INFINITY;
+            }
+            // ---- the running maximum, and the unit that the values' scales are counted in: both may lag (weights up to
+            // 2^8 and scales up to 2^7 units stay within fp16), and are brought up for all lanes of a row together
+            float big = x[0], wide = vs[0];
+#pragma unroll
+            for (int e = 1; e < 8; e++) big = fmaxf(big, x[e]), wide = fmaxf(wide, vs[e]);
+            if (__any(big > top + 8.f || wide * unit_of_s > 128.f || (unit_of_s == 0.f && wide > 0.f))) {
+                big = fmaxf(big, __shfl_xor(big, 16));
+                big = fmaxf(big, __shfl_xor(big, 32));
+                wide = fmaxf(wide, __shfl_xor(wide, 16));
+                wide = fmaxf(wide, __shfl_xor(wide, 32));
+                const float now = fmaxf(top, big), keep = __builtin_amdgcn_exp2f(top - now);
+                float by = keep;
+                if (wide > 0.f) {
+                    const float unit = power_to(wide, 6);
+                    if (unit_of_s == 0.f) {
+                        unit_of_s = unit;  // (nothing is summed yet but positions of scale 0)
+                    } else if (unit < unit_of_s) {
+                        by = keep * (unit / unit_of_s);
+                        unit_of_s = unit;
+                    }
+                }
+                top = now;
+                total *= keep;
+                mins *= keep;
+                weights *= by;
+#pragma unroll
+                for (int t = 0; t < L::VT; t++) o[t] *= by;
+            }
+            // ---- weights
+            half8 w[NP];
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const float p = __builtin_amdgcn_exp2f(x[e] - top);
+                float pw = p * (vs[e] * unit_of_s), pm = p * vm[e];
+                if (!whole && !(seen >> e & 1)) pw = pm = 0.f;  // (an infinity or NaN that the row does not see)
+                total += p;
+                mins += pm;
+                w[0][e] = (_Float16)pw;
+                if constexpr (NP == 2) w[NP - 1][e] = (_Float16)(pw - (float)w[0][e]);
+            }
+            if constexpr (NP == 1)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    weights = __builtin_amdgcn_fdot2(half2v{w[0][e], w[0][e + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, weights, false);
+            // ---- values: lane (n16, g) has columns [n16 DP/16, ...) of eight positions
+#pragma unroll
+            for (int t = 0; t < L::VT; t++) {
+                half8 val;
+                if constexpr (BITS == 8) {
+                    val = operand(pair_of(vw[0][t / 4], vw[1][t / 4], t % 4), pair_of(vw[2][t / 4], vw[3][t / 4], t % 4),
+                                  pair_of(vw[4][t / 4], vw[5][t / 4], t % 4), pair_of(vw[6][t / 4], vw[7][t / 4], t % 4));
+                } else {
+                    const int i = t / 2 % 4, d = t / 8;
+                    const uint32_t mask = t & 1 ? 0x00f000f0u : 0x000f000fu;
+                    val = operand(pair_of(vw[0][d], vw[1][d], i) & mask, pair_of(vw[2][d], vw[3][d], i) & mask,
+                                  pair_of(vw[4][d], vw[5][d], i) & mask, pair_of(vw[6][d], vw[7][d], i) & mask);
+                }
+                if constexpr (NP == 2) val = centred(val, all_of(BITS == 8 || (t & 1) ? 1152.f : 1032.f));
+#pragma unroll
+                for (int p = 0; p < NP; p++)
+                    o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[p], o[t], 0, 0, 0);
+            }
+        };
+
+        if (v.len > 0) {
+            load_keys(0);
+            load_values(0);
+            for (int u = 0; u < units; u++) {
+                if (base_of(u) < v.len) step(u);  // (of an item's last unit some waves may have no positions)
+                if (u + 1 < units) load_values(u + 1);
+            }
+        }
+
+        // ---- the four waves' parts joined
+        total += __shfl_xor(total, 16);
+        total += __shfl_xor(total, 32);
+        mins += __shfl_xor(mins, 16);
+        mins += __shfl_xor(mins, 32);
+        weights += __shfl_xor(weights, 16);
+        weights += __shfl_xor(weights, 32);
+        const float per = unit_of_s != 0.f ? 1.f / unit_of_s : 0.f;
+        const float rest = mins - weights * (kMiddle * per);  // (NP == 2: the codes were less their middle already)
+#pragma unroll
+        for (int t = 0; t < L::VT; t++) {
+            const float back = kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f) * per;
+#pragma unroll
+            for (int i = 0; i < 4; i++) sums[wave][n16][(4 * g + i) * L::VT + t] = fmaf(o[t][i], back, rest);
+        }
+        if (g == 0) {
+            tops[wave][n16] = top;
+            totals[wave][n16] = total;
+        }
+        __syncthreads();
+        {
+            const int r = threadIdx.x >> 4, c0 = threadIdx.x & 15;
+            const float t0 = tops[0][r], t1 = tops[1][r], t2 = tops[2][r], t3 = tops[3][r];
+            const float now = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
+            const float e0 = __builtin_amdgcn_exp2f(t0 - now), e1 = __builtin_amdgcn_exp2f(t1 - now);
+            const float e2 = __builtin_amdgcn_exp2f(t2 - now), e3 = __builtin_amdgcn_exp2f(t3 - now);
+            const float all = totals[0][r] * e0 + totals[1][r] * e1 + totals[2][r] * e2 + totals[3][r] * e3;
+            const bool whole = at.unit == 0 && units == v.units;
+            float *part = whole ? nullptr : plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2)) + r * (DP + 2);
+            const int64_t dst = ((token0 + (row0 + r) / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + (row0 + r) % a.group) * a.c.d;
+            const float inv = all != 0.f ? 1.f / all : 0.f;
+            if (r < nrows) {
+                for (int c = c0; c < a.c.d; c += 16) {
+                    const float x = sums[0][r][c] * e0 + sums[1][r][c] * e1 + sums[2][r][c] * e2 + sums[3][r][c] * e3;
+                    if (whole) store_result(a, dst + c, x * inv);
+                    else part[c] = x;
+                }
+                if (!whole && c0 == 0) part[DP] = now, part[DP + 1] = all;
+            }
+        }
+        __syncthreads();
+        cur += units;
+        if (cur < end) next_item<R>(a, &head, &at);
+    }
+}
+
+}  // namespace bf
