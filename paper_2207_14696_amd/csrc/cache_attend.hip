@@ -7,7 +7,7 @@ namespace bf {
 namespace {
 
 constexpr int kCUs = 256;
-constexpr int kRowsWorkgroups = 3 * kCUs;  // as many as run at a time
+constexpr int kRowsWorkgroups = 3 * kCUs, kChunkWorkgroups = 2 * kCUs;  // as many as run at a time
 
 // One workgroup a query row of an item that was shared: its parts are those of the workgroups [w0, w1], each with sums about a
 // maximum of its own.
@@ -96,16 +96,23 @@ int items_of(const AttendCall &a, int R) {
     return a.b.B * ((a.b.n * a.group + R - 1) / R);
 }
 
-size_t partial_floats() { return (size_t)kRowsWorkgroups * 2 * kRowsR * (256 + 2); }
+constexpr size_t kPartialFloats =
+    2 * 258 * std::max((size_t)kRowsWorkgroups * kRowsR, (size_t)kChunkWorkgroups * 64 * kChunkNT);
 
 }  // namespace
+
+template <int BITS>
+hipError_t attend_chunk_bits(const AttendCall &a, const AttendPlan &p, int dp);
+static hipError_t launch_attend_chunk(const AttendCall &a, const AttendPlan &p, int bits, int dp) {
+    return bits == 8 ? attend_chunk_bits<8>(a, p, dp) : attend_chunk_bits<4>(a, p, dp);
+}
 
 bool ensure_partial(bifeat_cache *h, hipStream_t s) {
     if (h->d_partial) return true;
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone) return false;
     void *p = nullptr;
-    if (hipMalloc(&p, sizeof(float) * partial_floats()) != hipSuccess) {
+    if (hipMalloc(&p, sizeof(float) * kPartialFloats) != hipSuccess) {
         (void)hipGetLastError();
         return false;
     }
@@ -115,15 +122,25 @@ bool ensure_partial(bifeat_cache *h, hipStream_t s) {
 
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     const int dp = a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256, bits = h->spec.bits;
+    const bool chunk = a.b.tokens * a.group > (int64_t)32 * a.b.B;
+    const int R = chunk ? 64 * kChunkNT : kRowsR, tok = !chunk ? kRowsTok : dp == 256 ? 32 : 64;
     AttendPlan p;
-    p.items = items_of(a, kRowsR);
-    const int64_t most = ((a.b.width << a.c.ps_log2) + kRowsTok - 1) / kRowsTok, all = (int64_t)p.items * a.c.heads;
+    p.items = items_of(a, R);
+    const int64_t most = ((a.b.width << a.c.ps_log2) + tok - 1) / tok, all = (int64_t)p.items * a.c.heads;
     // contexts of a few units, and calls that find no workspace: an item a workgroup, nothing to join
     const bool split = most > 4 && ensure_partial(h, a.s);
     p.partial = split ? h->d_partial : nullptr;
-    p.nw = (int)(split ? std::min<int64_t>(all * most, kRowsWorkgroups) : all);
-    launch_attend_rows(a, p, bits, dp);
-    if (split) launch_join<kRowsR, kRowsTok>(a, p, dp);
+    p.nw = (int)(split ? std::min<int64_t>(all * most, chunk ? kChunkWorkgroups : kRowsWorkgroups) : all);
+    if (chunk) {
+        if (hipError_t e = launch_attend_chunk(a, p, bits, dp)) return e;
+        if (split) {
+            if (dp == 256) launch_join<64 * kChunkNT, 32>(a, p, dp);
+            else launch_join<64 * kChunkNT, 64>(a, p, dp);
+        }
+    } else {
+        launch_attend_rows(a, p, bits, dp);
+        if (split) launch_join<kRowsR, kRowsTok>(a, p, dp);
+    }
     return hipGetLastError();
 }
 

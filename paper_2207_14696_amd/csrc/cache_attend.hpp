@@ -15,7 +15,12 @@
 namespace bf {
 
 constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel for few rows
+constexpr int kChunkNT = 2;                   // tiles of 16 rows a wave in the kernel for many
 constexpr float kLog2e = 1.4426950408889634f;
+// A row's weights are p = 2^(x - top), and fp16 gets p * s: `top` follows the largest x + log2(s), so that scales of values of
+// any size fit.  It may lag (products up to 2^15) and is brought up for all lanes of a row together, to leave them 2^8.  Rows
+// of one value (s = 0) count with the least scale, which leaves p within 2^105; their codes are 0.
+constexpr float kLeastScale = 8.077935669463161e-28f;  // 2^-90
 constexpr float kNothing = -1e30f;  // running maximum where nothing was seen: below any score, and finite
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
@@ -252,6 +257,26 @@ __device__ inline void store_result(const AttendCall &a, int64_t at, float x) {
     if (a.dtype == BIFEAT_F32) static_cast<float *>(a.out)[at] = x;
     else if (a.dtype == BIFEAT_F16) static_cast<Half16 *>(a.out)[at] = from_float<Half16>(x);
     else static_cast<Brain16 *>(a.out)[at] = from_float<Brain16>(x);
+}
+
+// N columns of a result row, of which `left` are there
+template <int N>
+__device__ inline void store_columns(const AttendCall &a, int64_t at, int left, const float (&x)[N]) {
+    if constexpr (N >= 8) {
+#pragma unroll
+        for (int k = 0; k < N; k += 8) {
+            float e[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) e[i] = x[k + i];
+            if (a.dtype == BIFEAT_F32) store8_any(static_cast<float *>(a.out) + at + k, left - k, e);
+            else if (a.dtype == BIFEAT_F16) store8_any(static_cast<Half16 *>(a.out) + at + k, left - k, e);
+            else store8_any(static_cast<Brain16 *>(a.out) + at + k, left - k, e);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < N; k++)
+            if (k < left) store_result(a, at + k, x[k]);
+    }
 }
 
 // y * f in units of log2, with the cap and the bias by distance (slope in the same units)

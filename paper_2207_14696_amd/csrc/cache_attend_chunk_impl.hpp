@@ -1,0 +1,384 @@
+// Attention over the paged cache for many query rows a cached head (prompts, chunks of them): 64 NT rows an item.
+//
+// Bound by vector instructions: a score takes about ten of them (scale and offset of the codes, the exponential at a quarter of
+// the rate, two sums, the weight and its rounding), its two products a third of that time on the matrix cores.  So codes become
+// operands once a workgroup: each wave makes its share of a tile of TOK positions from registers, where the tile after next
+// is on its way, into LDS in the very order in which the products take them (1 KB an operand, 16 bytes a lane, no conflict), and all
+// four waves read them there for rows of their own.  Scores are keys x queries as in the kernel for few rows, so that
+// weights need not be moved; NT tiles of 16 rows a wave share what is read.
+#pragma once
+
+#include "cache_attend.hpp"
+
+namespace bf {
+
+template <int BITS, int DP, int NT>
+struct ChunkShape {
+    static constexpr int R = 64 * NT, TOK = DP == 256 ? 32 : 64;
+    static constexpr int KS = DP / 32, VT = DP / 16;        // operands of 16 keys, of 32 values
+    static constexpr int KP = 64 / TOK, VP = 128 / TOK;     // waves that share those
+    static constexpr int KB = DP / 4 * BITS / 8 / KP;       // bytes of a key a lane brings
+    static constexpr int KL = KB < 16 ? KB : 16;
+    static constexpr int VB = DP / 16 * BITS / 8 / VP;      // and of a value
+    static constexpr int VW = VB < 4 ? 1 : VB / 4;
+    static constexpr int KEYS = TOK / 16 * KS, VALUES = TOK / 32 * VT;
+};
+
+template <int BITS, int DP, int NP, int NT>
+__global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chunk_kernel(AttendCall a, AttendPlan plan) {
+    using S = ChunkShape<BITS, DP, NT>;
+    constexpr int R = S::R, TOK = S::TOK;
+    constexpr float kMiddle = 1 << (BITS - 1);
+    extern __shared__ uint4 lds[];
+    uint4(*keys)[S::KEYS][64] = reinterpret_cast<uint4(*)[S::KEYS][64]>(lds);
+    uint4(*values)[S::VALUES][64] = reinterpret_cast<uint4(*)[S::VALUES][64]>(lds + 2 * S::KEYS * 64);
+    float(*params)[4][TOK] = reinterpret_cast<float(*)[4][TOK]>(lds + 2 * (S::KEYS + S::VALUES) * 64);
+    __shared__ int sh[16];
+    __shared__ float tops[4];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int n16 = lane & 15, g = lane >> 4;
+    int64_t cur, end;
+    int head;
+    Place at;
+    locate<R, TOK>(a, plan, blockIdx.x, &cur, &end, &head, &at, sh);
+
+    const int rb = a.c.rb;
+    // what this wave brings of a tile: of 16 keys kgroup a quarter of the columns a lane group, of 32 values vgroup
+    const int kgroup = wave / S::KP, kpart = wave % S::KP, vgroup = wave / S::VP, vpart = wave % S::VP;
+    uint32_t koff[S::KB / S::KL];
+#pragma unroll
+    for (int i = 0; i < S::KB / S::KL; i++) {
+        const int o = (g * S::KP + kpart) * S::KB + i * S::KL;
+        koff[i] = n16 * rb + (o < rb ? o : 0);
+    }
+    const int vo = (n16 * S::VP + vpart) * S::VB;
+    const uint32_t voff = 4 * g * rb + (vo < rb ? vo : 0);
+    // thread t < TOK brings the floats of four positions: array t / (TOK / 4), positions 4 (t % (TOK / 4))
+    const int farray = threadIdx.x / (TOK / 4) & 3, fat = 4 * (threadIdx.x % (TOK / 4));
+
+    while (cur < end) {
+        const View v = view_of<R, TOK>(a, at.seq, at.rt);
+        const int units = v.units - at.unit < end - cur ? v.units - at.unit : (int)(end - cur);
+        const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
+        const int64_t token0 = a.b.first(at.seq);
+
+        // ---- pages: lane (TOK / 16) i + j has the page of 16 positions, the j-th of the item's tile `paged` + i
+        int pages = 0, paged = -64;
+        const int32_t *table = a.b.tables + (int64_t)at.seq * a.b.width;
+        constexpr int kSub = TOK / 16;
+        auto base_of = [&](int u) {
+            u += at.unit;
+            return (u < v.skip_at ? u : u + v.skip) * TOK;
+        };
+        uint32_t kw[S::KB / 4], vw[8][S::VW];
+        float4 fw;
+        auto load = [&](int u) {
+            if (u - paged >= 64 / kSub) {
+                paged = u;
+                int j = base_of(u + lane / kSub) + 16 * (lane % kSub);
+                j = j < v.len ? j : v.len - 1;
+                pages = table[j >> a.c.ps_log2];
+            }
+            const int base = base_of(u), at16 = (u - paged) * kSub;
+            auto block = [&](int j) -> const uint8_t * { return a.c.block(__builtin_amdgcn_readlane(pages, at16 + j), head); };
+            auto slot = [&](int j) { return (base + 16 * j) & (a.c.ps() - 1); };
+            {
+                const uint8_t *kp = block(kgroup) + (int64_t)slot(kgroup) * rb;
+#pragma unroll
+                for (int i = 0; i < S::KB / S::KL; i++) load_bytes<S::KL>(kp + koff[i], &kw[i * S::KL / 4]);
+            }
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const uint8_t *vp = block(2 * vgroup + j) + a.c.codes(1) + (int64_t)slot(2 * vgroup + j) * rb;
+#pragma unroll
+                for (int i = 0; i < 4; i++) load_bytes<S::VB>(vp + voff + i * rb, vw[4 * j + i]);
+            }
+            const int page = __shfl(pages, at16 + fat / 16);  // (from any lane: all take part)
+            if (threadIdx.x < TOK) {
+                const uint8_t *fp = a.c.block(page, head) + a.c.floats(0) + ((int64_t)farray * 4 << a.c.ps_log2);
+                fw = *reinterpret_cast<const float4 *>(fp + 4 * ((base + fat) & (a.c.ps() - 1)));
+            }
+        };
+        float f = 0.f;  // scale of the products, in units of log2
+        auto make = [&](int u, int buf) {
+#pragma unroll
+            for (int c = 0; c < S::KS / S::KP; c++) {
+                half8 key;
+                if constexpr (BITS == 8) {
+                    const uint32_t w0 = kw[2 * c], w1 = kw[2 * c + 1];
+                    key = operand(bytes_of(w0, 0), bytes_of(w0, 2), bytes_of(w1, 0), bytes_of(w1, 2));
+                } else {
+                    const uint32_t w = kw[c], w8 = w >> 8;
+                    key = operand(w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u);
+                }
+                if constexpr (NP == 2) key = centred(key, BITS == 8 ? all_of(1152.f) : centre4());
+                keys[buf][kgroup * S::KS + kpart * (S::KS / S::KP) + c][lane] = __builtin_bit_cast(uint4, key);
+            }
+#pragma unroll
+            for (int t = 0; t < S::VT / S::VP; t++) {
+                half8 val;
+                if constexpr (BITS == 8) {
+                    val = operand(pair_of(vw[0][t / 4], vw[1][t / 4], t % 4), pair_of(vw[2][t / 4], vw[3][t / 4], t % 4),
+                                  pair_of(vw[4][t / 4], vw[5][t / 4], t % 4), pair_of(vw[6][t / 4], vw[7][t / 4], t % 4));
+                } else {
+                    const int i = t / 2 % 4, d = t / 8;
+                    const uint32_t mask = t & 1 ? 0x00f000f0u : 0x000f000fu;
+                    val = operand(pair_of(vw[0][d], vw[1][d], i) & mask, pair_of(vw[2][d], vw[3][d], i) & mask,
+                                  pair_of(vw[4][d], vw[5][d], i) & mask, pair_of(vw[6][d], vw[7][d], i) & mask);
+                }
+                if constexpr (NP == 2) val = centred(val, all_of(BITS == 8 || (t & 1) ? 1152.f : 1032.f));
+                values[buf][vgroup * S::VT + vpart * (S::VT / S::VP) + t][lane] = __builtin_bit_cast(uint4, val);
+            }
+            if (threadIdx.x < TOK) {
+                // what no token was written to may hold anything
+                const int left = v.len - base_of(u) - fat;
+                float4 x = fw;
+                if (left < 4) x.w = 0.f;
+                if (left < 3) x.z = 0.f;
+                if (left < 2) x.y = 0.f;
+                if (left < 1) x.x = 0.f;
+                *reinterpret_cast<float4 *>(&params[buf][farray][fat]) = x;
+            }
+        };
+
+        if (v.len > 0) load(0);
+
+        // ---- the queries of the wave's rows
+        const int wrow0 = row0 + 16 * NT * wave;  // of the sequence
+        half8 q[NP][NT][S::KS];
+        float qsum[NT], slope[NT];
+        int pos[NT], low[NT];
+        float big = 0.f;
+        {
+            float x[NT][DP / 4];
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                const int row = wrow0 + 16 * n + n16;
+                const bool real = row - row0 < nrows;
+                const int qi = row / a.group, qh = head * a.group + row % a.group;
+                pos[n] = real ? v.len - v.n + qi : -1;
+                low[n] = a.window && pos[n] - a.window >= 0 ? (int)(pos[n] - a.window) : -1;
+                slope[n] = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+#pragma unroll
+                for (int i = 0; i < DP / 4; i++) x[n][i] = 0.f;
+                if (real) load_query(a, token0 + qi, qh, g * (DP / 4), x[n]);
+#pragma unroll
+                for (int i = 0; i < DP / 4; i++) big = fmaxf(big, fabsf(x[n][i]) <= 3.402823466e38f ? fabsf(x[n][i]) : 0.f);
+            }
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
+            __syncthreads();
+            if (lane == 0) tops[wave] = big;
+            __syncthreads();
+            const float up = power_to(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), 14);
+            f = a.scale * kLog2e * (kUnit<NP> / up);
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < DP / 4; i++) {
+                    const float y = x[n][i] * up;
+                    const _Float16 hi = (_Float16)y;
+                    const _Float16 lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
+                    sum += (float)hi + (float)lo;
+                    const int e = i % 8, slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
+                    const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
+                    q[0][n][i / 8][slot] = hi * down;
+                    if constexpr (NP == 2) q[NP - 1][n][i / 8][slot] = lo * down;
+                }
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+                qsum[n] = sum * (f / kUnit<NP>);
+            }
+        }
+        const float cap = a.softcap * kLog2e;
+        const bool shaped = a.softcap > 0.f || a.slopes;
+        // first and last position of the wave's queries
+        const int wend = wrow0 + 16 * NT < row0 + nrows ? wrow0 + 16 * NT : row0 + nrows;
+        const bool any_row = wrow0 < row0 + nrows;
+        const int wfirst = v.len - v.n + wrow0 / a.group, wlast = v.len - v.n + (wend - 1) / a.group;
+
+        float top[NT], total[NT], mins[NT], weights[NT];
+        float4v o[NT][S::VT];
+#pragma unroll
+        for (int n = 0; n < NT; n++) {
+            top[n] = kNothing;
+            total[n] = mins[n] = weights[n] = 0.f;
+#pragma unroll
+            for (int t = 0; t < S::VT; t++) o[n][t] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
+
+        // 32 positions for the wave's rows
+        auto half_tile = [&](int base, int buf, int hf) {
+            const bool whole = base + 32 <= v.len && wfirst >= 0 &&
+                               ((base + 31 <= wfirst && (!a.window || base > wlast - a.window)) || base + 32 <= v.prefix);
+            float4v acc[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; n++) acc[n][0] = acc[n][1] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < 2; j++)
+#pragma unroll
+                for (int c = 0; c < S::KS; c++) {
+                    const half8 key = __builtin_bit_cast(half8, keys[buf][(2 * hf + j) * S::KS + c][lane]);
+#pragma unroll
+                    for (int p = 0; p < NP; p++)
+#pragma unroll
+                        for (int n = 0; n < NT; n++) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][n][c], acc[n][j], 0, 0, 0);
+                }
+            float ks[8], km[8], vs[8], vm[8];
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                float4 p[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) p[i] = *reinterpret_cast<const float4 *>(&params[buf][i][32 * hf + 16 * j + 4 * g]);
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int e = 4 * j + i;
+                    ks[e] = (&p[0].x)[i] * f;
+                    km[e] = NP == 2 ? fmaf((&p[0].x)[i], kMiddle, (&p[1].x)[i]) : (&p[1].x)[i];
+                    vs[e] = fmaxf((&p[2].x)[i], kLeastScale);
+                    vm[e] = fmaf(vs[e], kMiddle, (&p[3].x)[i]);
+                }
+            }
+            half8 w[NP][NT];
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                uint32_t seen = 0xffu;
+                if (!whole) {
+                    seen = 0;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        const int t = base + 16 * (e / 4) + 4 * g + e % 4;
+                        const bool is = t < v.len && pos[n] >= 0 && ((t <= pos[n] && t > low[n]) || t < v.prefix);
+                        seen |= (uint32_t)is << e;
+                    }
+                }
+                // score of position e less `ref`
+                auto score = [&](int e, float ref) {
+                    float x;
+                    if (!shaped) {
+                        x = fmaf(ks[e], acc[n][e / 4][e % 4], fmaf(km[e], qsum[n], -ref));
+                    } else {
+                        x = fmaf(ks[e], acc[n][e / 4][e % 4], km[e] * qsum[n]);
+                        if (a.softcap > 0.f) x = capped(x, cap);
+                        x = fmaf(slope[n], (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos[n]), x) - ref;
+                    }
+                    return whole || (seen >> e & 1) ? x : -INFINITY;
+                };
+                float p[8], pw[8];
+                auto weigh = [&] {
+                    float most = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        p[e] = __builtin_amdgcn_exp2f(score(e, top[n]));
+                        pw[e] = p[e] * vs[e];
+                        most = fmaxf(most, pw[e]);
+                    }
+                    return most;
+                };
+                if (__any(weigh() > 32768.f)) {
+                    float now = kNothing;
+#pragma unroll
+                    for (int e = 0; e < 8; e++) now = fmaxf(now, score(e, 0.f) + __builtin_amdgcn_logf(vs[e]));
+                    now = fmaxf(now, __shfl_xor(now, 16));
+                    now = fmaxf(now, __shfl_xor(now, 32));
+                    now = fmaxf(top[n], now - 8.f);
+                    const float keep = __builtin_amdgcn_exp2f(top[n] - now);
+                    top[n] = now;
+                    total[n] *= keep;
+                    mins[n] *= keep;
+                    weights[n] *= keep;
+#pragma unroll
+                    for (int t = 0; t < S::VT; t++) o[n][t] *= keep;
+                    weigh();
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    float pm = vm[e];
+                    if (!whole && !(seen >> e & 1)) pw[e] = pm = 0.f;  // (an infinity or NaN that the row does not see)
+                    total[n] += p[e];
+                    mins[n] = fmaf(p[e], pm, mins[n]);
+                    w[0][n][e] = (_Float16)pw[e];
+                    if constexpr (NP == 2) w[NP - 1][n][e] = (_Float16)(pw[e] - (float)w[0][n][e]);
+                }
+                if constexpr (NP == 1)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        weights[n] = __builtin_amdgcn_fdot2(half2v{w[0][n][e], w[0][n][e + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, weights[n], false);
+            }
+#pragma unroll
+            for (int t = 0; t < S::VT; t++) {
+                const half8 val = __builtin_bit_cast(half8, values[buf][hf * S::VT + t][lane]);
+#pragma unroll
+                for (int p = 0; p < NP; p++)
+#pragma unroll
+                    for (int n = 0; n < NT; n++) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[p][n], o[n][t], 0, 0, 0);
+            }
+        };
+
+        if (v.len > 0) {
+            make(0, 0);
+            if (units > 1) load(1);
+            __syncthreads();
+            for (int u = 0; u < units; u++) {
+                const int base = base_of(u), buf = u & 1;
+                if (u + 1 < units) make(u + 1, buf ^ 1);
+                if (u + 2 < units) load(u + 2);
+                if (any_row)
+#pragma unroll
+                    for (int hf = 0; hf < TOK / 32; hf++) {
+                        const int b = base + 32 * hf;
+                        // positions that none of the wave's rows sees
+                        if (b >= v.len || ((b > wlast || (a.window && b + 31 <= wfirst - a.window)) && b >= v.prefix)) continue;
+                        half_tile(b, buf, hf);
+                    }
+                __syncthreads();
+            }
+        }
+
+        const bool complete = at.unit == 0 && units == v.units;
+        if (any_row)
+#pragma unroll
+            for (int n = 0; n < NT; n++) {
+                float s = total[n], m = mins[n], ws = weights[n];
+                s += __shfl_xor(s, 16);
+                s += __shfl_xor(s, 32);
+                m += __shfl_xor(m, 16);
+                m += __shfl_xor(m, 32);
+                ws += __shfl_xor(ws, 16);
+                ws += __shfl_xor(ws, 32);
+                const int r = 16 * (NT * wave + n) + n16, row = row0 + r;
+                if (r >= nrows) continue;
+                const float rest = m - ws * kMiddle, inv = s != 0.f ? 1.f / s : 0.f;
+                const int64_t dst = ((token0 + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
+                float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2)) + r * (DP + 2);
+                if (!complete && g == 0) part[DP] = top[n], part[DP + 1] = s;
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    const int col = (4 * g + i) * S::VT;
+                    float x[S::VT];
+#pragma unroll
+                    for (int t = 0; t < S::VT; t++) x[t] = fmaf(o[n][t][i], kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f), rest);
+                    if (complete) {
+#pragma unroll
+                        for (int t = 0; t < S::VT; t++) x[t] *= inv;
+                        store_columns<S::VT>(a, dst + col, a.c.d - col, x);
+                    } else {
+#pragma unroll
+                        for (int t = 0; t < S::VT; t++) part[col + t] = x[t];
+                    }
+                }
+            }
+        cur += units;
+        if (cur < end) next_item<R>(a, &head, &at);
+    }
+}
+
+template <int BITS, int DP, int NT>
+constexpr size_t chunk_lds() {
+    using S = ChunkShape<BITS, DP, NT>;
+    return 2 * ((S::KEYS + S::VALUES) * 1024 + 4 * S::TOK * sizeof(float));
+}
+
+}  // namespace bf

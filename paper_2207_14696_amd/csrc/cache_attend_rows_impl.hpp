@@ -93,14 +93,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             }
             qsum += __shfl_xor(qsum, 16);
             qsum += __shfl_xor(qsum, 32);
-            qsum *= 1.f / kUnit<NP>;
+            qsum *= f / kUnit<NP>;
         }
         const float slope = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
         const float cap = a.softcap * kLog2e;
         const bool shaped = a.softcap > 0.f || a.slopes;
         const int low = a.window && pos - a.window >= 0 ? (int)(pos - a.window) : -1;  // positions above it are in the window
 
-        float top = kNothing, total = 0.f, mins = 0.f, weights = 0.f, unit_of_s = 0.f;
+        float top = kNothing, total = 0.f, mins = 0.f, weights = 0.f;
         float4v o[L::VT];
 #pragma unroll
         for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                     const int e = 4 * j + i;
                     ks[e] = (&p[0].x)[i];
                     km[e] = NP == 2 ? fmaf(ks[e], kMiddle, (&p[1].x)[i]) : (&p[1].x)[i];
-                    vs[e] = (&p[2].x)[i];
+                    vs[e] = fmaxf((&p[2].x)[i], kLeastScale);
                     vm[e] = fmaf(vs[e], kMiddle, (&p[3].x)[i]);
                 }
             }
@@ -176,14 +176,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                     const int t = base + 16 * (e / 4) + 4 * g + e % 4;
                     const bool is = t < v.len && pos >= 0 && ((t <= pos && t > low) || t < v.prefix);
                     seen |= (uint32_t)is << e;
-                    vs[e] = is ? vs[e] : 0.f;  // (the unit of the weights is not that of what the row does not see)
                 }
             }
             // ---- scores
-            float x[8];
+            float4v acc[2];
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                float4v acc{0.f, 0.f, 0.f, 0.f};
+                acc[j] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < L::KS; c++) {
                     half8 key;
@@ -196,62 +195,56 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                     }
                     if constexpr (NP == 2) key = centred(key, BITS == 8 ? all_of(1152.f) : centre4());
 #pragma unroll
-                    for (int p = 0; p < NP; p++) acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc, 0, 0, 0);
+                    for (int p = 0; p < NP; p++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc[j], 0, 0, 0);
                 }
-#pragma unroll
-                for (int i = 0; i < 4; i++) x[4 * j + i] = f * fmaf(ks[4 * j + i], acc[i], km[4 * j + i] * qsum);
             }
             if (u + 1 < units) load_keys(u + 1);
-            if (shaped) {
+            // score of position e less `ref`
+            auto score = [&](int e, float ref) {
+                float x = fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum);
+                if (shaped) {
+                    if (a.softcap > 0.f) x = capped(x, cap);
+                    x = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x);
+                }
+                return whole || (seen >> e & 1) ? x - ref : -INFINITY;
+            };
+            float p[8], pw[8];
+            auto weigh = [&] {
+                float most = 0.f;
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    if (a.softcap > 0.f) x[e] = capped(x[e], cap);
-                    x[e] = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x[e]);
+                    p[e] = __builtin_amdgcn_exp2f(score(e, top));
+                    pw[e] = p[e] * vs[e];
+                    most = fmaxf(most, pw[e]);
                 }
-            }
-            if (!whole) {
+                return most;
+            };
+            if (__any(weigh() > 32768.f)) {
+                float now = kNothing;
 #pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = seen >> e & 1 ? x[e] : -INFINITY;
-            }
-            // ---- the running maximum, and the unit that the values' scales are counted in: both may lag (weights up to
-            // 2^8 and scales up to 2^7 units stay within fp16), and are brought up for all lanes of a row together
-            float big = x[0], wide = vs[0];
-#pragma unroll
-            for (int e = 1; e < 8; e++) big = fmaxf(big, x[e]), wide = fmaxf(wide, vs[e]);
-            if (__any(big > top + 8.f || wide * unit_of_s > 128.f || (unit_of_s == 0.f && wide > 0.f))) {
-                big = fmaxf(big, __shfl_xor(big, 16));
-                big = fmaxf(big, __shfl_xor(big, 32));
-                wide = fmaxf(wide, __shfl_xor(wide, 16));
-                wide = fmaxf(wide, __shfl_xor(wide, 32));
-                const float now = fmaxf(top, big), keep = __builtin_amdgcn_exp2f(top - now);
-                float by = keep;
-                if (wide > 0.f) {
-                    const float unit = power_to(wide, 6);
-                    if (unit_of_s == 0.f) {
-                        unit_of_s = unit;  // (nothing is summed yet but positions of scale 0)
-                    } else if (unit < unit_of_s) {
-                        by = keep * (unit / unit_of_s);
-                        unit_of_s = unit;
-                    }
-                }
+                for (int e = 0; e < 8; e++) now = fmaxf(now, score(e, 0.f) + __builtin_amdgcn_logf(vs[e]));
+                now = fmaxf(now, __shfl_xor(now, 16));
+                now = fmaxf(now, __shfl_xor(now, 32));
+                now = fmaxf(top, now - 8.f);
+                const float keep = __builtin_amdgcn_exp2f(top - now);
                 top = now;
                 total *= keep;
                 mins *= keep;
-                weights *= by;
+                weights *= keep;
 #pragma unroll
-                for (int t = 0; t < L::VT; t++) o[t] *= by;
+                for (int t = 0; t < L::VT; t++) o[t] *= keep;
+                weigh();
             }
             // ---- weights
             half8 w[NP];
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                const float p = __builtin_amdgcn_exp2f(x[e] - top);
-                float pw = p * (vs[e] * unit_of_s), pm = p * vm[e];
-                if (!whole && !(seen >> e & 1)) pw = pm = 0.f;  // (an infinity or NaN that the row does not see)
-                total += p;
-                mins += pm;
-                w[0][e] = (_Float16)pw;
-                if constexpr (NP == 2) w[NP - 1][e] = (_Float16)(pw - (float)w[0][e]);
+                float pm = vm[e];
+                if (!whole && !(seen >> e & 1)) pw[e] = pm = 0.f;  // (an infinity or NaN that the row does not see)
+                total += p[e];
+                mins = fmaf(p[e], pm, mins);
+                w[0][e] = (_Float16)pw[e];
+                if constexpr (NP == 2) w[NP - 1][e] = (_Float16)(pw[e] - (float)w[0][e]);
             }
             if constexpr (NP == 1)
 #pragma unroll
@@ -293,11 +286,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
         mins += __shfl_xor(mins, 32);
         weights += __shfl_xor(weights, 16);
         weights += __shfl_xor(weights, 32);
-        const float per = unit_of_s != 0.f ? 1.f / unit_of_s : 0.f;
-        const float rest = mins - weights * (kMiddle * per);  // (NP == 2: the codes were less their middle already)
+        const float rest = mins - weights * kMiddle;  // (NP == 2: the codes were less their middle already)
 #pragma unroll
         for (int t = 0; t < L::VT; t++) {
-            const float back = kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f) * per;
+            const float back = kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f);
 #pragma unroll
             for (int i = 0; i < 4; i++) sums[wave][n16][(4 * g + i) * L::VT + t] = fmaf(o[t][i], back, rest);
         }
