@@ -9,85 +9,98 @@ namespace {
 constexpr int kCUs = 256;
 constexpr int kRowsWorkgroups = 3 * kCUs, kChunkWorkgroups = 2 * kCUs;  // as many as run at a time
 
-// One workgroup a query row of an item that was shared: its parts are those of the workgroups [w0, w1], each with sums about a
-// maximum of its own.
-template <int R, int TOK>
-__global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPlan plan, int dp) {
-    __shared__ float weight[1024], red[8];
-    __shared__ float part[4][256];
-    __shared__ int sh[8];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int r = blockIdx.x % R, item = (int)(blockIdx.x / R % plan.items), head = (int)(blockIdx.x / R / plan.items);
-    // the item's sequence, and the units of the head's items before it
-    const int seq = sequence_of_item<R>(a, item);
-    const int rt = item - first_item<R>(a, seq);
-    const View v = view_of<R, TOK>(a, seq, rt);
-    const int rows = v.n * a.group;
-    if (v.units == 0 || rt * R + r >= rows) return;
-    const int per = (plan.items + 255) / 256, i0 = tid * per, i1 = i0 + per < plan.items ? i0 + per : plan.items;
-    int sum = 0, before = 0;
-    if (i0 < i1) {
-        int s = sequence_of_item<R>(a, i0);
-        int next = first_item<R>(a, s + 1);
-        for (int i = i0; i < i1; i++) {
-            while (i >= next && s + 1 < a.b.B) next = first_item<R>(a, ++s + 1);
-            const int u = view_of<R, TOK>(a, s, i - first_item<R>(a, s)).units;
-            sum += u;
-            if (i < item) before += u;
+// Joins the parts of the items that several workgroups have.  Blocks (w, y): the item that workgroup w goes on with, if it is the
+// first to go on with it; WAVES waves a query row, 16 lanes a part.  The parts' order in the sums is fixed by their number.
+template <int R, int DP, int WAVES>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPlan plan) {
+    const int w = blockIdx.x;
+    const PartOf b = plan.begins[w];
+    if (w >= b.nw || b.unit == 0) return;
+    const int first = b.start - b.unit;  // the item's first unit
+    if (start_of(w - 1, b.all, b.nw) > first) return;
+    // parts: of w - 1, which has its beginning, and of [w, w1]
+    const int w1 = workgroup_of(first + b.units - 1, b.all, b.nw);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & 15;
+    constexpr int kGroups = 4 * WAVES, kRows = 4 / WAVES;  // part groups a row, rows at a time
+    const int group = (wave % WAVES) * 4 + lane / 16;
+    __shared__ float tops[4], dens[4], part[WAVES > 1 ? 4 : 1][DP];
+    const int64_t stride = R * (DP + 2);
+    const int left = (int)a.b.count(b.seq) * a.group - b.rt * R, rows = left < R ? left : R;
+    for (int r0 = blockIdx.y * kRows; r0 < rows; r0 += gridDim.y * kRows) {
+        const bool real = r0 + wave / WAVES < rows;
+        const int r = real ? r0 + wave / WAVES : rows - 1;
+        auto at = [&](int k) { return plan.partial + ((int64_t)k * 2 + (k == w - 1)) * stride; };
+        float top = kNothing;
+        for (int k = w - 1 + group * 16 + sub; k <= w1; k += kGroups * 16) top = fmaxf(top, at(k)[R * DP + r]);
+#pragma unroll
+        for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
+        if constexpr (WAVES > 1) {
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        }
+        float4 acc[DP / 64];  // columns 64 c + 4 sub
+        float den = 0.f;
+#pragma unroll
+        for (int c = 0; c < DP / 64; c++) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 2
+        for (int k = w - 1 + group; k <= w1; k += kGroups) {
+            const float *x = at(k);
+            const float e = __builtin_amdgcn_exp2f(x[R * DP + r] - top);
+            den += e * x[R * DP + R + r];
+#pragma unroll
+            for (int c = 0; c < DP / 64; c++) {
+                const float4 y = *reinterpret_cast<const float4 *>(x + r * DP + 64 * c + 4 * sub);
+                acc[c].x = fmaf(e, y.x, acc[c].x);
+                acc[c].y = fmaf(e, y.y, acc[c].y);
+                acc[c].z = fmaf(e, y.z, acc[c].z);
+                acc[c].w = fmaf(e, y.w, acc[c].w);
+            }
+        }
+#pragma unroll
+        for (int m = 16; m < 64; m *= 2) {
+            den += __shfl_xor(den, m);
+#pragma unroll
+            for (int c = 0; c < DP / 64; c++) {
+                acc[c].x += __shfl_xor(acc[c].x, m);
+                acc[c].y += __shfl_xor(acc[c].y, m);
+                acc[c].z += __shfl_xor(acc[c].z, m);
+                acc[c].w += __shfl_xor(acc[c].w, m);
+            }
+        }
+        if constexpr (WAVES > 1) {
+            if (lane == 0) dens[wave] = den;
+            if (lane < 16)
+#pragma unroll
+                for (int c = 0; c < DP / 64; c++) *reinterpret_cast<float4 *>(&part[wave][64 * c + 4 * sub]) = acc[c];
+            __syncthreads();
+            den = dens[0] + dens[1] + dens[2] + dens[3];
+        }
+        const int row = b.rt * R + r;
+        const int64_t dst = ((a.b.first(b.seq) + row / a.group) * ((int64_t)a.c.heads * a.group) + b.head * a.group + row % a.group) * a.c.d;
+        const float inv = den != 0.f ? 1.f / den : 0.f;
+        if constexpr (WAVES > 1) {
+            if (tid < a.c.d) store_result(a, dst + tid, (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) * inv);
+            __syncthreads();
+        } else if (real && lane < 16) {
+#pragma unroll
+            for (int c = 0; c < DP / 64; c++) {
+                const int col = 64 * c + 4 * sub;
+                const float x[4] = {acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv};
+                store_columns<4>(a, dst + col, a.c.d - col, x);
+            }
         }
     }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) sum += __shfl_xor(sum, m), before += __shfl_xor(before, m);
-    if (lane == 0) sh[wave] = sum, sh[4 + wave] = before;
-    __syncthreads();
-    const int64_t total = (int64_t)sh[0] + sh[1] + sh[2] + sh[3];
-    const int64_t u0 = total * head + sh[4] + sh[5] + sh[6] + sh[7], u1 = u0 + v.units - 1, all = total * a.c.heads;
-    const int64_t nw = all < plan.nw ? all : plan.nw;
-    const int w0 = (int)(((u0 + 1) * nw - 1) / all), w1 = (int)(((u1 + 1) * nw - 1) / all);
-    if (w0 == w1) return;  // one workgroup had it all
-    const int64_t stride = R * (dp + 2);
-    auto at = [&](int w) { return plan.partial + ((int64_t)w * 2 + (w == w0)) * stride + (int64_t)r * (dp + 2); };
-    float top = kNothing;
-    for (int w = w0 + tid; w <= w1; w += 256) top = fmaxf(top, at(w)[dp]);
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-    if (lane == 0) red[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-    // weights of 1024 parts at a time; each wave every fourth part, a lane 4 columns (d <= 256)
-    float acc[4] = {0.f, 0.f, 0.f, 0.f}, den = 0.f;
-    for (int from = w0; from <= w1; from += 1024) {
-        const int to = from + 1024 <= w1 ? from + 1024 : w1 + 1;
-        __syncthreads();
-        for (int w = from + tid; w < to; w += 256) {
-            const float e = __builtin_amdgcn_exp2f(at(w)[dp] - top);
-            weight[w - from] = e;
-            den += e * at(w)[dp + 1];
-        }
-        __syncthreads();
-        for (int w = from + wave; w < to; w += 4) {
-            const float e = weight[w - from];
-            const float *x = at(w);
-#pragma unroll
-            for (int k = 0; k < 4; k++)
-                if (lane + 64 * k < a.c.d) acc[k] += e * x[lane + 64 * k];
-        }
-    }
-#pragma unroll
-    for (int m = 1; m < 64; m *= 2) den += __shfl_xor(den, m);
-    if (lane == 0) red[4 + wave] = den;
-#pragma unroll
-    for (int k = 0; k < 4; k++) part[wave][lane + 64 * k] = acc[k];
-    __syncthreads();
-    den = red[4] + red[5] + red[6] + red[7];
-    const int row = rt * R + r;
-    const int64_t dst = ((a.b.first(seq) + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
-    if (tid < a.c.d) store_result(a, dst + tid, den != 0.f ? (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) / den : 0.f);
 }
 
-template <int R, int TOK>
-void launch_join(const AttendCall &a, const AttendPlan &p, int dp) {
-    attend_join_kernel<R, TOK><<<(unsigned)((int64_t)p.items * a.c.heads * R), 256, 0, a.s>>>(a, p, dp);
+// rows: the most that an item has
+template <int R>
+void launch_join(const AttendCall &a, const AttendPlan &p, int dp, int rows) {
+    constexpr int kWaves = R == 16 ? 4 : 1;
+    const dim3 grid(p.nw, std::min(16, (rows * kWaves + 3) / 4));
+    if (dp == 64) attend_join_kernel<R, 64, kWaves><<<grid, 256, 0, a.s>>>(a, p);
+    else if (dp == 128) attend_join_kernel<R, 128, kWaves><<<grid, 256, 0, a.s>>>(a, p);
+    else attend_join_kernel<R, 256, kWaves><<<grid, 256, 0, a.s>>>(a, p);
 }
 
 // numbers of a head's items, an upper bound where the batch is ragged
@@ -112,7 +125,7 @@ bool ensure_partial(bifeat_cache *h, hipStream_t s) {
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone) return false;
     void *p = nullptr;
-    if (hipMalloc(&p, sizeof(float) * kPartialFloats) != hipSuccess) {
+    if (hipMalloc(&p, sizeof(float) * kPartialFloats + sizeof(PartOf) * std::max(kRowsWorkgroups, kChunkWorkgroups)) != hipSuccess) {
         (void)hipGetLastError();
         return false;
     }
@@ -127,19 +140,18 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     AttendPlan p;
     p.items = items_of(a, R);
     const int64_t most = ((a.b.width << a.c.ps_log2) + tok - 1) / tok, all = (int64_t)p.items * a.c.heads;
-    // contexts of a few units, and calls that find no workspace: an item a workgroup, nothing to join
-    const bool split = most > 4 && ensure_partial(h, a.s);
+    // contexts of a few units, and calls that find no workspace: an item a workgroup, nothing to join (nor beyond 2^31 units)
+    const bool split = most > 4 && all * most <= INT32_MAX && ensure_partial(h, a.s);
     p.partial = split ? h->d_partial : nullptr;
+    p.begins = split ? reinterpret_cast<PartOf *>(h->d_partial + kPartialFloats) : nullptr;
     p.nw = (int)(split ? std::min<int64_t>(all * most, chunk ? kChunkWorkgroups : kRowsWorkgroups) : all);
+    const int rows = a.b.indptr ? R : std::min(R, a.b.n * a.group);
     if (chunk) {
         if (hipError_t e = launch_attend_chunk(a, p, bits, dp)) return e;
-        if (split) {
-            if (dp == 256) launch_join<64 * kChunkNT, 32>(a, p, dp);
-            else launch_join<64 * kChunkNT, 64>(a, p, dp);
-        }
+        if (split) launch_join<64 * kChunkNT>(a, p, dp, rows);
     } else {
         launch_attend_rows(a, p, bits, dp);
-        if (split) launch_join<kRowsR, kRowsTok>(a, p, dp);
+        if (split) launch_join<kRowsR>(a, p, dp, rows);
     }
     return hipGetLastError();
 }

@@ -12,6 +12,9 @@
 
 #include "cache.hpp"
 
+#ifndef BF_NT
+#define BF_NT 0
+#endif
 namespace bf {
 
 constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel for few rows
@@ -32,12 +35,26 @@ typedef float float16v __attribute__((ext_vector_type(16)));
 // head's), a unit is TOK positions of the cache that an item looks at.  The units of all items, in the order of heads,
 // then sequences, then rows, are dealt evenly to `nw` workgroups, each a run of them; contexts of any mixture of
 // lengths so keep all of them busy.  An item that several workgroups share is joined by a second kernel.
+struct PartOf {  // where a workgroup begins
+    int head, seq, rt;
+    int unit, units;  // the first unit it has of the item, and the item's
+    int nw;           // workgroups that have units (0: this one has none)
+    int start, all;   // units before it, and of the call
+};
 struct AttendPlan {
     int items;       // per head; of a ragged batch with numbers left free (see first_item)
     int nw;
     // null: a workgroup has one item, all of it (contexts are short, or there is no workspace)
-    float *partial;  // [nw][2][R][DP + 2]: sums, running maximum, sum of weights of an item begun before / not ended by a workgroup
+    float *partial;  // [nw][2]: of an item begun before / not ended by a workgroup sums [R][DP], reference [R], sum of weights [R]
+    PartOf *begins;  // [nw]
 };
+
+// `all` units over nw workgroups, nw <= all: the first all % nw have one more than the others
+__device__ inline int start_of(int w, int all, int nw) { return w * (all / nw) + (w < all % nw ? w : all % nw); }
+__device__ inline int workgroup_of(int unit, int all, int nw) {
+    const int q = all / nw, r = all % nw;
+    return unit < r * (q + 1) ? unit / (q + 1) : r + (unit - r * (q + 1)) / q;
+}
 
 // Sequence b's items have numbers from first_item(b) on.  In a ragged batch floor(rows before it / R) + b leaves every
 // sequence room for its own, rounded up, without a sum over the batch.
@@ -83,8 +100,8 @@ __device__ inline View view_of(const AttendCall &a, int b, int rt) {
 }
 
 struct Place {
-    int item, seq, rt;  // the item, its sequence, its number in it
-    int unit;           // of the item
+    int seq, rt;  // an item: its sequence, its number in it
+    int unit;     // of the item
 };
 
 // The sequence that item `i` of a head belongs to.
@@ -100,22 +117,22 @@ __device__ inline int sequence_of_item(const AttendCall &a, int i) {
     return lo;
 }
 
-// Sums the units of a head's items: the total, and the place of unit `want` modulo it.  All threads of a workgroup.
+// Deals the units: workgroup w's are [*start, *end) of the call's, the first of them at *at.  All threads of a workgroup;
 // sh: 16 ints.
 template <int R, int TOK>
-__device__ inline int64_t locate(const AttendCall &a, const AttendPlan &p, int64_t w, int64_t *start, int64_t *end, int *head, Place *at,
-                                 int *sh) {
+__device__ inline void locate(const AttendCall &a, const AttendPlan &p, int w, int *start, int *end, int *head, Place *at, int *sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
     if (!p.partial) {
-        at->item = (int)(w % p.items);
-        at->seq = sequence_of_item<R>(a, at->item);
-        at->rt = at->item - first_item<R>(a, at->seq);
+        const int item = w % p.items;
+        at->seq = sequence_of_item<R>(a, item);
+        at->rt = item - first_item<R>(a, at->seq);
         at->unit = 0;
-        *head = (int)(w / p.items);
+        *head = w / p.items;
         *start = 0;
         *end = view_of<R, TOK>(a, at->seq, at->rt).units;
-        return *end;
+        return;
     }
+    // a thread sums the units of some of a head's items
     const int per = (p.items + (int)blockDim.x - 1) / (int)blockDim.x;
     const int i0 = tid * per, i1 = i0 + per < p.items ? i0 + per : p.items;
     int sum = 0;
@@ -133,36 +150,40 @@ __device__ inline int64_t locate(const AttendCall &a, const AttendPlan &p, int64
     }
     if (lane == 63) sh[wave] = upto;
     __syncthreads();
-    int64_t total = 0, before = upto - sum;
+    int total = 0, before = upto - sum;
     for (int k = 0; k < waves; k++) {
         if (k < wave) before += sh[k];
         total += sh[k];
     }
-    const int64_t all = total * a.c.heads, nw = all < p.nw ? all : p.nw;  // (none has nothing between two that have)
-    *start = w < nw ? w * all / nw : all;
-    *end = w < nw ? (w + 1) * all / nw : all;
-    *head = total ? (int)(*start / total) : 0;
-    const int64_t want = total && *start < all ? *start % total : -1;
+    total = __builtin_amdgcn_readfirstlane(total);
+    const int all = total * a.c.heads, nw = all < p.nw ? all : p.nw;  // (none has nothing between two that have)
+    if (w >= nw) {
+        *start = *end = 0;
+        if (tid == 0) p.begins[w].nw = 0;
+        return;
+    }
+    *start = start_of(w, all, nw);
+    *end = start_of(w + 1, all, nw);
+    *head = *start / total;
+    const int want = *start - *head * total;
     if (want >= before && want < before + sum) {
-        int left = (int)(want - before);
+        int left = want - before;
         s = seq, next = first_item<R>(a, s + 1);
         for (int i = i0; i < i1; i++) {
             while (i >= next && s + 1 < a.b.B) next = first_item<R>(a, ++s + 1);
             const int rt = i - first_item<R>(a, s), u = view_of<R, TOK>(a, s, rt).units;
             if (left < u) {
-                sh[8] = i, sh[9] = s, sh[10] = rt, sh[11] = left;
+                sh[8] = s, sh[9] = rt, sh[10] = left;
+                p.begins[w] = {*head, s, rt, left, u, nw, *start, all};
                 break;
             }
             left -= u;
         }
     }
     __syncthreads();
-    if (want < 0) return total;
-    at->item = __builtin_amdgcn_readfirstlane(sh[8]);
-    at->seq = __builtin_amdgcn_readfirstlane(sh[9]);
-    at->rt = __builtin_amdgcn_readfirstlane(sh[10]);
-    at->unit = __builtin_amdgcn_readfirstlane(sh[11]);
-    return total;
+    at->seq = __builtin_amdgcn_readfirstlane(sh[8]);
+    at->rt = __builtin_amdgcn_readfirstlane(sh[9]);
+    at->unit = __builtin_amdgcn_readfirstlane(sh[10]);
 }
 
 // The next item that has units, of this head or the next.
@@ -179,11 +200,11 @@ __device__ inline void next_item(const AttendCall &a, int *head, Place *at) {
     }
 }
 
-// Power of two that brings `top` to [2^to, 2^(to+1)).
+// Power of two that brings `top` to [2^to, 2^(to+1)) (within 2^-80 .. 2^80; 1 for 0).
 __device__ inline float power_to(float top, int to) {
-    int e = top > 0.f ? ilogbf(top) : to;
-    e = e < -80 ? -80 : e > 80 ? 80 : e;
-    return ldexpf(1.f, to - e);
+    int e = (int)(__builtin_bit_cast(uint32_t, top) >> 23 & 255) - 127;
+    e = top > 0.f ? (e < -80 ? -80 : e > 80 ? 80 : e) : to;
+    return __builtin_bit_cast(float, (uint32_t)(127 + to - e) << 23);
 }
 
 // codes -> fp16 operands ----------------------------------------------------------------------------------------------
@@ -220,26 +241,31 @@ __device__ inline half8 centre4() {
 // the unit of a product with a code: codes are subnormals, or (NP = 2) whole numbers
 template <int NP> constexpr float kUnit = NP == 2 ? 1.f : 16777216.f;
 
+// Loads from a head's block of a page, whose address all lanes share: a descriptor in scalar registers, a 32-bit offset a lane
+// and one for all, where 64-bit addresses would take two vector registers and three vector instructions a load.  (The
+// hardware gives zeros past the block's end.)
+__device__ inline __amdgpu_buffer_rsrc_t block_buffer(const CachePages &c, int page, int head) {
+    return __builtin_amdgcn_make_buffer_rsrc(c.block(page, head), 0, (int)c.head_bytes, 0x00027000);
+}
 template <int N>
-__device__ inline void load_bytes(const uint8_t *p, uint32_t *w) {
+__device__ inline void load_bytes(__amdgpu_buffer_rsrc_t r, uint32_t each, uint32_t all, uint32_t *w) {
     if constexpr (N == 16) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
+        const auto q = __builtin_amdgcn_raw_buffer_load_b128(r, each, all, BF_NT);
+        w[0] = q[0], w[1] = q[1], w[2] = q[2], w[3] = q[3];
     } else if constexpr (N == 8) {
-        const uint2 q = *reinterpret_cast<const uint2 *>(p);
-        w[0] = q.x, w[1] = q.y;
+        const auto q = __builtin_amdgcn_raw_buffer_load_b64(r, each, all, BF_NT);
+        w[0] = q[0], w[1] = q[1];
     } else if constexpr (N == 4) {
-        w[0] = *reinterpret_cast<const uint32_t *>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, each, all, BF_NT);
     } else if constexpr (N == 2) {
-        w[0] = *reinterpret_cast<const uint16_t *>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, each, all, BF_NT);
     } else {
-        w[0] = *p;
+        w[0] = __builtin_amdgcn_raw_buffer_load_b8(r, each, all, BF_NT);
     }
 }
-
 // one query's elements as floats, zeros from column a.c.d on
 template <int N>
-__device__ inline void load_query(const AttendCall &a, int64_t token, int head, int col, float (&x)[N]) {
+__device__ inline void load_query(const AttendCall &a, int64_t token, int head, int col, float *x) {
     const int64_t at = token * a.q.token_stride + head * a.q.head_stride + col;
 #pragma unroll
     for (int k = 0; k < N; k += 8) {

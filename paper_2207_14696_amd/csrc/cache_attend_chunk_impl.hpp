@@ -38,10 +38,9 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g = lane >> 4;
-    int64_t cur, end;
-    int head;
+    int cur, end, head;
     Place at;
-    locate<R, TOK>(a, plan, blockIdx.x, &cur, &end, &head, &at, sh);
+    locate<R, TOK>(a, plan, (int)blockIdx.x, &cur, &end, &head, &at, sh);
 
     const int rb = a.c.rb;
     // what this wave brings of a tile: of 16 keys kgroup a quarter of the columns a lane group, of 32 values vgroup
@@ -59,7 +58,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 
     while (cur < end) {
         const View v = view_of<R, TOK>(a, at.seq, at.rt);
-        const int units = v.units - at.unit < end - cur ? v.units - at.unit : (int)(end - cur);
+        const int units = v.units - at.unit < end - cur ? v.units - at.unit : end - cur;
         const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
         const int64_t token0 = a.b.first(at.seq);
 
@@ -81,18 +80,20 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 pages = table[j >> a.c.ps_log2];
             }
             const int base = base_of(u), at16 = (u - paged) * kSub;
-            auto block = [&](int j) -> const uint8_t * { return a.c.block(__builtin_amdgcn_readlane(pages, at16 + j), head); };
+            auto buffer = [&](int j) { return block_buffer(a.c, __builtin_amdgcn_readlane(pages, at16 + j), head); };
             auto slot = [&](int j) { return (base + 16 * j) & (a.c.ps() - 1); };
             {
-                const uint8_t *kp = block(kgroup) + (int64_t)slot(kgroup) * rb;
+                const auto b = buffer(kgroup);
+                const uint32_t all = slot(kgroup) * rb;
 #pragma unroll
-                for (int i = 0; i < S::KB / S::KL; i++) load_bytes<S::KL>(kp + koff[i], &kw[i * S::KL / 4]);
+                for (int i = 0; i < S::KB / S::KL; i++) load_bytes<S::KL>(b, koff[i], all, &kw[i * S::KL / 4]);
             }
 #pragma unroll
             for (int j = 0; j < 2; j++) {
-                const uint8_t *vp = block(2 * vgroup + j) + a.c.codes(1) + (int64_t)slot(2 * vgroup + j) * rb;
+                const auto b = buffer(2 * vgroup + j);
+                const uint32_t all = (uint32_t)a.c.codes(1) + slot(2 * vgroup + j) * rb;
 #pragma unroll
-                for (int i = 0; i < 4; i++) load_bytes<S::VB>(vp + voff + i * rb, vw[4 * j + i]);
+                for (int i = 0; i < 4; i++) load_bytes<S::VB>(b, voff, all + i * rb, vw[4 * j + i]);
             }
             const int page = __shfl(pages, at16 + fat / 16);  // (from any lane: all take part)
             if (threadIdx.x < TOK) {
@@ -162,7 +163,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 slope[n] = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
 #pragma unroll
                 for (int i = 0; i < DP / 4; i++) x[n][i] = 0.f;
-                if (real) load_query(a, token0 + qi, qh, g * (DP / 4), x[n]);
+                if (real) load_query<DP / 4>(a, token0 + qi, qh, g * (DP / 4), x[n]);
 #pragma unroll
                 for (int i = 0; i < DP / 4; i++) big = fmaxf(big, fabsf(x[n][i]) <= 3.402823466e38f ? fabsf(x[n][i]) : 0.f);
             }
@@ -352,8 +353,8 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 if (r >= nrows) continue;
                 const float rest = m - ws * kMiddle, inv = s != 0.f ? 1.f / s : 0.f;
                 const int64_t dst = ((token0 + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
-                float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2)) + r * (DP + 2);
-                if (!complete && g == 0) part[DP] = top[n], part[DP + 1] = s;
+                float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2));
+                if (!complete && g == 0) part[R * DP + r] = top[n], part[R * DP + R + r] = s;
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int col = (4 * g + i) * S::VT;
@@ -366,7 +367,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                         store_columns<S::VT>(a, dst + col, a.c.d - col, x);
                     } else {
 #pragma unroll
-                        for (int t = 0; t < S::VT; t++) part[col + t] = x[t];
+                        for (int t = 0; t < S::VT; t++) part[r * DP + col + t] = x[t];
                     }
                 }
             }

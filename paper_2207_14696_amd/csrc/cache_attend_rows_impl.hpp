@@ -16,7 +16,8 @@ namespace bf {
 template <int BITS, int DP>
 struct RowLanes {
     static constexpr int KB = DP / 4 * BITS / 8;   // bytes of a key that a lane reads (its quarter of the columns)
-    static constexpr int KL = KB < 16 ? KB : 16;   // in loads of so many
+    static constexpr int KL = KB < 16 ? KB : 16;   // in loads of so many, four lanes' next to each other
+    static constexpr int KC = KL * 8 / BITS;       // columns a load
     static constexpr int VB = DP / 16 * BITS / 8;  // bytes of a value (its sixteenth)
     static constexpr int KS = DP / 32;             // products over the columns
     static constexpr int VT = DP / 16;             // tiles of the values' columns
@@ -36,10 +37,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int n16 = lane & 15, g = lane >> 4;
-    int64_t cur, end;
-    int head;
+    int cur, end, head;
     Place at;
-    locate<R, TOK>(a, plan, blockIdx.x, &cur, &end, &head, &at, sh);
+    locate<R, TOK>(a, plan, (int)blockIdx.x, &cur, &end, &head, &at, sh);
 
     // byte offsets in a row; past its end (columns the row is too short for) any byte will do: the queries have zeros there,
     // and the sums of such columns are not written
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
     uint32_t koff[L::KB / L::KL];
 #pragma unroll
     for (int i = 0; i < L::KB / L::KL; i++) {
-        const int o = g * L::KB + i * L::KL;
+        const int o = (4 * i + g) * L::KL;
         koff[i] = n16 * rb + (o < rb ? o : 0);
     }
     const uint32_t voff = 4 * g * rb + (n16 * L::VB < rb ? n16 * L::VB : 0);
@@ -56,11 +56,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
 
     while (cur < end) {
         const View v = view_of<R, TOK>(a, at.seq, at.rt);
-        const int units = v.units - at.unit < end - cur ? v.units - at.unit : (int)(end - cur);
+        const int units = v.units - at.unit < end - cur ? v.units - at.unit : end - cur;
         const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
         const int64_t token0 = a.b.first(at.seq);
 
-        // ---- the queries: lane (n16, g) has columns [g DP/4, (g+1) DP/4) of row n16, in the order of the keys' codes
+        // ---- the queries: lane (n16, g) has a quarter of the columns of row n16, those of the keys that it reads
         const int row = row0 + n16;
         const bool real = n16 < nrows;
         const int qi = row / a.group, qh = head * a.group + row % a.group;
@@ -71,7 +71,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             float x[DP / 4];
 #pragma unroll
             for (int i = 0; i < DP / 4; i++) x[i] = 0.f;
-            if (real) load_query(a, token0 + qi, qh, g * (DP / 4), x);
+            if (real)
+#pragma unroll
+                for (int i = 0; i < DP / 4; i += L::KC) load_query<L::KC>(a, token0 + qi, qh, 4 * i + g * L::KC, x + i);
             float top = 0.f;
 #pragma unroll
             for (int i = 0; i < DP / 4; i++) top = fmaxf(top, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
@@ -114,10 +116,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
         };
         uint32_t kw[2][L::KB / 4], vw[8][L::VW];
         float4 fw;
-        auto block_of = [&](int u, int j) -> const uint8_t * {
-            return a.c.block(__builtin_amdgcn_readlane(pages, 2 * (u - paged) + j), head);
-        };
-        auto slot_of = [&](int u, int j) { return (base_of(u) + 16 * j) & (a.c.ps() - 1); };
+        __amdgpu_buffer_rsrc_t block0, block1;  // of the step's two halves
+        int slot0, slot1;
         auto load_keys = [&](int u) {
             if (u - paged >= 32) {
                 paged = u;
@@ -125,24 +125,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                 j = j < v.len ? j : v.len - 1;
                 pages = table[j >> a.c.ps_log2];
             }
-            const uint8_t *fp[2];
+            const int page0 = __builtin_amdgcn_readlane(pages, 2 * (u - paged)), page1 = __builtin_amdgcn_readlane(pages, 2 * (u - paged) + 1);
+            block0 = block_buffer(a.c, page0, head);
+            block1 = block_buffer(a.c, page1, head);
+            slot0 = base_of(u) & (a.c.ps() - 1);
+            slot1 = (base_of(u) + 16) & (a.c.ps() - 1);
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const int slot = slot_of(u, j);
-                const uint8_t *block = block_of(u, j), *kp = block + (int64_t)slot * rb;
+            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(block0, koff[i], slot0 * rb, &kw[0][i * L::KL / 4]);
 #pragma unroll
-                for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(kp + koff[i], &kw[j][i * L::KL / 4]);
-                fp[j] = block + a.c.floats(0) + 4 * slot;
-            }
-            fw = *reinterpret_cast<const float4 *>((lane & 4 ? fp[1] : fp[0]) + foff);
+            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(block1, koff[i], slot1 * rb, &kw[1][i * L::KL / 4]);
+            const uint8_t *fp = a.c.block(lane & 4 ? page1 : page0, head) + a.c.floats(0) + 4 * (lane & 4 ? slot1 : slot0);
+            fw = *reinterpret_cast<const float4 *>(fp + foff);
         };
-        auto load_values = [&](int u) {
+        auto load_values = [&] {  // of the step whose keys were asked for last
+            const uint32_t at0 = (uint32_t)a.c.codes(1) + slot0 * rb, at1 = (uint32_t)a.c.codes(1) + slot1 * rb;
 #pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const uint8_t *vp = block_of(u, j) + a.c.codes(1) + (int64_t)slot_of(u, j) * rb;
+            for (int i = 0; i < 4; i++) load_bytes<L::VB>(block0, voff, at0 + i * rb, vw[i]);
 #pragma unroll
-                for (int i = 0; i < 4; i++) load_bytes<L::VB>(vp + voff + i * rb, vw[4 * j + i]);
-            }
+            for (int i = 0; i < 4; i++) load_bytes<L::VB>(block1, voff, at1 + i * rb, vw[4 + i]);
         };
 
         auto step = [&](int u) {
@@ -272,10 +272,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
 
         if (v.len > 0) {
             load_keys(0);
-            load_values(0);
+            load_values();
             for (int u = 0; u < units; u++) {
                 if (base_of(u) < v.len) step(u);  // (of an item's last unit some waves may have no positions)
-                if (u + 1 < units) load_values(u + 1);
+                if (u + 1 < units) load_values();
             }
         }
 
@@ -306,16 +306,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             const float e2 = __builtin_amdgcn_exp2f(t2 - now), e3 = __builtin_amdgcn_exp2f(t3 - now);
             const float all = totals[0][r] * e0 + totals[1][r] * e1 + totals[2][r] * e2 + totals[3][r] * e3;
             const bool whole = at.unit == 0 && units == v.units;
-            float *part = whole ? nullptr : plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2)) + r * (DP + 2);
+            float *part = whole ? nullptr : plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2));
             const int64_t dst = ((token0 + (row0 + r) / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + (row0 + r) % a.group) * a.c.d;
             const float inv = all != 0.f ? 1.f / all : 0.f;
             if (r < nrows) {
                 for (int c = c0; c < a.c.d; c += 16) {
                     const float x = sums[0][r][c] * e0 + sums[1][r][c] * e1 + sums[2][r][c] * e2 + sums[3][r][c] * e3;
                     if (whole) store_result(a, dst + c, x * inv);
-                    else part[c] = x;
+                    else part[r * DP + c] = x;
                 }
-                if (!whole && c0 == 0) part[DP] = now, part[DP + 1] = all;
+                if (!whole && c0 == 0) part[R * DP + r] = now, part[R * DP + R + r] = all;
             }
         }
         __syncthreads();

@@ -1,84 +1,77 @@
 // The paged cache written and read back: rows of head_dim columns, each with a range of its own.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.hpp"
 
 namespace bf {
 namespace {
 
-// LPR lanes a row, 8 columns a lane; rows of a token are its heads' keys, then its heads' values, so that a
-// wave's rows are a few tokens'.  The place of a wave's first token is looked up by the whole wave.
-struct RowPlace {
-    bool there;     // a row of the call, with a place in the cache
-    int64_t token;  // of the call
-    int which, head;
-    int64_t slot;
-    uint8_t *block;
+// A workgroup takes up to kTokens tokens of the call, all their heads, keys and values.  Where they lie in the cache is looked up
+// once a token.  Then LPR lanes take a row, 8 columns each; a wave's rows are consecutive tokens' of a head, which lie next to
+// each other in a page as far as the call's tokens do in their sequence.
+constexpr int kTokens = 16;
+
+struct Places {
+    int64_t page[kTokens];  // byte offset of the page, -1: before the sequence's beginning
+    int slot[kTokens];
 };
 
-template <int LPR>
-__device__ inline RowPlace place_row(const CachePages &c, const CacheBatch &b, int64_t &row, bool &in_call) {
-    const int64_t wave = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
-    const int64_t first_row = wave * (64 / LPR);
-    const int per = 2 * c.heads;
-    int64_t t0 = first_row / per;
-    if (t0 >= b.tokens) t0 = b.tokens - 1;
-    int seq = sequence_of(b, t0);
-    row = first_row + (threadIdx.x & 63) / LPR;
-    RowPlace p;
-    p.token = row / per;
-    in_call = p.token < b.tokens;
-    const int r = (int)(row - p.token * per);
-    p.which = r >= c.heads;
-    p.head = r - p.which * c.heads;
-    p.there = false;
-    p.slot = 0;
-    p.block = nullptr;
-    if (!in_call) return p;
-    if (b.indptr)
-        while (seq + 1 < b.B && b.indptr[seq + 1] <= p.token) seq++;
-    else
-        seq = (int)(p.token / b.n);
-    const int64_t pos = b.length(seq, c.ps_log2) - b.count(seq) + (p.token - b.first(seq));
-    if (pos < 0) return p;
-    p.there = true;
-    p.slot = pos & (c.ps() - 1);
-    p.block = c.block(b.tables[(int64_t)seq * b.width + (pos >> c.ps_log2)], p.head);
-    return p;
+__device__ inline void find_places(const CachePages &c, const CacheBatch &b, int64_t t0, int count, Places &sh) {
+    if (threadIdx.x < 64) {
+        int seq = sequence_of(b, t0);
+        if ((int)threadIdx.x < count) {
+            const int64_t t = t0 + threadIdx.x;
+            if (b.indptr)
+                while (seq + 1 < b.B && b.indptr[seq + 1] <= t) seq++;
+            else
+                seq = (int)(t / b.n);
+            const int64_t pos = b.length(seq, c.ps_log2) - b.count(seq) + (t - b.first(seq));
+            sh.slot[threadIdx.x] = (int)(pos & (c.ps() - 1));
+            sh.page[threadIdx.x] = pos < 0 ? -1 : b.tables[(int64_t)seq * b.width + (pos >> c.ps_log2)] * c.page_bytes;
+        }
+    }
+    __syncthreads();
 }
 
-template <typename T, int BITS, int LPR>
-__global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, CacheBatch b, HeadRows k, HeadRows v) {
-    int64_t row;
-    bool in_call;
-    const RowPlace p = place_row<LPR>(c, b, row, in_call);
+// the smallest, or largest, of LPR neighbouring lanes' values, in all of them
+template <int LPR, bool MAX>
+__device__ inline float extreme(float x) {
+    auto of = [](float a, float b) { return MAX ? fmaxf(a, b) : fminf(a, b); };
+    auto moved = [](float a, auto ctrl) {
+        return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, a), decltype(ctrl)::value, 0xf, 0xf, true));
+    };
+    x = of(x, moved(x, std::integral_constant<int, 0xb1>{}));   // lane ^ 1
+    x = of(x, moved(x, std::integral_constant<int, 0x4e>{}));   // lane ^ 2
+    x = of(x, moved(x, std::integral_constant<int, 0x141>{}));  // the other four of eight
+    if constexpr (LPR > 8) x = of(x, moved(x, std::integral_constant<int, 0x140>{}));  // the other eight of sixteen
+    if constexpr (LPR > 16) x = of(x, __shfl_xor(x, 16));
+    return x;
+}
+
+// Eight of a row's columns by each of its LPR lanes.  All lanes of a wave.
+template <int BITS, int LPR>
+__device__ inline void write_row(const CachePages &c, const float (&x)[8], bool real, uint8_t *block, int which, int slot) {
     const int sub = threadIdx.x % LPR, col = 8 * sub;
-    float x[8];
     float mn = INFINITY, mx = -INFINITY;
-    int bad = 0;
-    if (p.there) {
-        const HeadRows &h = p.which ? v : k;
-        load8_any(static_cast<const T *>(h.data) + p.token * h.token_stride + p.head * h.head_stride + col, c.d - col, x);
+    bool nan = false;
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (col + i < c.d) {
-                bad |= !(fabsf(x[i]) <= 3.402823466e38f);
-                mn = fminf(mn, x[i]);
-                mx = fmaxf(mx, x[i]);
-            }
-    }
-#pragma unroll
-    for (int m = 1; m < LPR; m *= 2) {
-        mn = fminf(mn, __shfl_xor(mn, m));
-        mx = fmaxf(mx, __shfl_xor(mx, m));
-        bad |= __shfl_xor(bad, m);
-    }
-    if (!p.there) return;
+    for (int i = 0; i < 8; i++)
+        if (col + i < c.d) {
+            nan |= x[i] != x[i];
+            mn = fminf(mn, x[i]);
+            mx = fmaxf(mx, x[i]);
+        }
+    const uint64_t nans = __ballot(nan) >> (threadIdx.x % 64 / LPR * LPR);
+    const bool any_nan = (uint32_t)nans & (uint32_t)((1ull << LPR) - 1);
+    mn = extreme<LPR, false>(mn);
+    mx = extreme<LPR, true>(mx);
+    if (!real) return;
     constexpr float kTop = (1 << BITS) - 1;
     const float span = mx - mn;
     float inv = kTop / span, scale = span / kTop;
     if (!(fabsf(inv) <= 3.402823466e38f)) inv = scale = 0.f;
-    if (bad || !(span <= 3.402823466e38f)) {
+    if (any_nan || !(span <= 3.402823466e38f)) {  // (an infinity makes the span infinite or NaN)
         mn = scale = NAN;
         inv = 0.f;
     }
@@ -88,9 +81,8 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, Cac
         const float f = fminf(fmaxf(rintf((x[i] - mn) * inv), 0.f), kTop);  // (a NaN becomes 0)
         q[i] = col + i < c.d ? (uint32_t)f : 0u;
     }
-    uint8_t *codes = p.block + c.codes(p.which) + p.slot * c.rb;
-    constexpr int kBytes = BITS;  // of 8 codes
-    if (sub * kBytes < c.rb) {
+    uint8_t *codes = block + c.codes(which) + slot * c.rb;
+    if (sub * BITS < c.rb) {  // 8 codes are BITS bytes
         if constexpr (BITS == 8) {
             uint2 w;
             w.x = q[0] | q[1] << 8 | q[2] << 16 | q[3] << 24;
@@ -104,35 +96,92 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, Cac
         }
     }
     if (sub == 0) {
-        float *f = reinterpret_cast<float *>(p.block + c.floats(p.which)) + p.slot;
+        float *f = reinterpret_cast<float *>(block + c.floats(which)) + slot;
         f[0] = scale;
         f[c.ps()] = mn;
     }
 }
 
+// Bound by the bytes of k and v and of the codes.
 template <typename T, int BITS, int LPR>
-__global__ __launch_bounds__(kThreads) void cache_read_kernel(CachePages c, CacheBatch b, T *k, T *v) {
-    int64_t row;
-    bool in_call;
-    const RowPlace p = place_row<LPR>(c, b, row, in_call);
-    const int sub = threadIdx.x % LPR, col = 8 * sub;
-    if (!in_call || col >= c.d) return;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (p.there) {
-        const uint8_t *codes = p.block + c.codes(p.which) + p.slot * c.rb;
-        const float *f = reinterpret_cast<const float *>(p.block + c.floats(p.which)) + p.slot;
-        const float scale = f[0], mn = f[c.ps()];
-        if constexpr (BITS == 8) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(codes + 8 * sub);
+__global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, CacheBatch b, HeadRows k, HeadRows v, int per) {
+    __shared__ Places places;
+    const int64_t t0 = (int64_t)blockIdx.x * per;
+    const int count = b.tokens - t0 < per ? (int)(b.tokens - t0) : per;
+    find_places(c, b, t0, count, places);
+    const int sub = threadIdx.x % LPR, col = 8 * sub, rows = count * 2 * c.heads;
+    constexpr int kAhead = 2, kStep = kThreads / LPR;  // rows in flight
+    // (a wave's rows are taken together, those past the end as zeros that are not stored)
+    for (int r0 = threadIdx.x / 64 * (64 / LPR); r0 < rows; r0 += kAhead * kStep) {
+        float xs[kAhead][8];
+        bool reals[kAhead];
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = fmaf((float)((i < 4 ? w.x : w.y) >> 8 * (i & 3) & 255), scale, mn);
-        } else {
-            const uint32_t w = *reinterpret_cast<const uint32_t *>(codes + 4 * sub);
+        for (int i = 0; i < kAhead; i++) {
+            const int r = r0 + i * kStep + threadIdx.x % 64 / LPR, token = r % count, hw = r / count, which = hw >= c.heads;
+            reals[i] = r < rows && places.page[token] >= 0;
 #pragma unroll
-            for (int i = 0; i < 8; i++) x[i] = fmaf((float)(w >> 4 * i & 15), scale, mn);
+            for (int e = 0; e < 8; e++) xs[i][e] = 0.f;
+            if (reals[i]) {
+                const HeadRows &h = which ? v : k;
+                load8_any(static_cast<const T *>(h.data) + (t0 + token) * h.token_stride + (hw - which * c.heads) * h.head_stride + col,
+                          c.d - col, xs[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            const int r = r0 + i * kStep + threadIdx.x % 64 / LPR, token = r % count, hw = r / count, which = hw >= c.heads;
+            write_row<BITS, LPR>(c, xs[i], reals[i], c.pages + places.page[token] + (hw - which * c.heads) * c.head_bytes, which,
+                                 places.slot[token]);
         }
     }
-    store8_any((p.which ? v : k) + (p.token * c.heads + p.head) * c.d + col, c.d - col, x);
+}
+
+// Bound by the bytes of the result, twice (fp32: four times) the codes'.
+template <typename T, int BITS, int LPR>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(CachePages c, CacheBatch b, T *k, T *v, int per) {
+    __shared__ Places places;
+    const int64_t t0 = (int64_t)blockIdx.x * per;
+    const int count = b.tokens - t0 < per ? (int)(b.tokens - t0) : per;
+    find_places(c, b, t0, count, places);
+    const int sub = threadIdx.x % LPR, col = 8 * sub, rows = count * 2 * c.heads;
+    if (col >= c.d) return;
+    constexpr int kAhead = 4;  // rows in flight
+    for (int r0 = threadIdx.x / LPR; r0 < rows; r0 += kAhead * (kThreads / LPR)) {
+        uint32_t w[kAhead][BITS / 4];
+        float scale[kAhead], mn[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            const int r = r0 + i * (kThreads / LPR), token = r % count, hw = r / count, which = hw >= c.heads, head = hw - which * c.heads;
+            scale[i] = mn[i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < BITS / 4; e++) w[i][e] = 0;
+            if (r < rows && places.page[token] >= 0) {
+                const uint8_t *block = c.pages + places.page[token] + head * c.head_bytes;
+                const int slot = places.slot[token];
+                const uint8_t *codes = block + c.codes(which) + slot * c.rb;
+                if constexpr (BITS == 8) {
+                    const uint2 u = *reinterpret_cast<const uint2 *>(codes + 8 * sub);
+                    w[i][0] = u.x, w[i][BITS / 4 - 1] = u.y;
+                } else {
+                    w[i][0] = *reinterpret_cast<const uint32_t *>(codes + 4 * sub);
+                }
+                const float *f = reinterpret_cast<const float *>(block + c.floats(which)) + slot;
+                scale[i] = f[0], mn[i] = f[c.ps()];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) {
+            const int r = r0 + i * (kThreads / LPR), token = r % count, hw = r / count, which = hw >= c.heads, head = hw - which * c.heads;
+            if (r >= rows) break;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; e++) {
+                const uint32_t q = BITS == 8 ? w[i][e / 4 % (BITS / 4)] >> 8 * (e & 3) & 255 : w[i][0] >> 4 * e & 15;
+                x[e] = fmaf((float)q, scale[i], mn[i]);
+            }
+            store8_any((which ? v : k) + ((t0 + token) * c.heads + head) * c.d + col, c.d - col, x);
+        }
+    }
 }
 
 __global__ __launch_bounds__(kThreads) void cache_check_kernel(CacheBatch b, int ps_log2, int64_t num_pages, int32_t *bad) {
@@ -154,11 +203,9 @@ __global__ void cache_check_zero_kernel(int32_t *bad) { *bad = 0; }
 
 int lanes_per_row(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
-// workgroups of `b.tokens` tokens; below 2^31, as the entry points see to
-unsigned row_blocks(const CachePages &c, const CacheBatch &b, int lpr) {
-    const int64_t rows = b.tokens * 2 * c.heads, per = kThreads / lpr;
-    return (unsigned)((rows + per - 1) / per);
-}
+// tokens a workgroup: few calls' worth over many workgroups, many over few enough that each looks up several at once
+int tokens_per(const CacheBatch &b) { return (int)std::max<int64_t>(1, std::min<int64_t>(kTokens, b.tokens / 1024)); }
+unsigned row_blocks(const CacheBatch &b, int per) { return (unsigned)((b.tokens + per - 1) / per); }
 
 }  // namespace
 
@@ -169,11 +216,11 @@ unsigned row_blocks(const CachePages &c, const CacheBatch &b, int lpr) {
 
 hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const HeadRows &k, const HeadRows &v, int bits, int dtype,
                               hipStream_t s) {
-    const int lpr = lanes_per_row(c.d);
-    const unsigned grid = row_blocks(c, b, lpr);
+    const int lpr = lanes_per_row(c.d), per = tokens_per(b);
+    const unsigned grid = row_blocks(b, per);
 #define BF_GO(T, LPR)                                                                     \
-    if (bits == 8) cache_write_kernel<T, 8, LPR><<<grid, kThreads, 0, s>>>(c, b, k, v);   \
-    else cache_write_kernel<T, 4, LPR><<<grid, kThreads, 0, s>>>(c, b, k, v)
+    if (bits == 8) cache_write_kernel<T, 8, LPR><<<grid, kThreads, 0, s>>>(c, b, k, v, per);   \
+    else cache_write_kernel<T, 4, LPR><<<grid, kThreads, 0, s>>>(c, b, k, v, per)
 #define BF_LPR(T) if (lpr == 8) { BF_GO(T, 8); } else if (lpr == 16) { BF_GO(T, 16); } else { BF_GO(T, 32); }
     BF_BY_TYPE(BF_LPR)
 #undef BF_GO
@@ -181,11 +228,11 @@ hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const He
 }
 
 hipError_t launch_cache_read(const CachePages &c, const CacheBatch &b, void *k, void *v, int bits, int dtype, hipStream_t s) {
-    const int lpr = lanes_per_row(c.d);
-    const unsigned grid = row_blocks(c, b, lpr);
+    const int lpr = lanes_per_row(c.d), per = tokens_per(b);
+    const unsigned grid = row_blocks(b, per);
 #define BF_GO(T, LPR)                                                                                       \
-    if (bits == 8) cache_read_kernel<T, 8, LPR><<<grid, kThreads, 0, s>>>(c, b, (T *)k, (T *)v);            \
-    else cache_read_kernel<T, 4, LPR><<<grid, kThreads, 0, s>>>(c, b, (T *)k, (T *)v)
+    if (bits == 8) cache_read_kernel<T, 8, LPR><<<grid, kThreads, 0, s>>>(c, b, (T *)k, (T *)v, per);            \
+    else cache_read_kernel<T, 4, LPR><<<grid, kThreads, 0, s>>>(c, b, (T *)k, (T *)v, per)
     BF_BY_TYPE(BF_LPR)
 #undef BF_GO
 #undef BF_LPR
