@@ -1,7 +1,7 @@
 """ctypes binding of the C ABI in ``include/bifeat.h``: same names, argument
 marshalling only.  Tensors are torch CUDA tensors; their ``data_ptr()`` and the
-current stream's handle are what crosses the boundary.  ``gather_dequant``, ``gather_mean`` and
-``gather_sum`` without ``out`` go through a native module (``csrc/calls.cpp``) to the same entry points where it is built."""
+current stream's handle are what crosses the boundary.  ``gather_dequant``, ``gather_mean``, ``gather_sum`` and the paged cache's
+calls (``cache.py``) without ``out`` go through a native module (``csrc/calls.cpp``) to the same entry points where it is built."""
 from __future__ import annotations
 
 import ctypes as C
@@ -156,7 +156,7 @@ def _load_calls():
             from . import _calls as module
             _calls = module
         except ImportError as e:
-            warnings.warn(f"gather_dequant, gather_mean and gather_sum go through ctypes, 5 us a call slower ({e}); "
+            warnings.warn(f"gather_dequant, gather_mean, gather_sum and the paged cache's calls go through ctypes, 5 us a call slower ({e}); "
                           "`python -m paper_2207_14696_amd.build` builds the native module", RuntimeWarning, stacklevel=3)
             _calls = False
     return _calls

@@ -41,7 +41,7 @@ def _compile_calls() -> None:
         f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", f'-DBF_TORCH_VERSION="{torch.__version__}"',
         "-isystem", os.path.join(base, "include"),
         "-isystem", os.path.join(base, "include", "torch", "csrc", "api", "include"),
-        "-I", sysconfig.get_path("include"), os.path.join(CSRC, "calls.cpp"), "-o", tmp,
+        "-I", os.path.join(ROOT, "include"), "-I", sysconfig.get_path("include"), os.path.join(CSRC, "calls.cpp"), "-o", tmp,
         "-L", os.path.join(base, "lib"), "-ltorch_python", "-ltorch", "-ltorch_cpu", "-lc10",
         "-Wl,-rpath," + os.path.join(base, "lib")])
     os.replace(tmp, CALLS)

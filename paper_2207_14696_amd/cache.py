@@ -1,6 +1,7 @@
 """A paged cache of keys and values in few bits: written as a model answers, read back, and attended
 to.  Argument marshalling only, as in ``binding.py``; the entry points are ``bifeat_cache_*`` of
-``include/bifeat.h``, which defines layout and arithmetic."""
+``include/bifeat.h``, which defines layout and arithmetic.  Ordinary calls go through the native module (``csrc/calls.cpp``) where
+it is built; what it leaves goes through ctypes, behind the checks here."""
 from __future__ import annotations
 
 import ctypes as C
@@ -48,9 +49,16 @@ class PagedCache:
         self._h = h
         self.bits, self.heads, self.head_dim, self.page_size = int(bits), int(heads), int(head_dim), int(page_size)
         self.page_bytes = int(self._lib.bifeat_cache_page_bytes(h))
+        self._scale = 1.0 / math.sqrt(self.head_dim)
+        # what the native module's calls begin with: entry point, handle, sizes
+        rest = (h.value, self.page_bytes, self.heads, self.head_dim)
+        self._write, self._read, self._attend = (
+            (_b._address(fn),) + rest
+            for fn in (self._lib.bifeat_cache_write, self._lib.bifeat_cache_read, self._lib.bifeat_cache_attend))
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
+        self._write = self._read = self._attend = (0,) * 5  # (no address of a destroyed object is left)
         if h:
             self._lib.bifeat_cache_destroy(h)
 
@@ -96,6 +104,10 @@ class PagedCache:
 
     def write(self, pages, k, v, tables, lengths, indptr=None) -> None:
         """Quantises k and v, [tokens, heads, head_dim], into the pages."""
+        if calls := _b._calls or _b._load_calls():
+            r = calls.cache_write(*self._write, pages, k, v, tables, lengths, indptr)
+            if r is not None:
+                return _check(r)
         rows = [_head_rows(t, self.heads, self.head_dim, name) for t, name in ((k, "k"), (v, "v"))]
         if k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must be alike")
@@ -107,6 +119,12 @@ class PagedCache:
         """Keys and values of the last tokens of each sequence, ``tokens`` in all, as they stand in
         the cache: two [tokens, heads, head_dim] of ``dtype`` (float32)."""
         import torch
+        if out is None and (calls := _b._calls or _b._load_calls()):
+            r = calls.cache_read(*self._read, pages, tokens, _type(dtype or torch.float32), tables, lengths, indptr)
+            if r is not None:
+                if r.__class__ is int:
+                    _check(r)
+                return r
         shape = (tokens, self.heads, self.head_dim)
         if out is None:
             dtype = dtype or torch.float32
@@ -125,6 +143,13 @@ class PagedCache:
         ``softcap`` c > 0: c * tanh(score / c); ``window`` w > 0: the last w positions only; ``prefix`` int64
         [B]: positions that all queries see; ``slopes`` float32 [query heads]: bias by distance.  Returns
         [tokens, query heads, head_dim] of q's dtype."""
+        scale = self._scale if scale is None else scale
+        if out is None and (calls := _b._calls or _b._load_calls()):
+            r = calls.cache_attend(*self._attend, pages, q, scale, softcap, window, prefix, slopes, tables, lengths, indptr)
+            if r is not None:
+                if r.__class__ is int:
+                    _check(r)
+                return r
         import torch
         if q.dim() != 3:
             raise ValueError("q must be [tokens, query heads, head_dim]")
@@ -139,7 +164,7 @@ class PagedCache:
         if slopes is not None and slopes.shape != (heads,):
             raise ValueError("slopes must be [query heads]")
         ptr, count = self._pages(pages)
-        options = _b._CAttendOptions(1.0 / math.sqrt(self.head_dim) if scale is None else scale, softcap, window,
+        options = _b._CAttendOptions(scale, softcap, window,
                                      _dev_ptr(prefix, (torch.int64,)), _dev_ptr(slopes, (torch.float32,)))
         _check(self._lib.bifeat_cache_attend(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, q.shape[0])),
                                              C.byref(rows), heads, _type(q.dtype), C.byref(options), _dev_ptr(out), _stream()))

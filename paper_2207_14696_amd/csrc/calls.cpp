@@ -18,9 +18,14 @@
 #include <cstdint>
 #include <string>
 
+#include "bifeat.h"
+
 namespace {
 
 using DequantFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, int64_t, float *, void *);
+using CacheWriteFn = decltype(&bifeat_cache_write);
+using CacheReadFn = decltype(&bifeat_cache_read);
+using CacheAttendFn = decltype(&bifeat_cache_attend);
 using AggregateFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, const void *, int64_t, int64_t, float *,
                             void *);
 
@@ -129,9 +134,163 @@ PyObject *aggregate(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
+// ---- the paged cache.  Each call begins with (address of the entry point, handle, page bytes, heads, head_dim), then pages,
+// and has tables, lengths, indptr (or None) in a row.
+
+struct Cache {
+    void *fn, *handle;
+    int64_t page_bytes, heads, d;
+    const at::Tensor *pages;
+};
+
+bool cache_of(PyObject *const *a, Cache *c) {
+    c->fn = PyLong_AsVoidPtr(a[0]);
+    c->handle = PyLong_AsVoidPtr(a[1]);
+    c->page_bytes = PyLong_AsLongLong(a[2]);
+    c->heads = PyLong_AsLongLong(a[3]);
+    c->d = PyLong_AsLongLong(a[4]);
+    c->pages = tensor(a[5], at::kByte, at::kByte);
+    return !PyErr_Occurred() && c->fn && c->handle && c->pages && c->pages->dim() == 2 && c->pages->size(1) == c->page_bytes &&
+           !watched();
+}
+
+bool batch_of(PyObject *const *a, int64_t tokens, bifeat_cache_batch *b) {
+    const at::Tensor *tables = tensor(a[0], at::kInt, at::kInt), *lengths = tensor(a[1], at::kLong, at::kLong), *indptr = nullptr;
+    if (!tables || !lengths || tables->dim() != 2 || lengths->dim() != 1 || lengths->size(0) != tables->size(0)) return false;
+    const int64_t B = tables->size(0);
+    if (a[2] != Py_None) {
+        indptr = tensor(a[2], at::kLong, at::kLong);
+        if (!indptr || indptr->dim() != 1 || indptr->size(0) != B + 1) return false;
+    }
+    *b = {static_cast<const int32_t *>(tables->data_ptr()), tables->size(1), static_cast<const int64_t *>(lengths->data_ptr()),
+          indptr ? static_cast<const int64_t *>(indptr->data_ptr()) : nullptr, B, tokens};
+    return true;
+}
+
+// [tokens, heads, head_dim] of one of the three types, columns next to each other
+const at::Tensor *head_rows(PyObject *o, int64_t d, bifeat_head_rows *r, int32_t *dtype) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda() || t.dim() != 3 || t.layout() != at::kStrided || !t.unsafeGetTensorImpl()->has_storage() ||
+        t.size(2) != d || t.stride(2) != 1)
+        return nullptr;
+    const auto type = t.scalar_type();
+    if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return nullptr;
+    *dtype = type == at::kFloat ? BIFEAT_F32 : type == at::kHalf ? BIFEAT_F16 : BIFEAT_BF16;
+    *r = {t.data_ptr(), t.stride(0), t.stride(1)};
+    return &t;
+}
+
+// cache_write(..., pages, k, v, tables, lengths, indptr): the status, or None
+PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    try {
+        Cache c;
+        bifeat_head_rows k, v;
+        bifeat_cache_batch b;
+        int32_t dtype, other;
+        void *s = nullptr;
+        const at::Tensor *tk, *tv;
+        if (!cache_of(a, &c) || !(tk = head_rows(a[6], c.d, &k, &dtype)) || !(tv = head_rows(a[7], c.d, &v, &other)) || dtype != other ||
+            tk->size(1) != c.heads || tv->size(1) != c.heads || tk->size(0) != tv->size(0) || !batch_of(a + 8, tk->size(0), &b) ||
+            !stream(&s)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const int64_t count = c.pages->size(0);
+        auto *p = static_cast<uint8_t *>(c.pages->data_ptr());
+        int status;
+        {
+            Released interpreter;
+            status = reinterpret_cast<CacheWriteFn>(c.fn)(static_cast<bifeat_cache *>(c.handle), p, count, &b, &k, &v, dtype, s);
+        }
+        return PyLong_FromLong(status);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// cache_read(..., pages, tokens, dtype, tables, lengths, indptr): (k, v), an error status, or None
+PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    try {
+        Cache c;
+        bifeat_cache_batch b;
+        void *s = nullptr;
+        const int64_t tokens = PyLong_AsLongLong(a[6]), dtype = PyLong_AsLongLong(a[7]);
+        if (PyErr_Occurred() || tokens < 0 || !cache_of(a, &c) || !batch_of(a + 8, tokens, &b) || !stream(&s)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const int64_t count = c.pages->size(0);
+        const auto *p = static_cast<const uint8_t *>(c.pages->data_ptr());
+        const auto options = at::TensorOptions()
+                                 .dtype(dtype == BIFEAT_F32 ? at::kFloat : dtype == BIFEAT_F16 ? at::kHalf : at::kBFloat16)
+                                 .device(c.pages->device());
+        at::Tensor k, v;
+        int status;
+        {
+            Released interpreter;
+            k = torch::empty({tokens, c.heads, c.d}, options);
+            v = torch::empty({tokens, c.heads, c.d}, options);
+            status = reinterpret_cast<CacheReadFn>(c.fn)(static_cast<bifeat_cache *>(c.handle), p, count, &b, k.data_ptr(), v.data_ptr(),
+                                                         (int32_t)dtype, s);
+        }
+        if (status != 0) return PyLong_FromLong(status);
+        PyObject *pk = THPVariable_Wrap(k), *pv = pk ? THPVariable_Wrap(v) : nullptr, *both = pv ? PyTuple_Pack(2, pk, pv) : nullptr;
+        Py_XDECREF(pk);
+        Py_XDECREF(pv);
+        return both;
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// cache_attend(..., pages, q, scale, softcap, window, prefix, slopes, tables, lengths, indptr): the output, an error status, or None
+PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 15) Py_RETURN_NONE;
+    try {
+        Cache c;
+        bifeat_head_rows q;
+        bifeat_cache_batch b;
+        bifeat_attend_options o{};
+        int32_t dtype;
+        void *s = nullptr;
+        const at::Tensor *tq, *prefix = nullptr, *slopes = nullptr;
+        o.scale = (float)PyFloat_AsDouble(a[7]);
+        o.softcap = (float)PyFloat_AsDouble(a[8]);
+        o.window = PyLong_AsLongLong(a[9]);
+        if (PyErr_Occurred() || !cache_of(a, &c) || !(tq = head_rows(a[6], c.d, &q, &dtype)) || !batch_of(a + 12, tq->size(0), &b) ||
+            (a[10] != Py_None && (!(prefix = tensor(a[10], at::kLong, at::kLong)) || prefix->dim() != 1 || prefix->size(0) != b.sequences)) ||
+            (a[11] != Py_None && (!(slopes = tensor(a[11], at::kFloat, at::kFloat)) || slopes->dim() != 1 || slopes->size(0) != tq->size(1))) ||
+            tq->size(1) > INT32_MAX || !stream(&s)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        if (prefix) o.prefix = static_cast<const int64_t *>(prefix->data_ptr());
+        if (slopes) o.slopes = static_cast<const float *>(slopes->data_ptr());
+        const int64_t count = c.pages->size(0);
+        const auto *p = static_cast<const uint8_t *>(c.pages->data_ptr());
+        at::Tensor out;
+        int status;
+        {
+            Released interpreter;
+            out = torch::empty(tq->sizes(), at::TensorOptions().dtype(tq->scalar_type()).device(tq->device()));
+            status = reinterpret_cast<CacheAttendFn>(c.fn)(static_cast<bifeat_cache *>(c.handle), p, count, &b, &q, (int32_t)tq->size(1), dtype,
+                                                           &o, out.data_ptr(), s);
+        }
+        return finish(status, out);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 PyMethodDef methods[] = {
     {"gather_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gather_dequant)), METH_FASTCALL, nullptr},
     {"aggregate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(aggregate)), METH_FASTCALL, nullptr},
+    {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, nullptr},
+    {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
+    {"cache_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attend)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 
