@@ -1,6 +1,8 @@
 // The paged cache: what its translation units share.
 #pragma once
 
+#include <type_traits>
+
 #include "common.hpp"
 
 struct bifeat_cache {

@@ -7,7 +7,9 @@ namespace bf {
 namespace {
 
 constexpr int kCUs = 256;
-constexpr int kRowsWorkgroups = 3 * kCUs, kChunkWorkgroups = 2 * kCUs;  // as many as run at a time
+// workgroups: as many as run at a time
+constexpr int rows_workgroups(int dp) { return kCUs * (dp == 64 ? 3 : dp == 128 ? 2 : 1); }
+constexpr int chunk_workgroups(int dp, int np) { return kCUs * (dp == 256 && np == 2 ? 1 : 2); }
 
 // Joins the parts of the items that several workgroups have.  Blocks (w, y): the item that workgroup w goes on with, if it is the
 // first to go on with it; WAVES waves a query row, 16 lanes a part.  The parts' order in the sums is fixed by their number.
@@ -110,7 +112,7 @@ int items_of(const AttendCall &a, int R) {
 }
 
 constexpr size_t kPartialFloats =
-    2 * 258 * std::max((size_t)kRowsWorkgroups * kRowsR, (size_t)kChunkWorkgroups * 64 * kChunkNT);
+    2 * (size_t)chunk_workgroups(128, 1) * 128 * (128 + 2);  // (the most that any kernel's leave: 128 rows of 128 columns)
 
 }  // namespace
 
@@ -125,7 +127,7 @@ bool ensure_partial(bifeat_cache *h, hipStream_t s) {
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone) return false;
     void *p = nullptr;
-    if (hipMalloc(&p, sizeof(float) * kPartialFloats + sizeof(PartOf) * std::max(kRowsWorkgroups, kChunkWorkgroups)) != hipSuccess) {
+    if (hipMalloc(&p, sizeof(float) * kPartialFloats + sizeof(PartOf) * rows_workgroups(64)) != hipSuccess) {
         (void)hipGetLastError();
         return false;
     }
@@ -136,7 +138,8 @@ bool ensure_partial(bifeat_cache *h, hipStream_t s) {
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     const int dp = a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256, bits = h->spec.bits;
     const bool chunk = a.b.tokens * a.group > (int64_t)32 * a.b.B;
-    const int R = chunk ? 64 * kChunkNT : kRowsR, tok = !chunk ? kRowsTok : dp == 256 ? 32 : 64;
+    const int np = a.dtype == BIFEAT_F32 ? 2 : 1;
+    const int R = chunk ? 64 * chunk_tiles(dp, np) : kRowsR, tok = !chunk ? kRowsTok : dp == 256 ? 32 : 64;
     AttendPlan p;
     p.items = items_of(a, R);
     const int64_t most = ((a.b.width << a.c.ps_log2) + tok - 1) / tok, all = (int64_t)p.items * a.c.heads;
@@ -144,11 +147,11 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     const bool split = most > 4 && all * most <= INT32_MAX && ensure_partial(h, a.s);
     p.partial = split ? h->d_partial : nullptr;
     p.begins = split ? reinterpret_cast<PartOf *>(h->d_partial + kPartialFloats) : nullptr;
-    p.nw = (int)(split ? std::min<int64_t>(all * most, chunk ? kChunkWorkgroups : kRowsWorkgroups) : all);
+    p.nw = (int)(split ? std::min<int64_t>(all * most, chunk ? chunk_workgroups(dp, np) : rows_workgroups(dp)) : all);
     const int rows = a.b.indptr ? R : std::min(R, a.b.n * a.group);
     if (chunk) {
         if (hipError_t e = launch_attend_chunk(a, p, bits, dp)) return e;
-        if (split) launch_join<64 * kChunkNT>(a, p, dp, rows);
+        if (split) R == 128 ? launch_join<128>(a, p, dp, rows) : launch_join<64>(a, p, dp, rows);
     } else {
         launch_attend_rows(a, p, bits, dp);
         if (split) launch_join<kRowsR>(a, p, dp, rows);

@@ -18,7 +18,10 @@
 namespace bf {
 
 constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel for few rows
-constexpr int kChunkNT = 2;                   // tiles of 16 rows a wave in the kernel for many
+// Tiles of 16 rows a wave in the kernel for many.  None of these kernels may spill vector registers: this compiler (clang 22
+// for gfx950) has been seen to place such a spill at the join of a divergent branch before it restores the lanes' mask, so
+// that the lanes outside the branch got their values back wrong.  Two tiles where sums and queries leave room for it.
+constexpr int chunk_tiles(int dp, int np) { return dp == 64 || (dp == 128 && np == 1) ? 2 : 1; }
 constexpr float kLog2e = 1.4426950408889634f;
 // A row's weights are p = 2^(x - top), and fp16 gets p * s: `top` follows the largest x + log2(s), so that scales of values of
 // any size fit.  It may lag (products up to 2^15) and is brought up for all lanes of a row together, to leave them 2^8.  Rows
@@ -80,7 +83,7 @@ __device__ inline View view_of(const AttendCall &a, int b, int rt) {
     v.n = (int)a.b.count(b);
     const int rows = v.n * a.group;
     if (rt * R >= rows) {
-        v.units = 0;
+        v.first = v.last = v.prefix = v.skip_at = v.skip = v.units = 0;
         return v;
     }
     const int end_row = rt * R + R < rows ? rt * R + R : rows;
@@ -97,6 +100,15 @@ __device__ inline View view_of(const AttendCall &a, int b, int rt) {
     if (v.skip < 0) v.skip = 0;
     v.units = total - v.skip > 1 ? total - v.skip : 1;  // an item that sees nothing still has its zeros to write
     return v;
+}
+
+// The same value in all lanes, in a scalar register.
+__device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ inline int64_t uniform(int64_t x) {
+    return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32;
+}
+__device__ inline View uniform(const View &v) {
+    return {uniform(v.len), uniform(v.n), uniform(v.first), uniform(v.last), uniform(v.prefix), uniform(v.skip_at), uniform(v.skip), uniform(v.units)};
 }
 
 struct Place {
@@ -124,12 +136,12 @@ __device__ inline void locate(const AttendCall &a, const AttendPlan &p, int w, i
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
     if (!p.partial) {
         const int item = w % p.items;
-        at->seq = sequence_of_item<R>(a, item);
-        at->rt = item - first_item<R>(a, at->seq);
+        at->seq = uniform(sequence_of_item<R>(a, item));
+        at->rt = uniform(item - first_item<R>(a, at->seq));
         at->unit = 0;
         *head = w / p.items;
         *start = 0;
-        *end = view_of<R, TOK>(a, at->seq, at->rt).units;
+        *end = uniform(view_of<R, TOK>(a, at->seq, at->rt).units);
         return;
     }
     // a thread sums the units of some of a head's items
@@ -191,7 +203,7 @@ template <int R>
 __device__ inline void next_item(const AttendCall &a, int *head, Place *at) {
     at->unit = 0;
     at->rt++;
-    while (at->rt * R >= (int)a.b.count(at->seq) * a.group) {
+    while (at->rt * R >= uniform((int)a.b.count(at->seq)) * a.group) {
         at->rt = 0;
         if (++at->seq == a.b.B) {
             at->seq = 0;
@@ -303,6 +315,28 @@ __device__ inline void store_columns(const AttendCall &a, int64_t at, int left, 
         for (int k = 0; k < N; k++)
             if (k < left) store_result(a, at + k, x[k]);
     }
+}
+
+// What a query row sees, as bounds for a position: t <= high and t > low, or t < prefix.
+struct Sight {
+    int high, low, prefix;
+};
+__device__ inline Sight sight_of(const AttendCall &a, const View &v, int pos) {
+    Sight s;
+    s.high = pos < v.len ? pos : v.len - 1;  // (-1 or less for a row that is not there, or lies before the beginning: nothing)
+    s.low = a.window && pos - a.window >= 0 ? (int)(pos - a.window) : -1;
+    s.prefix = pos >= 0 ? v.prefix : 0;
+    return s;
+}
+// the same of positions at + 0, 1, 2, 3, 16, 17, 18, 19 as eight bits
+__device__ inline uint32_t seen_of(const Sight &s, int at) {
+    uint32_t seen = 0;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const int t = 16 * (e / 4) + e % 4;
+        seen |= (uint32_t)((t <= s.high - at && t > s.low - at) || t < s.prefix - at) << e;
+    }
+    return seen;
 }
 
 // y * f in units of log2, with the cap and the bias by distance (slope in the same units)

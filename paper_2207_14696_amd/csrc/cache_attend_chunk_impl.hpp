@@ -24,7 +24,8 @@ struct ChunkShape {
     static constexpr int KEYS = TOK / 16 * KS, VALUES = TOK / 32 * VT;
 };
 
-template <int BITS, int DP, int NP, int NT>
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); SHAPED: scores are capped or biased
+template <int BITS, int DP, int NP, int NT, bool SHAPED>
 __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chunk_kernel(AttendCall a, AttendPlan plan) {
     using S = ChunkShape<BITS, DP, NT>;
     constexpr int R = S::R, TOK = S::TOK;
@@ -53,14 +54,15 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
     }
     const int vo = (n16 * S::VP + vpart) * S::VB;
     const uint32_t voff = 4 * g * rb + (vo < rb ? vo : 0);
-    // thread t < TOK brings the floats of four positions: array t / (TOK / 4), positions 4 (t % (TOK / 4))
-    const int farray = threadIdx.x / (TOK / 4) & 3, fat = 4 * (threadIdx.x % (TOK / 4));
+    // wave w brings array w of the floats in LDS, a position a lane: key scale times f, key offset (NP == 2: the middle
+    // code's value), value scale, value of the middle code
+    const int fat = lane % TOK;
 
     while (cur < end) {
-        const View v = view_of<R, TOK>(a, at.seq, at.rt);
+        const View v = uniform(view_of<R, TOK>(a, at.seq, at.rt));
         const int units = v.units - at.unit < end - cur ? v.units - at.unit : end - cur;
         const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
-        const int64_t token0 = a.b.first(at.seq);
+        const int64_t token0 = uniform(a.b.first(at.seq));
 
         // ---- pages: lane (TOK / 16) i + j has the page of 16 positions, the j-th of the item's tile `paged` + i
         int pages = 0, paged = -64;
@@ -71,7 +73,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
             return (u < v.skip_at ? u : u + v.skip) * TOK;
         };
         uint32_t kw[S::KB / 4], vw[8][S::VW];
-        float4 fw;
+        float fscale, fmin = 0.f;
         auto load = [&](int u) {
             if (u - paged >= 64 / kSub) {
                 paged = u;
@@ -95,11 +97,10 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 #pragma unroll
                 for (int i = 0; i < 4; i++) load_bytes<S::VB>(b, voff, all + i * rb, vw[4 * j + i]);
             }
-            const int page = __shfl(pages, at16 + fat / 16);  // (from any lane: all take part)
-            if (threadIdx.x < TOK) {
-                const uint8_t *fp = a.c.block(page, head) + a.c.floats(0) + ((int64_t)farray * 4 << a.c.ps_log2);
-                fw = *reinterpret_cast<const float4 *>(fp + 4 * ((base + fat) & (a.c.ps() - 1)));
-            }
+            const int page = __shfl(pages, at16 + fat / 16);
+            const uint8_t *fp = a.c.block(page, head) + a.c.floats(wave / 2) + 4 * ((base + fat) & (a.c.ps() - 1));
+            fscale = *reinterpret_cast<const float *>(fp);
+            if (wave & 1) fmin = *reinterpret_cast<const float *>(fp + (4 << a.c.ps_log2));
         };
         float f = 0.f;  // scale of the products, in units of log2
         auto make = [&](int u, int buf) {
@@ -131,16 +132,12 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 if constexpr (NP == 2) val = centred(val, all_of(BITS == 8 || (t & 1) ? 1152.f : 1032.f));
                 values[buf][vgroup * S::VT + vpart * (S::VT / S::VP) + t][lane] = __builtin_bit_cast(uint4, val);
             }
-            if (threadIdx.x < TOK) {
-                // what no token was written to may hold anything
-                const int left = v.len - base_of(u) - fat;
-                float4 x = fw;
-                if (left < 4) x.w = 0.f;
-                if (left < 3) x.z = 0.f;
-                if (left < 2) x.y = 0.f;
-                if (left < 1) x.x = 0.f;
-                *reinterpret_cast<float4 *>(&params[buf][farray][fat]) = x;
-            }
+            const bool there = base_of(u) + fat < v.len;  // what no token was written to may hold anything
+            float x = there ? fscale : 0.f;
+            if (wave >= 2) x = fmaxf(x, kLeastScale);
+            if (wave == 0) x *= f;
+            if (wave & 1) x = fmaf(x, wave == 3 || NP == 2 ? kMiddle : 0.f, there ? fmin : 0.f);
+            if (lane < TOK) params[buf][wave][fat] = x;
         };
 
         if (v.len > 0) load(0);
@@ -149,23 +146,21 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
         const int wrow0 = row0 + 16 * NT * wave;  // of the sequence
         half8 q[NP][NT][S::KS];
         float qsum[NT], slope[NT];
-        int pos[NT], low[NT];
-        float big = 0.f;
+        int pos[NT];
+        auto query = [&](int n, float(&x)[DP / 4]) {
+            const int row = wrow0 + 16 * n + n16;
+#pragma unroll
+            for (int i = 0; i < DP / 4; i++) x[i] = 0.f;
+            if (row - row0 < nrows) load_query<DP / 4>(a, token0 + row / a.group, head * a.group + row % a.group, g * (DP / 4), x);
+        };
         {
-            float x[NT][DP / 4];
+            float big = 0.f;
 #pragma unroll
             for (int n = 0; n < NT; n++) {
-                const int row = wrow0 + 16 * n + n16;
-                const bool real = row - row0 < nrows;
-                const int qi = row / a.group, qh = head * a.group + row % a.group;
-                pos[n] = real ? v.len - v.n + qi : -1;
-                low[n] = a.window && pos[n] - a.window >= 0 ? (int)(pos[n] - a.window) : -1;
-                slope[n] = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+                float x[DP / 4];
+                query(n, x);
 #pragma unroll
-                for (int i = 0; i < DP / 4; i++) x[n][i] = 0.f;
-                if (real) load_query<DP / 4>(a, token0 + qi, qh, g * (DP / 4), x[n]);
-#pragma unroll
-                for (int i = 0; i < DP / 4; i++) big = fmaxf(big, fabsf(x[n][i]) <= 3.402823466e38f ? fabsf(x[n][i]) : 0.f);
+                for (int i = 0; i < DP / 4; i++) big = fmaxf(big, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
             }
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
@@ -176,10 +171,11 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
             f = a.scale * kLog2e * (kUnit<NP> / up);
 #pragma unroll
             for (int n = 0; n < NT; n++) {
-                float sum = 0.f;
+                float x[DP / 4], sum = 0.f;
+                query(n, x);
 #pragma unroll
                 for (int i = 0; i < DP / 4; i++) {
-                    const float y = x[n][i] * up;
+                    const float y = x[i] * up;
                     const _Float16 hi = (_Float16)y;
                     const _Float16 lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
                     sum += (float)hi + (float)lo;
@@ -191,29 +187,30 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 qsum[n] = sum * (f / kUnit<NP>);
+                const int row = wrow0 + 16 * n + n16;
+                const bool real = row - row0 < nrows;
+                pos[n] = real ? v.len - v.n + row / a.group : -1;
+                slope[n] = SHAPED && a.slopes && real ? a.slopes[head * a.group + row % a.group] * kLog2e : 0.f;
             }
         }
         const float cap = a.softcap * kLog2e;
-        const bool shaped = a.softcap > 0.f || a.slopes;
         // first and last position of the wave's queries
         const int wend = wrow0 + 16 * NT < row0 + nrows ? wrow0 + 16 * NT : row0 + nrows;
         const bool any_row = wrow0 < row0 + nrows;
         const int wfirst = v.len - v.n + wrow0 / a.group, wlast = v.len - v.n + (wend - 1) / a.group;
 
-        float top[NT], total[NT], mins[NT], weights[NT];
+        float top[NT], total[NT], mins[NT];  // mins: what is not in the products with the codes
         float4v o[NT][S::VT];
 #pragma unroll
         for (int n = 0; n < NT; n++) {
             top[n] = kNothing;
-            total[n] = mins[n] = weights[n] = 0.f;
+            total[n] = mins[n] = 0.f;
 #pragma unroll
             for (int t = 0; t < S::VT; t++) o[n][t] = float4v{0.f, 0.f, 0.f, 0.f};
         }
 
-        // 32 positions for the wave's rows
-        auto half_tile = [&](int base, int buf, int hf) {
-            const bool whole = base + 32 <= v.len && wfirst >= 0 &&
-                               ((base + 31 <= wfirst && (!a.window || base > wlast - a.window)) || base + 32 <= v.prefix);
+        // 32 positions for the wave's rows; `whole`: all of them see all
+        auto half_tile = [&](bool whole, int base, int buf, int hf) {
             float4v acc[NT][2];
 #pragma unroll
             for (int n = 0; n < NT; n++) acc[n][0] = acc[n][1] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -236,43 +233,45 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 #pragma unroll
                 for (int i = 0; i < 4; i++) {
                     const int e = 4 * j + i;
-                    ks[e] = (&p[0].x)[i] * f;
-                    km[e] = NP == 2 ? fmaf((&p[0].x)[i], kMiddle, (&p[1].x)[i]) : (&p[1].x)[i];
-                    vs[e] = fmaxf((&p[2].x)[i], kLeastScale);
-                    vm[e] = fmaf(vs[e], kMiddle, (&p[3].x)[i]);
+                    ks[e] = (&p[0].x)[i];
+                    km[e] = (&p[1].x)[i];
+                    vs[e] = (&p[2].x)[i];
+                    vm[e] = (&p[3].x)[i];
                 }
             }
             half8 w[NP][NT];
 #pragma unroll
             for (int n = 0; n < NT; n++) {
                 uint32_t seen = 0xffu;
-                if (!whole) {
-                    seen = 0;
+                if (!whole) seen = seen_of(sight_of(a, v, pos[n]), base + 4 * g);
+                float x[8], p[8], pw[8];
+                if constexpr (SHAPED) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = fmaf(ks[e], acc[n][e / 4][e % 4], km[e] * qsum[n]);
+                    if (a.softcap > 0.f)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) x[e] = capped(x[e], cap);
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = fmaf(slope[n], (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos[n]), x[e]);
+                }
+                // scores less `ref`, -infinity where the row does not see the position
+                float y[8];
+                auto score = [&](float ref) {
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        const int t = base + 16 * (e / 4) + 4 * g + e % 4;
-                        const bool is = t < v.len && pos[n] >= 0 && ((t <= pos[n] && t > low[n]) || t < v.prefix);
-                        seen |= (uint32_t)is << e;
+                        if constexpr (SHAPED) y[e] = x[e] - ref;
+                        else y[e] = fmaf(ks[e], acc[n][e / 4][e % 4], fmaf(km[e], qsum[n], -ref));
                     }
-                }
-                // score of position e less `ref`
-                auto score = [&](int e, float ref) {
-                    float x;
-                    if (!shaped) {
-                        x = fmaf(ks[e], acc[n][e / 4][e % 4], fmaf(km[e], qsum[n], -ref));
-                    } else {
-                        x = fmaf(ks[e], acc[n][e / 4][e % 4], km[e] * qsum[n]);
-                        if (a.softcap > 0.f) x = capped(x, cap);
-                        x = fmaf(slope[n], (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos[n]), x) - ref;
-                    }
-                    return whole || (seen >> e & 1) ? x : -INFINITY;
+                    if (!whole)
+#pragma unroll
+                        for (int e = 0; e < 8; e++) y[e] = seen >> e & 1 ? y[e] : -INFINITY;
                 };
-                float p[8], pw[8];
                 auto weigh = [&] {
                     float most = 0.f;
+                    score(top[n]);
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        p[e] = __builtin_amdgcn_exp2f(score(e, top[n]));
+                        p[e] = __builtin_amdgcn_exp2f(y[e]);
                         pw[e] = p[e] * vs[e];
                         most = fmaxf(most, pw[e]);
                     }
@@ -280,8 +279,9 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 };
                 if (__any(weigh() > 32768.f)) {
                     float now = kNothing;
+                    score(0.f);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) now = fmaxf(now, score(e, 0.f) + __builtin_amdgcn_logf(vs[e]));
+                    for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(vs[e]));
                     now = fmaxf(now, __shfl_xor(now, 16));
                     now = fmaxf(now, __shfl_xor(now, 32));
                     now = fmaxf(top[n], now - 8.f);
@@ -289,24 +289,30 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                     top[n] = now;
                     total[n] *= keep;
                     mins[n] *= keep;
-                    weights[n] *= keep;
 #pragma unroll
                     for (int t = 0; t < S::VT; t++) o[n][t] *= keep;
                     weigh();
                 }
+                if (whole) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) mins[n] = fmaf(p[e], vm[e], mins[n]);
+                } else {  // (an infinity or NaN that the row does not see is not to reach it)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) {
+                        mins[n] = seen >> e & 1 ? fmaf(p[e], vm[e], mins[n]) : mins[n];
+                        pw[e] = seen >> e & 1 ? pw[e] : 0.f;
+                    }
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    float pm = vm[e];
-                    if (!whole && !(seen >> e & 1)) pw[e] = pm = 0.f;  // (an infinity or NaN that the row does not see)
                     total[n] += p[e];
-                    mins[n] = fmaf(p[e], pm, mins[n]);
                     w[0][n][e] = (_Float16)pw[e];
                     if constexpr (NP == 2) w[NP - 1][n][e] = (_Float16)(pw[e] - (float)w[0][n][e]);
                 }
                 if constexpr (NP == 1)
 #pragma unroll
                     for (int e = 0; e < 8; e += 2)
-                        weights[n] = __builtin_amdgcn_fdot2(half2v{w[0][n][e], w[0][n][e + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, weights[n], false);
+                        mins[n] = __builtin_amdgcn_fdot2(half2v{w[0][n][e], w[0][n][e + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins[n], false);
             }
 #pragma unroll
             for (int t = 0; t < S::VT; t++) {
@@ -327,12 +333,15 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 if (u + 1 < units) make(u + 1, buf ^ 1);
                 if (u + 2 < units) load(u + 2);
                 if (any_row)
-#pragma unroll
+#pragma unroll 1
                     for (int hf = 0; hf < TOK / 32; hf++) {
                         const int b = base + 32 * hf;
                         // positions that none of the wave's rows sees
                         if (b >= v.len || ((b > wlast || (a.window && b + 31 <= wfirst - a.window)) && b >= v.prefix)) continue;
-                        half_tile(b, buf, hf);
+                        // do all rows see all of them?
+                        const bool whole = b + 32 <= v.len && wfirst >= 0 &&
+                                           ((b + 31 <= wfirst && (!a.window || b > wlast - a.window)) || b + 32 <= v.prefix);
+                        half_tile(whole, b, buf, hf);
                     }
                 __syncthreads();
             }
@@ -342,16 +351,14 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
         if (any_row)
 #pragma unroll
             for (int n = 0; n < NT; n++) {
-                float s = total[n], m = mins[n], ws = weights[n];
+                float s = total[n], rest = mins[n];
                 s += __shfl_xor(s, 16);
                 s += __shfl_xor(s, 32);
-                m += __shfl_xor(m, 16);
-                m += __shfl_xor(m, 32);
-                ws += __shfl_xor(ws, 16);
-                ws += __shfl_xor(ws, 32);
+                rest += __shfl_xor(rest, 16);
+                rest += __shfl_xor(rest, 32);
                 const int r = 16 * (NT * wave + n) + n16, row = row0 + r;
                 if (r >= nrows) continue;
-                const float rest = m - ws * kMiddle, inv = s != 0.f ? 1.f / s : 0.f;
+                const float inv = s != 0.f ? 1.f / s : 0.f;
                 const int64_t dst = ((token0 + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
                 float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2));
                 if (!complete && g == 0) part[R * DP + r] = top[n], part[R * DP + R + r] = s;

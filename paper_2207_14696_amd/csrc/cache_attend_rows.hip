@@ -3,8 +3,11 @@
 namespace bf {
 template <int BITS, int DP>
 static void go(const AttendCall &a, const AttendPlan &p) {
-    if (a.dtype == BIFEAT_F32) attend_rows_kernel<BITS, DP, 2><<<p.nw, 256, 0, a.s>>>(a, p);
-    else attend_rows_kernel<BITS, DP, 1><<<p.nw, 256, 0, a.s>>>(a, p);
+    const bool shaped = a.softcap > 0.f || a.slopes;
+    auto kernel = a.dtype == BIFEAT_F32 ? shaped ? attend_rows_kernel<BITS, DP, 2, true> : attend_rows_kernel<BITS, DP, 2, false>
+                  : shaped              ? attend_rows_kernel<BITS, DP, 1, true>
+                                        : attend_rows_kernel<BITS, DP, 1, false>;
+    kernel<<<p.nw, 256, 0, a.s>>>(a, p);
 }
 void launch_attend_rows(const AttendCall &a, const AttendPlan &p, int bits, int dp) {
     if (bits == 8) dp == 64 ? go<8, 64>(a, p) : dp == 128 ? go<8, 128>(a, p) : go<8, 256>(a, p);

@@ -24,9 +24,9 @@ struct RowLanes {
     static constexpr int VW = VB < 4 ? 1 : VB / 4;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries)
-template <int BITS, int DP, int NP>
-__global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); SHAPED: scores are capped or biased
+template <int BITS, int DP, int NP, bool SHAPED>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
     using L = RowLanes<BITS, DP>;
     constexpr int R = kRowsR, TOK = kRowsTok;
     constexpr float kMiddle = 1 << (BITS - 1);
@@ -55,10 +55,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
     const uint32_t foff = ((lane >> 3 & 3) * 4u << a.c.ps_log2) + 16 * (lane & 3);
 
     while (cur < end) {
-        const View v = view_of<R, TOK>(a, at.seq, at.rt);
+        const View v = uniform(view_of<R, TOK>(a, at.seq, at.rt));
         const int units = v.units - at.unit < end - cur ? v.units - at.unit : end - cur;
         const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
-        const int64_t token0 = a.b.first(at.seq);
+        const int64_t token0 = uniform(a.b.first(at.seq));
 
         // ---- the queries: lane (n16, g) has a quarter of the columns of row n16, those of the keys that it reads
         const int row = row0 + n16;
@@ -97,12 +97,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             qsum += __shfl_xor(qsum, 32);
             qsum *= f / kUnit<NP>;
         }
-        const float slope = a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+        const float slope = SHAPED && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
         const float cap = a.softcap * kLog2e;
-        const bool shaped = a.softcap > 0.f || a.slopes;
-        const int low = a.window && pos - a.window >= 0 ? (int)(pos - a.window) : -1;  // positions above it are in the window
 
-        float top = kNothing, total = 0.f, mins = 0.f, weights = 0.f;
+        float top = kNothing, total = 0.f, mins = 0.f;  // mins: what is not in the products with the codes
         float4v o[L::VT];
 #pragma unroll
         for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -145,11 +143,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             for (int i = 0; i < 4; i++) load_bytes<L::VB>(block1, voff, at1 + i * rb, vw[4 + i]);
         };
 
-        auto step = [&](int u) {
-            const int base = base_of(u);
-            // all rows see all 32 positions?
-            const bool whole = base + 32 <= v.len && v.first >= 0 &&
-                               ((base + 31 <= v.first && (!a.window || base > v.last - a.window)) || base + 32 <= v.prefix);
+        auto step = [&](bool whole, int base, bool more, int next) {
             wave_sync();
             if (lane < 32) *reinterpret_cast<float4 *>(&params[wave][lane >> 3][4 * (lane & 7)]) = fw;
             wave_sync();
@@ -169,15 +163,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                 }
             }
             uint32_t seen = 0xffu;
-            if (!whole) {
-                seen = 0;
-#pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    const int t = base + 16 * (e / 4) + 4 * g + e % 4;
-                    const bool is = t < v.len && pos >= 0 && ((t <= pos && t > low) || t < v.prefix);
-                    seen |= (uint32_t)is << e;
-                }
-            }
+            if (!whole) seen = seen_of(sight_of(a, v, pos), base + 4 * g);
             // ---- scores
             float4v acc[2];
 #pragma unroll
@@ -198,22 +184,35 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                     for (int p = 0; p < NP; p++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc[j], 0, 0, 0);
                 }
             }
-            if (u + 1 < units) load_keys(u + 1);
-            // score of position e less `ref`
-            auto score = [&](int e, float ref) {
-                float x = fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum);
-                if (shaped) {
-                    if (a.softcap > 0.f) x = capped(x, cap);
-                    x = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x);
-                }
-                return whole || (seen >> e & 1) ? x - ref : -INFINITY;
-            };
-            float p[8], pw[8];
-            auto weigh = [&] {
-                float most = 0.f;
+            if (more) load_keys(next);
+            float x[8], p[8], pw[8];
+            if constexpr (SHAPED) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum);
+                if (a.softcap > 0.f)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) x[e] = capped(x[e], cap);
+#pragma unroll
+                for (int e = 0; e < 8; e++) x[e] = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x[e]);
+            }
+            // scores less `ref`, -infinity where the row does not see the position
+            float y[8];
+            auto score = [&](float ref) {
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    p[e] = __builtin_amdgcn_exp2f(score(e, top));
+                    if constexpr (SHAPED) y[e] = x[e] - ref;
+                    else y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, -ref));
+                }
+                if (!whole)
+#pragma unroll
+                    for (int e = 0; e < 8; e++) y[e] = seen >> e & 1 ? y[e] : -INFINITY;
+            };
+            auto weigh = [&] {
+                float most = 0.f;
+                score(top);
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    p[e] = __builtin_amdgcn_exp2f(y[e]);
                     pw[e] = p[e] * vs[e];
                     most = fmaxf(most, pw[e]);
                 }
@@ -221,8 +220,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             };
             if (__any(weigh() > 32768.f)) {
                 float now = kNothing;
+                score(0.f);
 #pragma unroll
-                for (int e = 0; e < 8; e++) now = fmaxf(now, score(e, 0.f) + __builtin_amdgcn_logf(vs[e]));
+                for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(vs[e]));
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(now, __shfl_xor(now, 32));
                 now = fmaxf(top, now - 8.f);
@@ -230,26 +230,32 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
                 top = now;
                 total *= keep;
                 mins *= keep;
-                weights *= keep;
 #pragma unroll
                 for (int t = 0; t < L::VT; t++) o[t] *= keep;
                 weigh();
             }
             // ---- weights
             half8 w[NP];
+            if (whole) {
+#pragma unroll
+                for (int e = 0; e < 8; e++) mins = fmaf(p[e], vm[e], mins);
+            } else {  // (an infinity or NaN that the row does not see is not to reach it)
+#pragma unroll
+                for (int e = 0; e < 8; e++) {
+                    mins = seen >> e & 1 ? fmaf(p[e], vm[e], mins) : mins;
+                    pw[e] = seen >> e & 1 ? pw[e] : 0.f;
+                }
+            }
 #pragma unroll
             for (int e = 0; e < 8; e++) {
-                float pm = vm[e];
-                if (!whole && !(seen >> e & 1)) pw[e] = pm = 0.f;  // (an infinity or NaN that the row does not see)
                 total += p[e];
-                mins = fmaf(p[e], pm, mins);
                 w[0][e] = (_Float16)pw[e];
                 if constexpr (NP == 2) w[NP - 1][e] = (_Float16)(pw[e] - (float)w[0][e]);
             }
             if constexpr (NP == 1)
 #pragma unroll
                 for (int e = 0; e < 8; e += 2)
-                    weights = __builtin_amdgcn_fdot2(half2v{w[0][e], w[0][e + 1]}, half2v{(_Float16)1.f, (_Float16)1.f}, weights, false);
+                    mins = __builtin_amdgcn_fdot2(half2v{w[0][e], w[0][e + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins, false);
             // ---- values: lane (n16, g) has columns [n16 DP/16, ...) of eight positions
 #pragma unroll
             for (int t = 0; t < L::VT; t++) {
@@ -274,8 +280,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
             load_keys(0);
             load_values();
             for (int u = 0; u < units; u++) {
-                if (base_of(u) < v.len) step(u);  // (of an item's last unit some waves may have no positions)
-                if (u + 1 < units) load_values();
+                const int base = base_of(u);
+                const bool more = u + 1 < units;
+                if (base < v.len) {  // (of an item's last unit some waves may have no positions)
+                    // do all rows see all 32 positions?
+                    const bool whole = base + 32 <= v.len && v.first >= 0 &&
+                                       ((base + 31 <= v.first && (!a.window || base > v.last - a.window)) || base + 32 <= v.prefix);
+                    step(whole, base, more, u + 1);
+                }
+                if (more) load_values();
             }
         }
 
@@ -284,14 +297,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 2 : 3) void attend_rows_kernel(Att
         total += __shfl_xor(total, 32);
         mins += __shfl_xor(mins, 16);
         mins += __shfl_xor(mins, 32);
-        weights += __shfl_xor(weights, 16);
-        weights += __shfl_xor(weights, 32);
-        const float rest = mins - weights * kMiddle;  // (NP == 2: the codes were less their middle already)
 #pragma unroll
         for (int t = 0; t < L::VT; t++) {
             const float back = kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f);
 #pragma unroll
-            for (int i = 0; i < 4; i++) sums[wave][n16][(4 * g + i) * L::VT + t] = fmaf(o[t][i], back, rest);
+            for (int i = 0; i < 4; i++) sums[wave][n16][(4 * g + i) * L::VT + t] = fmaf(o[t][i], back, mins);
         }
         if (g == 0) {
             tops[wave][n16] = top;

@@ -117,3 +117,45 @@ def test_reference_attention_is_softmax_attention():
     assert np.allclose(ref.attend(q, k, v, n, m, 0.4), want.transpose(0, 1).numpy(), atol=1e-12)
     assert not ref.attend(q, k[:3], v[:3], n, 3, 0.4)[:2].any()
     assert np.allclose(ref.attend(q, k, v, n, m, 0.4, window=1), np.repeat(v[m - n:], G, 1))
+
+
+def _kernels_of(library):
+    """(name, vector registers spilled) of the kernels in the library's code objects, from the notes that the compiler left."""
+    import re
+    import struct
+    import subprocess
+    import tempfile
+    data, at, found = open(library, "rb").read(), 0, []
+    magic = b"__CLANG_OFFLOAD_BUNDLE__"
+    while (at := data.find(magic, at)) >= 0:
+        count, = struct.unpack_from("<Q", data, at + 24)
+        p = at + 32
+        for _ in range(count):
+            offset, size, n = struct.unpack_from("<QQQ", data, p)
+            target = data[p + 24:p + 24 + n]
+            p += 24 + n
+            if b"gfx950" not in target or not size:
+                continue
+            with tempfile.NamedTemporaryFile(suffix=".co") as f:
+                f.write(data[at + offset:at + offset + size])
+                f.flush()
+                notes = subprocess.run([READELF, "--notes", f.name], capture_output=True, text=True, check=True).stdout
+            names = re.findall(r"\.name:\s+(_Z\S+)", notes)
+            spills = re.findall(r"\.vgpr_spill_count:\s+(\d+)", notes)
+            found += list(zip(names, map(int, spills)))
+        at += len(magic)
+    return found
+
+
+READELF = "/opt/rocm/llvm/bin/llvm-readelf"
+
+
+def test_the_attention_kernels_spill_no_vector_registers(bf):
+    # a spill at the join of a divergent branch was stored before the lanes' mask was restored: lanes outside the branch read
+    # another value back, a result's address among them
+    import os
+    if not os.path.exists(READELF):
+        pytest.skip("no llvm-readelf")
+    kernels = [(n, s) for n, s in _kernels_of(bf.library_path()) if "attend_" in n]
+    assert len(kernels) >= 40, len(kernels)
+    assert not [k for k in kernels if k[1]]
