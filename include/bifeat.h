@@ -422,6 +422,7 @@ typedef struct bifeat_cache bifeat_cache;
  * lies in page tables[b * table_width + j / page_size], slot j % page_size.
  * Where n_b > lengths[b], the first n_b - lengths[b] tokens lie before the sequence's
  * beginning: they are not written, read as zeros, and see nothing.
+ * A sequence has room for at most 2^30 positions (BIFEAT_EINVAL).
  * Contract (checked with option "validate" or by bifeat_cache_check): indptr begins with
  * 0, does not decrease and ends with `tokens`; 0 <= lengths[b] <= table_width *
  * page_size; table entries of pages below lengths[b] lie in [0, num_pages).  Others are

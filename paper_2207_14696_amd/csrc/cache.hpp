@@ -101,6 +101,8 @@ __device__ inline void store8_any(T *p, int left, const float (&x)[8]) {
     }
 }
 
+constexpr int kMostPositions = 1 << 30;  // of a sequence: positions, and their differences, are 32-bit numbers in the kernels
+
 struct HeadRows {
     const void *data;
     int64_t token_stride, head_stride;
@@ -113,7 +115,7 @@ struct AttendCall {
     int group;  // query heads a cached head
     int dtype;
     float scale, softcap;
-    int64_t window;
+    int window;  // 0: none; at most kMostPositions
     const int64_t *prefix;
     const float *slopes;
     void *out;

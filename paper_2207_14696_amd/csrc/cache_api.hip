@@ -2,6 +2,7 @@
 #include <math.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 
 #include "cache.hpp"
@@ -22,10 +23,10 @@ bool spec_ok(const bifeat_cache_spec *s) {
 bool type_ok(int32_t d) { return d == BIFEAT_F32 || d == BIFEAT_F16 || d == BIFEAT_BF16; }
 uintptr_t type_bytes(int32_t d) { return d == BIFEAT_F32 ? 4 : 2; }
 
-// The batch alone; rows: how many rows (of tokens x heads) the call's kernels are launched for.
-bool batch_ok(const bifeat_cache_batch *b, int64_t heads) {
+// The batch alone; heads: rows a token that the call's kernels are launched for.
+bool batch_ok(const bifeat_cache *c, const bifeat_cache_batch *b, int64_t heads) {
     if (!b || b->sequences < 0 || b->tokens < 0 || b->table_width < 0) return false;
-    if (b->sequences > INT32_MAX || b->table_width > INT32_MAX || b->tokens > (int64_t)INT32_MAX / heads) return false;
+    if (b->sequences > INT32_MAX || b->table_width > bf::kMostPositions / c->spec.page_size || b->tokens > (int64_t)INT32_MAX / heads) return false;
     if (b->tokens == 0) return true;
     if (b->sequences == 0 || !b->lengths || (b->table_width > 0 && !b->tables)) return false;
     if ((uintptr_t)b->lengths % 8 || (uintptr_t)b->indptr % 8 || (uintptr_t)b->tables % 4) return false;
@@ -63,7 +64,7 @@ int check(const bifeat_cache *c, int64_t num_pages, const bf::CacheBatch &b, hip
 // What the three calls ask of their common arguments.
 int common(const bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch, int64_t heads,
            int32_t dtype) {
-    if (!c || !type_ok(dtype) || num_pages < 0 || num_pages > INT32_MAX || !batch_ok(batch, heads)) return BIFEAT_EINVAL;
+    if (!c || !type_ok(dtype) || num_pages < 0 || num_pages > INT32_MAX || !batch_ok(c, batch, heads)) return BIFEAT_EINVAL;
     if ((uintptr_t)pages % 16 || (batch->tokens > 0 && num_pages > 0 && !pages)) return BIFEAT_EINVAL;
     return BIFEAT_OK;
 }
@@ -109,7 +110,7 @@ int bifeat_cache_reserve(bifeat_cache *c, void *stream) {
 }
 
 int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_cache_batch *batch, void *stream) {
-    if (!c || num_pages < 0 || !batch_ok(batch, 1)) return BIFEAT_EINVAL;
+    if (!c || num_pages < 0 || !batch_ok(c, batch, 1)) return BIFEAT_EINVAL;
     if (batch->tokens == 0) return BIFEAT_OK;
     return check(c, num_pages, batch_of(batch), (hipStream_t)stream);
 }
@@ -152,7 +153,7 @@ int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages
     if (c->opt_validate)
         if (int rc = check(c, num_pages, b, (hipStream_t)stream)) return rc;
     const bf::AttendCall a{pages_of(c, pages), b, rows_of(q), query_heads / c->spec.heads, dtype, options->scale, options->softcap,
-                           options->window, options->prefix, options->slopes, out, (hipStream_t)stream};
+                           (int)std::min<int64_t>(options->window, bf::kMostPositions), options->prefix, options->slopes, out, (hipStream_t)stream};
     BF_HIP(bf::launch_cache_attend(c, a));
     return BIFEAT_OK;
 }

@@ -262,9 +262,11 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                         if constexpr (SHAPED) y[e] = x[e] - ref;
                         else y[e] = fmaf(ks[e], acc[n][e / 4][e % 4], fmaf(km[e], qsum[n], -ref));
                     }
-                    if (!whole)
+                    if (!whole) {
+                        const uint32_t bits = here(seen);
 #pragma unroll
-                        for (int e = 0; e < 8; e++) y[e] = seen >> e & 1 ? y[e] : -INFINITY;
+                        for (int e = 0; e < 8; e++) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
+                    }
                 };
                 auto weigh = [&] {
                     float most = 0.f;
@@ -297,10 +299,11 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 #pragma unroll
                     for (int e = 0; e < 8; e++) mins[n] = fmaf(p[e], vm[e], mins[n]);
                 } else {  // (an infinity or NaN that the row does not see is not to reach it)
+                    const uint32_t bits = here(seen);
 #pragma unroll
                     for (int e = 0; e < 8; e++) {
-                        mins[n] = seen >> e & 1 ? fmaf(p[e], vm[e], mins[n]) : mins[n];
-                        pw[e] = seen >> e & 1 ? pw[e] : 0.f;
+                        mins[n] = bits >> e & 1 ? fmaf(p[e], vm[e], mins[n]) : mins[n];
+                        pw[e] = bits >> e & 1 ? pw[e] : 0.f;
                     }
                 }
 #pragma unroll

@@ -203,9 +203,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                     if constexpr (SHAPED) y[e] = x[e] - ref;
                     else y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, -ref));
                 }
-                if (!whole)
+                if (!whole) {
+                    const uint32_t bits = here(seen);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) y[e] = seen >> e & 1 ? y[e] : -INFINITY;
+                    for (int e = 0; e < 8; e++) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
+                }
             };
             auto weigh = [&] {
                 float most = 0.f;
@@ -240,10 +242,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
 #pragma unroll
                 for (int e = 0; e < 8; e++) mins = fmaf(p[e], vm[e], mins);
             } else {  // (an infinity or NaN that the row does not see is not to reach it)
+                const uint32_t bits = here(seen);
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    mins = seen >> e & 1 ? fmaf(p[e], vm[e], mins) : mins;
-                    pw[e] = seen >> e & 1 ? pw[e] : 0.f;
+                    mins = bits >> e & 1 ? fmaf(p[e], vm[e], mins) : mins;
+                    pw[e] = bits >> e & 1 ? pw[e] : 0.f;
                 }
             }
 #pragma unroll
