@@ -23,8 +23,8 @@ constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel f
 // that the lanes outside the branch got their values back wrong.  Two tiles where sums and queries leave room for it.
 constexpr int chunk_tiles(int dp, int np) { return dp == 64 || (dp == 128 && np == 1) ? 2 : 1; }
 constexpr float kLog2e = 1.4426950408889634f;
-// A row's weights are p = 2^(x - top), and fp16 gets p * s: `top` follows the largest x + log2(s), so that scales of values of
-// any size fit.  It may lag (products up to 2^15) and is brought up for all lanes of a row together, to leave them 2^8.  Rows
+// A row's weights are p = 2^(x - top), and fp16 gets p * s: `top`, a whole number, follows the largest x + log2(s), so that
+// scales of values of any size fit.  It may lag (products up to 2^15) and is brought up for all lanes of a row together, to leave them 2^8.  Rows
 // of one value (s = 0) count with the least scale, which leaves p within 2^105; their codes are 0.
 constexpr float kLeastScale = 8.077935669463161e-28f;  // 2^-90
 constexpr float kNothing = -1e30f;  // running maximum where nothing was seen: below any score, and finite
@@ -334,14 +334,11 @@ __device__ inline Sight sight_of(const AttendCall &a, const View &v, int pos) {
     s.prefix = pos >= 0 ? v.prefix : 0;
     return s;
 }
-// the same of positions at + 0, 1, 2, 3, 16, 17, 18, 19 as eight bits
+// the same of positions at + 0, 1, 2, 3 as four bits
 __device__ inline uint32_t seen_of(const Sight &s, int at) {
     uint32_t seen = 0;
 #pragma unroll
-    for (int e = 0; e < 8; e++) {
-        const int t = 16 * (e / 4) + e % 4;
-        seen |= (uint32_t)((t <= s.high - at && t > s.low - at) || t < s.prefix - at) << e;
-    }
+    for (int t = 0; t < 4; t++) seen |= (uint32_t)((t <= s.high - at && t > s.low - at) || t < s.prefix - at) << t;
     return seen;
 }
 

@@ -24,8 +24,9 @@ struct ChunkShape {
     static constexpr int KEYS = TOK / 16 * KS, VALUES = TOK / 32 * VT;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); SHAPED: scores are capped or biased
-template <int BITS, int DP, int NP, int NT, bool SHAPED>
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); MODE: 1: scores are biased by
+// distance, 2: capped (and biased)
+template <int BITS, int DP, int NP, int NT, int MODE>
 __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chunk_kernel(AttendCall a, AttendPlan plan) {
     using S = ChunkShape<BITS, DP, NT>;
     constexpr int R = S::R, TOK = S::TOK;
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 const int row = wrow0 + 16 * n + n16;
                 const bool real = row - row0 < nrows;
                 pos[n] = real ? v.len - v.n + row / a.group : -1;
-                slope[n] = SHAPED && a.slopes && real ? a.slopes[head * a.group + row % a.group] * kLog2e : 0.f;
+                slope[n] = MODE && a.slopes && real ? a.slopes[head * a.group + row % a.group] * kLog2e : 0.f;
             }
         }
         const float cap = a.softcap * kLog2e;
@@ -211,119 +212,141 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 
         // 32 positions for the wave's rows; `whole`: all of them see all
         auto half_tile = [&](bool whole, int base, int buf, int hf) {
+            // operands are read ahead of the products that wait for them, as many as there are registers for
+            constexpr int kAhead = S::KS < 8 ? S::KS : 4;
             float4v acc[NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; n++) acc[n][0] = acc[n][1] = float4v{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int j = 0; j < 2; j++)
-#pragma unroll
-                for (int c = 0; c < S::KS; c++) {
-                    const half8 key = __builtin_bit_cast(half8, keys[buf][(2 * hf + j) * S::KS + c][lane]);
-#pragma unroll
-                    for (int p = 0; p < NP; p++)
-#pragma unroll
-                        for (int n = 0; n < NT; n++) acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][n][c], acc[n][j], 0, 0, 0);
-                }
-            float ks[8], km[8], vs[8], vm[8];
-#pragma unroll
             for (int j = 0; j < 2; j++) {
-                float4 p[4];
 #pragma unroll
-                for (int i = 0; i < 4; i++) p[i] = *reinterpret_cast<const float4 *>(&params[buf][i][32 * hf + 16 * j + 4 * g]);
+                for (int n = 0; n < NT; n++) acc[n][j] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const int e = 4 * j + i;
-                    ks[e] = (&p[0].x)[i];
-                    km[e] = (&p[1].x)[i];
-                    vs[e] = (&p[2].x)[i];
-                    vm[e] = (&p[3].x)[i];
+                for (int c0 = 0; c0 < S::KS; c0 += kAhead) {
+                    half8 key[kAhead];
+#pragma unroll
+                    for (int c = 0; c < kAhead; c++) key[c] = __builtin_bit_cast(half8, keys[buf][(2 * hf + j) * S::KS + c0 + c][lane]);
+#pragma unroll
+                    for (int c = 0; c < kAhead; c++)
+#pragma unroll
+                        for (int p = 0; p < NP; p++)
+#pragma unroll
+                            for (int n = 0; n < NT; n++)
+                                acc[n][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key[c], q[p][n][c0 + c], acc[n][j], 0, 0, 0);
                 }
             }
+            constexpr int kValues = S::VT < 8 ? S::VT : DP * NT > 128 ? 4 : 8;
+            half8 val[kValues];
+#pragma unroll
+            for (int t = 0; t < kValues; t++) val[t] = __builtin_bit_cast(half8, values[buf][hf * S::VT + t][lane]);
+            __builtin_amdgcn_sched_barrier(0);
             half8 w[NP][NT];
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                uint32_t seen = 0xffu;
-                if (!whole) seen = seen_of(sight_of(a, v, pos[n]), base + 4 * g);
-                float x[8], p[8], pw[8];
-                if constexpr (SHAPED) {
+            for (int j = 0; j < 2; j++) {
+                float ks[4], km[4], vs[4], vm[4];
+                {
+                    float4 x[4];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) x[e] = fmaf(ks[e], acc[n][e / 4][e % 4], km[e] * qsum[n]);
-                    if (a.softcap > 0.f)
+                    for (int i = 0; i < 4; i++) x[i] = *reinterpret_cast<const float4 *>(&params[buf][i][32 * hf + 16 * j + 4 * g]);
 #pragma unroll
-                        for (int e = 0; e < 8; e++) x[e] = capped(x[e], cap);
-#pragma unroll
-                    for (int e = 0; e < 8; e++) x[e] = fmaf(slope[n], (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos[n]), x[e]);
+                    for (int i = 0; i < 4; i++) ks[i] = (&x[0].x)[i], km[i] = (&x[1].x)[i], vs[i] = (&x[2].x)[i], vm[i] = (&x[3].x)[i];
                 }
-                // scores less `ref`, -infinity where the row does not see the position
-                float y[8];
-                auto score = [&](float ref) {
+                const int at4 = base + 16 * j + 4 * g;
+                uint32_t seen[NT];
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        if constexpr (SHAPED) y[e] = x[e] - ref;
-                        else y[e] = fmaf(ks[e], acc[n][e / 4][e % 4], fmaf(km[e], qsum[n], -ref));
+                for (int n = 0; n < NT; n++) seen[n] = whole ? 15u : seen_of(sight_of(a, v, pos[n]), at4);
+                float p[NT][4], pw[NT][4];
+                // scores less `ref`, -infinity where the row does not see the position
+                auto score = [&](int n, float ref, float(&y)[4]) {
+                    if constexpr (MODE == 0) {
+#pragma unroll
+                        for (int i = 0; i < 4; i++) y[i] = fmaf(ks[i], acc[n][j][i], fmaf(km[i], qsum[n], -ref));
+                    } else if constexpr (MODE == 1) {
+                        const float from = fmaf(slope[n], (float)(at4 - pos[n]), -ref);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) y[i] = fmaf(ks[i], acc[n][j][i], fmaf(km[i], qsum[n], fmaf(slope[n], (float)i, from)));
+                    } else {
+                        const float from = fmaf(slope[n], (float)(at4 - pos[n]), -ref);
+#pragma unroll
+                        for (int i = 0; i < 4; i++)
+                            y[i] = capped(fmaf(ks[i], acc[n][j][i], km[i] * qsum[n]), cap) + fmaf(slope[n], (float)i, from);
                     }
                     if (!whole) {
-                        const uint32_t bits = here(seen);
+                        const uint32_t bits = here(seen[n]);
 #pragma unroll
-                        for (int e = 0; e < 8; e++) y[e] = bits >> e & 1 ? y[e] : -INFINITY;
+                        for (int i = 0; i < 4; i++) y[i] = bits >> i & 1 ? y[i] : -INFINITY;
                     }
                 };
                 auto weigh = [&] {
                     float most = 0.f;
-                    score(top[n]);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        p[e] = __builtin_amdgcn_exp2f(y[e]);
-                        pw[e] = p[e] * vs[e];
-                        most = fmaxf(most, pw[e]);
+                    for (int n = 0; n < NT; n++) {
+                        float y[4];
+                        score(n, top[n], y);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            p[n][i] = __builtin_amdgcn_exp2f(y[i]);
+                            pw[n][i] = p[n][i] * vs[i];
+                            most = fmaxf(most, pw[n][i]);
+                        }
                     }
                     return most;
                 };
                 if (__any(weigh() > 32768.f)) {
-                    float now = kNothing;
-                    score(0.f);
 #pragma unroll
-                    for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(vs[e]));
-                    now = fmaxf(now, __shfl_xor(now, 16));
-                    now = fmaxf(now, __shfl_xor(now, 32));
-                    now = fmaxf(top[n], now - 8.f);
-                    const float keep = __builtin_amdgcn_exp2f(top[n] - now);
-                    top[n] = now;
-                    total[n] *= keep;
-                    mins[n] *= keep;
+                    for (int n = 0; n < NT; n++) {
+                        float y[4], now = kNothing;
+                        score(n, 0.f, y);
 #pragma unroll
-                    for (int t = 0; t < S::VT; t++) o[n][t] *= keep;
+                        for (int i = 0; i < 4; i++) now = fmaxf(now, y[i] + __builtin_amdgcn_logf(vs[i]));
+                        now = fmaxf(now, __shfl_xor(now, 16));
+                        now = fmaxf(now, __shfl_xor(now, 32));
+                        now = fmaxf(top[n], ceilf(now) - 8.f);  // (whole numbers: what is kept is kept exactly)
+                        const float keep = __builtin_amdgcn_exp2f(top[n] - now);
+                        top[n] = now;
+                        total[n] *= keep;
+                        mins[n] *= keep;
+#pragma unroll
+                        for (int t = 0; t < S::VT; t++) o[n][t] *= keep;
+                        if (j)
+#pragma unroll
+                            for (int k = 0; k < NP; k++)
+#pragma unroll
+                                for (int i = 0; i < 4; i++) w[k][n][i] *= (_Float16)keep;
+                    }
                     weigh();
                 }
-                if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) mins[n] = fmaf(p[e], vm[e], mins[n]);
-                } else {  // (an infinity or NaN that the row does not see is not to reach it)
-                    const uint32_t bits = here(seen);
+                for (int n = 0; n < NT; n++) {
+                    if (whole) {
 #pragma unroll
-                    for (int e = 0; e < 8; e++) {
-                        mins[n] = bits >> e & 1 ? fmaf(p[e], vm[e], mins[n]) : mins[n];
-                        pw[e] = bits >> e & 1 ? pw[e] : 0.f;
+                        for (int i = 0; i < 4; i++) mins[n] = fmaf(p[n][i], vm[i], mins[n]);
+                    } else {  // (an infinity or NaN that the row does not see is not to reach it)
+                        const uint32_t bits = here(seen[n]);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) {
+                            mins[n] = bits >> i & 1 ? fmaf(p[n][i], vm[i], mins[n]) : mins[n];
+                            pw[n][i] = bits >> i & 1 ? pw[n][i] : 0.f;
+                        }
                     }
-                }
 #pragma unroll
-                for (int e = 0; e < 8; e++) {
-                    total[n] += p[e];
-                    w[0][n][e] = (_Float16)pw[e];
-                    if constexpr (NP == 2) w[NP - 1][n][e] = (_Float16)(pw[e] - (float)w[0][n][e]);
-                }
-                if constexpr (NP == 1)
+                    for (int i = 0; i < 4; i++) {
+                        total[n] += p[n][i];
+                        w[0][n][4 * j + i] = (_Float16)pw[n][i];
+                        if constexpr (NP == 2) w[NP - 1][n][4 * j + i] = (_Float16)(pw[n][i] - (float)w[0][n][4 * j + i]);
+                    }
+                    if constexpr (NP == 1)
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2)
-                        mins[n] = __builtin_amdgcn_fdot2(half2v{w[0][n][e], w[0][n][e + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins[n], false);
+                        for (int i = 4 * j; i < 4 * j + 4; i += 2)
+                            mins[n] = __builtin_amdgcn_fdot2(half2v{w[0][n][i], w[0][n][i + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins[n], false);
+                }
             }
 #pragma unroll
             for (int t = 0; t < S::VT; t++) {
-                const half8 val = __builtin_bit_cast(half8, values[buf][hf * S::VT + t][lane]);
+                if (t >= kValues) val[t % kValues] = __builtin_bit_cast(half8, values[buf][hf * S::VT + t][lane]);
 #pragma unroll
                 for (int p = 0; p < NP; p++)
 #pragma unroll
-                    for (int n = 0; n < NT; n++) o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[p][n], o[n][t], 0, 0, 0);
+                    for (int n = 0; n < NT; n++)
+                        o[n][t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val[t % kValues], w[p][n], o[n][t], 0, 0, 0);
             }
         };
 

@@ -3,10 +3,13 @@
 namespace bf {
 template <int BITS, int DP>
 static void go(const AttendCall &a, const AttendPlan &p) {
-    const bool shaped = a.softcap > 0.f || a.slopes;
-    auto kernel = a.dtype == BIFEAT_F32 ? shaped ? attend_rows_kernel<BITS, DP, 2, true> : attend_rows_kernel<BITS, DP, 2, false>
-                  : shaped              ? attend_rows_kernel<BITS, DP, 1, true>
-                                        : attend_rows_kernel<BITS, DP, 1, false>;
+    const int mode = a.softcap > 0.f ? 2 : a.slopes ? 1 : 0;
+    auto kernel = a.dtype == BIFEAT_F32 ? mode == 0   ? attend_rows_kernel<BITS, DP, 2, 0>
+                                          : mode == 1 ? attend_rows_kernel<BITS, DP, 2, 1>
+                                                      : attend_rows_kernel<BITS, DP, 2, 2>
+                  : mode == 0           ? attend_rows_kernel<BITS, DP, 1, 0>
+                  : mode == 1           ? attend_rows_kernel<BITS, DP, 1, 1>
+                                        : attend_rows_kernel<BITS, DP, 1, 2>;
     kernel<<<p.nw, 256, 0, a.s>>>(a, p);
 }
 void launch_attend_rows(const AttendCall &a, const AttendPlan &p, int bits, int dp) {

@@ -24,8 +24,9 @@ struct RowLanes {
     static constexpr int VW = VB < 4 ? 1 : VB / 4;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); SHAPED: scores are capped or biased
-template <int BITS, int DP, int NP, bool SHAPED>
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); MODE: 1: scores are biased by
+// distance, 2: capped (and biased)
+template <int BITS, int DP, int NP, int MODE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
     using L = RowLanes<BITS, DP>;
     constexpr int R = kRowsR, TOK = kRowsTok;
@@ -97,7 +98,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             qsum += __shfl_xor(qsum, 32);
             qsum *= f / kUnit<NP>;
         }
-        const float slope = SHAPED && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+        const float slope = MODE && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
         const float cap = a.softcap * kLog2e;
 
         float top = kNothing, total = 0.f, mins = 0.f;  // mins: what is not in the products with the codes
@@ -163,7 +164,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 }
             }
             uint32_t seen = 0xffu;
-            if (!whole) seen = seen_of(sight_of(a, v, pos), base + 4 * g);
+            if (!whole) {
+                const Sight sight = sight_of(a, v, pos);
+                seen = seen_of(sight, base + 4 * g) | seen_of(sight, base + 16 + 4 * g) << 4;
+            }
             // ---- scores
             float4v acc[2];
 #pragma unroll
@@ -185,23 +189,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 }
             }
             if (more) load_keys(next);
-            float x[8], p[8], pw[8];
-            if constexpr (SHAPED) {
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum);
-                if (a.softcap > 0.f)
-#pragma unroll
-                    for (int e = 0; e < 8; e++) x[e] = capped(x[e], cap);
-#pragma unroll
-                for (int e = 0; e < 8; e++) x[e] = fmaf(slope, (float)(base + 16 * (e / 4) + 4 * g + e % 4 - pos), x[e]);
-            }
+            float p[8], pw[8], y[8];
             // scores less `ref`, -infinity where the row does not see the position
-            float y[8];
             auto score = [&](float ref) {
+                const float from = MODE ? fmaf(slope, (float)(base + 4 * g - pos), -ref) : -ref;
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
-                    if constexpr (SHAPED) y[e] = x[e] - ref;
-                    else y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, -ref));
+                    const float bias = MODE ? fmaf(slope, (float)(16 * (e / 4) + e % 4), from) : from;
+                    if constexpr (MODE < 2) y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, bias));
+                    else y[e] = capped(fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum), cap) + bias;
                 }
                 if (!whole) {
                     const uint32_t bits = here(seen);
@@ -227,7 +223,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(vs[e]));
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(now, __shfl_xor(now, 32));
-                now = fmaxf(top, now - 8.f);
+                now = fmaxf(top, ceilf(now) - 8.f);  // (whole numbers: what is kept is kept exactly)
                 const float keep = __builtin_amdgcn_exp2f(top - now);
                 top = now;
                 total *= keep;
