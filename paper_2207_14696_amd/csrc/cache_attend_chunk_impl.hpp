@@ -69,8 +69,10 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
         int pages = 0, paged = -64;
         const int32_t *table = a.b.tables + (int64_t)at.seq * a.b.width;
         constexpr int kSub = TOK / 16;
+        // the nearest positions first: with a bias by distance theirs are the largest scores, and sums begun there need not be
+        // scaled down tile by tile
         auto base_of = [&](int u) {
-            u += at.unit;
+            u = at.unit + units - 1 - u;
             return (u < v.skip_at ? u : u + v.skip) * TOK;
         };
         uint32_t kw[S::KB / 4], vw[8][S::VW];
@@ -78,7 +80,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
         auto load = [&](int u) {
             if (u - paged >= 64 / kSub) {
                 paged = u;
-                int j = base_of(u + lane / kSub) + 16 * (lane % kSub);
+                int j = u + lane / kSub < units ? base_of(u + lane / kSub) + 16 * (lane % kSub) : 0;
                 j = j < v.len ? j : v.len - 1;
                 pages = table[j >> a.c.ps_log2];
             }

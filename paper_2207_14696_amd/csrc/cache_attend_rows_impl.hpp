@@ -110,7 +110,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         int pages = 0, paged = -64;
         const int32_t *table = a.b.tables + (int64_t)at.seq * a.b.width;
         auto base_of = [&](int u) {  // first position of the wave's step in unit u of the item
-            u += at.unit;
+            u = at.unit + units - 1 - u;  // the nearest first
             return (u < v.skip_at ? u : u + v.skip) * TOK + 32 * wave;
         };
         uint32_t kw[2][L::KB / 4], vw[8][L::VW];
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         auto load_keys = [&](int u) {
             if (u - paged >= 32) {
                 paged = u;
-                int j = base_of(u + (lane >> 1)) + 16 * (lane & 1);
+                int j = u + (lane >> 1) < units ? base_of(u + (lane >> 1)) + 16 * (lane & 1) : 0;
                 j = j < v.len ? j : v.len - 1;
                 pages = table[j >> a.c.ps_log2];
             }
@@ -281,11 +281,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             for (int u = 0; u < units; u++) {
                 const int base = base_of(u);
                 const bool more = u + 1 < units;
-                if (base < v.len) {  // (of an item's last unit some waves may have no positions)
+                if (base < v.len) {  // (of the context's last positions some waves may have none)
                     // do all rows see all 32 positions?
                     const bool whole = base + 32 <= v.len && v.first >= 0 &&
                                        ((base + 31 <= v.first && (!a.window || base > v.last - a.window)) || base + 32 <= v.prefix);
                     step(whole, base, more, u + 1);
+                } else if (more) {
+                    load_keys(u + 1);
                 }
                 if (more) load_values();
             }
