@@ -88,8 +88,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPl
 #pragma unroll
             for (int c = 0; c < DP / 64; c++) {
                 const int col = 64 * c + 4 * sub;
-                const float x[4] = {acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv};
-                store_columns<4>(a, dst + col, a.c.d - col, x);
+                store_four(a, dst + col, a.c.d - col, make_float4(acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv));
             }
         }
     }

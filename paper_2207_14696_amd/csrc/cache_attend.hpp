@@ -275,20 +275,79 @@ __device__ inline void load_bytes(__amdgpu_buffer_rsrc_t r, uint32_t each, uint3
         w[0] = __builtin_amdgcn_raw_buffer_load_b8(r, each, all, BF_NT);
     }
 }
-// one query's elements as floats, zeros from column a.c.d on
-template <int N>
-__device__ inline void load_query(const AttendCall &a, int64_t token, int head, int col, float *x) {
-    const int64_t at = token * a.q.token_stride + head * a.q.head_stride + col;
+// x, which nothing that is made of it is to leave this place: mask bits tested ahead of a branch that seldom needs them cost 16 of
+// 50 instructions, and addresses worked out once for all items the registers that sums need.
+__device__ inline uint32_t here(uint32_t x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+// Queries to LDS, as they are: rows row0 .. row0 + N - 1 of a sequence and cached head, zeros from column a.c.d and row `rows`
+// on; by `threads` threads of which this is number `me`, in pieces of P columns (which divides a.c.d).  row0 < rows.  E: uint16_t or
+// float.
+template <int N, int DP, int STRIDE, int P, typename E>
+__device__ inline void stage_pieces(const AttendCall &a, int64_t token0, int head, int row0, int rows, E *to, int me, int threads) {
+    const E *q = static_cast<const E *>(a.q.data) + token0 * a.q.token_stride + (int64_t)head * a.group * a.q.head_stride;
+    struct __attribute__((packed, aligned(sizeof(E)))) Piece { E v[P]; };
+    struct __attribute__((aligned(P * sizeof(E)))) Slot { E v[P]; };
+    constexpr int kPer = DP / P, kBatch = 8;  // pieces a row, and in flight
+#pragma unroll 1
+    for (int i0 = me; i0 < N * kPer; i0 += kBatch * threads) {
+        Slot x[kBatch];
 #pragma unroll
-    for (int k = 0; k < N; k += 8) {
-        float e[8];
-        const int left = a.c.d - col - k;
-        if (a.dtype == BIFEAT_F32) load8_any(static_cast<const float *>(a.q.data) + at + k, left, e);
-        else if (a.dtype == BIFEAT_F16) load8_any(static_cast<const Half16 *>(a.q.data) + at + k, left, e);
-        else load8_any(static_cast<const Brain16 *>(a.q.data) + at + k, left, e);
+        for (int k = 0; k < kBatch; k++) {
+            const int i = i0 + k * threads, r = row0 + i / kPer, col = i % kPer * P;
+            const bool there = i < N * kPer && r < rows && col < a.c.d;
+            const int rr = there ? r : row0;
+            const Piece y = *reinterpret_cast<const Piece *>(q + rr / a.group * a.q.token_stride + rr % a.group * a.q.head_stride + (there ? col : 0));
 #pragma unroll
-        for (int i = 0; i < 8; i++) x[k + i] = e[i];
+            for (int e = 0; e < P; e++) x[k].v[e] = there ? y.v[e] : (E)0;
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; k++) {
+            const int i = i0 + k * threads;
+            if (i < N * kPer) *reinterpret_cast<Slot *>(to + i / kPer * STRIDE + i % kPer * P) = x[k];
+        }
     }
+}
+template <int N, int DP, int STRIDE, typename E>
+__device__ inline void stage_queries(const AttendCall &a, int64_t token0, int head, int row0, int rows, E *to, int me, int threads) {
+    me = (int)here((uint32_t)me);
+    if (a.c.d % 4 == 0) stage_pieces<N, DP, STRIDE, 4>(a, token0, head, row0, rows, to, me, threads);
+    else stage_pieces<N, DP, STRIDE, 1>(a, token0, head, row0, rows, to, me, threads);
+}
+// 8 of them, and as floats
+template <typename E>
+struct __attribute__((aligned(8 * sizeof(E)))) Queries8 { E v[8]; };
+template <typename E>
+__device__ inline void floats_of(const Queries8<E> &q, bool half, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) {
+        if constexpr (sizeof(E) == 4) x[i] = q.v[i];
+        else x[i] = half ? to_float(Half16{q.v[i]}) : to_float(Brain16{q.v[i]});
+    }
+}
+__device__ inline float largest_finite(float most, const float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
+    return most;
+}
+// 8 columns as an operand beside 8 codes: of 4-bit codes, which come as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16, the odd ones' are
+// a 16th.  Returns what they add up to.
+template <int BITS, int NP>
+__device__ inline float query_operand(const float (&x)[8], float up, half8 &hi8, half8 &lo8) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+        const float y = x[e] * up;
+        const _Float16 hi = (_Float16)y, lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
+        sum += (float)hi + (float)lo;
+        const int slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
+        const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
+        hi8[slot] = hi * down;
+        if constexpr (NP == 2) lo8[slot] = lo * down;
+    }
+    return sum;
 }
 
 __device__ inline void store_result(const AttendCall &a, int64_t at, float x) {
@@ -297,30 +356,40 @@ __device__ inline void store_result(const AttendCall &a, int64_t at, float x) {
     else static_cast<Brain16 *>(a.out)[at] = from_float<Brain16>(x);
 }
 
-// N columns of a result row, of which `left` are there
-template <int N>
-__device__ inline void store_columns(const AttendCall &a, int64_t at, int left, const float (&x)[N]) {
-    if constexpr (N >= 8) {
+// four columns of a result row, of which `left` are there
+__device__ inline void store_four(const AttendCall &a, int64_t at, int left, const float4 &x) {
+    if (a.c.d % 4 == 0 && left >= 4) {
+        if (a.dtype == BIFEAT_F32) {
+            struct __attribute__((packed, aligned(4))) Four { float4 v; };
+            *reinterpret_cast<Four *>(static_cast<float *>(a.out) + at) = Four{x};
+        } else {
+            struct __attribute__((packed, aligned(2))) Four { uint16_t v[4]; };
+            const float e[4] = {x.x, x.y, x.z, x.w};
+            Four y;
 #pragma unroll
-        for (int k = 0; k < N; k += 8) {
-            float e[8];
-#pragma unroll
-            for (int i = 0; i < 8; i++) e[i] = x[k + i];
-            if (a.dtype == BIFEAT_F32) store8_any(static_cast<float *>(a.out) + at + k, left - k, e);
-            else if (a.dtype == BIFEAT_F16) store8_any(static_cast<Half16 *>(a.out) + at + k, left - k, e);
-            else store8_any(static_cast<Brain16 *>(a.out) + at + k, left - k, e);
+            for (int i = 0; i < 4; i++) y.v[i] = a.dtype == BIFEAT_F16 ? from_float<Half16>(e[i]).bits : from_float<Brain16>(e[i]).bits;
+            *reinterpret_cast<Four *>(static_cast<uint16_t *>(a.out) + at) = y;
         }
     } else {
-#pragma unroll
-        for (int k = 0; k < N; k++)
-            if (k < left) store_result(a, at + k, x[k]);
+        if (left > 0) store_result(a, at, x.x);
+        if (left > 1) store_result(a, at + 1, x.y);
+        if (left > 2) store_result(a, at + 2, x.z);
+        if (left > 3) store_result(a, at + 3, x.w);
     }
 }
 
-// x, which nothing that is made of it is to leave this place (its bits tested where they are not wanted cost 16 of 50 instructions)
-__device__ inline uint32_t here(uint32_t x) {
-    asm volatile("" : "+v"(x));
-    return x;
+// 16 rows of results in LDS, those below `rows`, to where they belong.  A wave.
+template <int DP, int STRIDE>
+__device__ inline void put_rows(const AttendCall &a, int64_t token0, int head, int row0, int rows, const float *x, int lane) {
+    const int64_t heads = (int64_t)a.c.heads * a.group;
+    lane = (int)here((uint32_t)lane);
+#pragma unroll 1
+    for (int i = lane; i < 16 * DP / 4; i += 64) {
+        const int r = i / (DP / 4), row = row0 + r, col = i % (DP / 4) * 4;
+        if (row >= rows || col >= a.c.d) continue;
+        const float4 y = *reinterpret_cast<const float4 *>(x + r * STRIDE + col);
+        store_four(a, ((token0 + row / a.group) * heads + head * a.group + row % a.group) * a.c.d + col, a.c.d - col, y);
+    }
 }
 
 // What a query row sees, as bounds for a position: t <= high and t > low, or t < prefix.

@@ -147,59 +147,58 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
 
         // ---- the queries of the wave's rows
         const int wrow0 = row0 + 16 * NT * wave;  // of the sequence
+        const bool any_row = wrow0 < row0 + nrows;
         half8 q[NP][NT][S::KS];
         float qsum[NT], slope[NT];
         int pos[NT];
-        auto query = [&](int n, float(&x)[DP / 4]) {
-            const int row = wrow0 + 16 * n + n16;
-#pragma unroll
-            for (int i = 0; i < DP / 4; i++) x[i] = 0.f;
-            if (row - row0 < nrows) load_query<DP / 4>(a, token0 + row / a.group, head * a.group + row % a.group, g * (DP / 4), x);
-        };
         {
+            // by way of LDS, where no tile is now
+            using E = std::conditional_t<NP == 2, float, uint16_t>;
+            constexpr int kStride = DP + (NP == 2 && DP != 128 ? 0 : 8);
+            E *rows = reinterpret_cast<E *>(lds) + 16 * NT * wave * kStride;
+            static_assert(R * kStride * sizeof(E) <= 2 * (S::KEYS + S::VALUES) * 1024, "queries fit the tiles");
+            const int at_lane = (int)here((uint32_t)lane);
+            const E *own = rows + (at_lane & 15) * kStride + (at_lane >> 4) * (DP / 4);
+            if (any_row) stage_queries<16 * NT, DP, kStride>(a, token0, head, wrow0, row0 + nrows, rows, lane, 64);
+            wave_sync();
+            const bool half = a.dtype == BIFEAT_F16;
             float big = 0.f;
 #pragma unroll
-            for (int n = 0; n < NT; n++) {
-                float x[DP / 4];
-                query(n, x);
+            for (int n = 0; n < NT; n++)
 #pragma unroll
-                for (int i = 0; i < DP / 4; i++) big = fmaxf(big, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
-            }
+                for (int c = 0; c < S::KS; c++) {
+                    float x[8];
+                    floats_of(*reinterpret_cast<const Queries8<E> *>(own + 16 * n * kStride + 8 * c), half, x);
+                    big = largest_finite(big, x);
+                }
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
-            __syncthreads();
-            if (lane == 0) tops[wave] = big;
+            if (lane == 0) tops[wave] = any_row ? big : 0.f;
             __syncthreads();
             const float up = power_to(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), 14);
             f = a.scale * kLog2e * (kUnit<NP> / up);
 #pragma unroll
             for (int n = 0; n < NT; n++) {
-                float x[DP / 4], sum = 0.f;
-                query(n, x);
+                float sum = 0.f;
 #pragma unroll
-                for (int i = 0; i < DP / 4; i++) {
-                    const float y = x[i] * up;
-                    const _Float16 hi = (_Float16)y;
-                    const _Float16 lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
-                    sum += (float)hi + (float)lo;
-                    const int e = i % 8, slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
-                    const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
-                    q[0][n][i / 8][slot] = hi * down;
-                    if constexpr (NP == 2) q[NP - 1][n][i / 8][slot] = lo * down;
+                for (int c = 0; c < S::KS; c++) {
+                    float x[8];
+                    floats_of(*reinterpret_cast<const Queries8<E> *>(own + 16 * n * kStride + 8 * c), half, x);
+                    sum += query_operand<BITS, NP>(x, up, q[0][n][c], q[NP - 1][n][c]);
                 }
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
                 qsum[n] = sum * (f / kUnit<NP>);
-                const int row = wrow0 + 16 * n + n16;
+                const int row = wrow0 + 16 * n + (at_lane & 15);
                 const bool real = row - row0 < nrows;
                 pos[n] = real ? v.len - v.n + row / a.group : -1;
                 slope[n] = MODE && a.slopes && real ? a.slopes[head * a.group + row % a.group] * kLog2e : 0.f;
             }
+            __syncthreads();
         }
         const float cap = a.softcap * kLog2e;
         // first and last position of the wave's queries
         const int wend = wrow0 + 16 * NT < row0 + nrows ? wrow0 + 16 * NT : row0 + nrows;
-        const bool any_row = wrow0 < row0 + nrows;
         const int wfirst = v.len - v.n + wrow0 / a.group, wlast = v.len - v.n + (wend - 1) / a.group;
 
         float top[NT], total[NT], mins[NT];  // mins: what is not in the products with the codes
@@ -376,7 +375,10 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
         }
 
         const bool complete = at.unit == 0 && units == v.units;
-        if (any_row)
+        constexpr int kOut = DP + 4;
+        static_assert(4 * 16 * kOut * sizeof(float) <= 2 * (S::KEYS + S::VALUES) * 1024 + 8 * TOK * sizeof(float), "a tile of rows a wave fits");
+        if (any_row) {
+            const int at_lane = (int)here((uint32_t)lane), row16 = at_lane & 15, quarter = at_lane >> 4;
 #pragma unroll
             for (int n = 0; n < NT; n++) {
                 float s = total[n], rest = mins[n];
@@ -384,28 +386,30 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 s += __shfl_xor(s, 32);
                 rest += __shfl_xor(rest, 16);
                 rest += __shfl_xor(rest, 32);
-                const int r = 16 * (NT * wave + n) + n16, row = row0 + r;
-                if (r >= nrows) continue;
-                const float inv = s != 0.f ? 1.f / s : 0.f;
-                const int64_t dst = ((token0 + row / a.group) * ((int64_t)a.c.heads * a.group) + head * a.group + row % a.group) * a.c.d;
-                float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2));
-                if (!complete && g == 0) part[R * DP + r] = top[n], part[R * DP + R + r] = s;
+                // by way of LDS, where the tiles are done with, to rows of consecutive columns
+                const float inv = complete ? (s != 0.f ? 1.f / s : 0.f) : 1.f;
+                float *x = reinterpret_cast<float *>(lds) + wave * 16 * kOut;
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const int col = (4 * g + i) * S::VT;
-                    float x[S::VT];
+                for (int i = 0; i < 4; i++)
 #pragma unroll
-                    for (int t = 0; t < S::VT; t++) x[t] = fmaf(o[n][t][i], kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f), rest);
-                    if (complete) {
-#pragma unroll
-                        for (int t = 0; t < S::VT; t++) x[t] *= inv;
-                        store_columns<S::VT>(a, dst + col, a.c.d - col, x);
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < S::VT; t++) part[r * DP + col + t] = x[t];
-                    }
+                    for (int t = 0; t < S::VT; t++)
+                        x[row16 * kOut + (4 * quarter + i) * S::VT + t] =
+                            fmaf(o[n][t][i], kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f), rest) * inv;
+                wave_sync();
+                const int r0 = 16 * (NT * wave + n);
+                if (complete) {
+                    put_rows<DP, kOut>(a, token0, head, row0 + r0, row0 + nrows, x, lane);
+                } else {
+                    float *part = plan.partial + ((int64_t)blockIdx.x * 2 + (at.unit == 0)) * (R * (DP + 2));
+                    if (quarter == 0) part[R * DP + r0 + row16] = top[n], part[R * DP + R + r0 + row16] = s;
+#pragma unroll 1
+                    for (int i = at_lane; i < 16 * DP / 4; i += 64)
+                        *reinterpret_cast<float4 *>(part + r0 * DP + 4 * i) = *reinterpret_cast<const float4 *>(x + i / (DP / 4) * kOut + i % (DP / 4) * 4);
                 }
+                wave_sync();
             }
+        }
+        __syncthreads();
         cur += units;
         if (cur < end) next_item<R>(a, &head, &at);
     }

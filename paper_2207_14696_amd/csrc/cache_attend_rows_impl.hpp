@@ -61,51 +61,6 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         const int row0 = at.rt * R, nrows = v.n * a.group - row0 < R ? v.n * a.group - row0 : R;
         const int64_t token0 = uniform(a.b.first(at.seq));
 
-        // ---- the queries: lane (n16, g) has a quarter of the columns of row n16, those of the keys that it reads
-        const int row = row0 + n16;
-        const bool real = n16 < nrows;
-        const int qi = row / a.group, qh = head * a.group + row % a.group;
-        const int pos = real ? v.len - v.n + qi : -1;
-        half8 q[NP][L::KS];
-        float qsum = 0.f, f;
-        {
-            float x[DP / 4];
-#pragma unroll
-            for (int i = 0; i < DP / 4; i++) x[i] = 0.f;
-            if (real)
-#pragma unroll
-                for (int i = 0; i < DP / 4; i += L::KC) load_query<L::KC>(a, token0 + qi, qh, 4 * i + g * L::KC, x + i);
-            float top = 0.f;
-#pragma unroll
-            for (int i = 0; i < DP / 4; i++) top = fmaxf(top, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
-#pragma unroll
-            for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-            const float up = power_to(top, 14);
-            f = a.scale * kLog2e * (kUnit<NP> / up);
-#pragma unroll
-            for (int i = 0; i < DP / 4; i++) {
-                const float y = x[i] * up;
-                const _Float16 hi = (_Float16)y;
-                const _Float16 lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
-                qsum += (float)hi + (float)lo;
-                // 4-bit codes come as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16 of eight
-                const int e = i % 8, slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
-                const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
-                q[0][i / 8][slot] = hi * down;
-                if constexpr (NP == 2) q[NP - 1][i / 8][slot] = lo * down;
-            }
-            qsum += __shfl_xor(qsum, 16);
-            qsum += __shfl_xor(qsum, 32);
-            qsum *= f / kUnit<NP>;
-        }
-        const float slope = MODE && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
-        const float cap = a.softcap * kLog2e;
-
-        float top = kNothing, total = 0.f, mins = 0.f;  // mins: what is not in the products with the codes
-        float4v o[L::VT];
-#pragma unroll
-        for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
-
         // ---- pages: lane 2 i + j has the page of the wave's i-th step from `paged` on, half j
         int pages = 0, paged = -64;
         const int32_t *table = a.b.tables + (int64_t)at.seq * a.b.width;
@@ -143,6 +98,76 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
 #pragma unroll
             for (int i = 0; i < 4; i++) load_bytes<L::VB>(block1, voff, at1 + i * rb, vw[4 + i]);
         };
+
+        if (v.len > 0) {
+            load_keys(0);
+            load_values();
+        }
+
+        // ---- the queries: lane (n16, g) has a quarter of the columns of row n16, those of the keys that it reads
+        const int row = row0 + n16;
+        const bool real = n16 < nrows;
+        const int qi = row / a.group, qh = head * a.group + row % a.group;
+        const int pos = real ? v.len - v.n + qi : -1;
+        half8 q[NP][L::KS];
+        float qsum = 0.f, f;
+        {
+            using E = std::conditional_t<NP == 2, float, uint16_t>;
+            constexpr int kStride = DP + 8;
+            Queries8<E> raw[L::KS];  // the columns of the c-th 8 codes of this lane's keys
+            const int at_lane = (int)here((uint32_t)lane);
+            auto column = [&](int c) { return (4 * (8 * c / L::KC) + (at_lane >> 4)) * L::KC + 8 * c % L::KC; };
+            if (a.c.d % 4 == 0) {
+                const int r = real ? row : row0;
+                const E *q = static_cast<const E *>(a.q.data) + (token0 + r / a.group) * a.q.token_stride +
+                             ((int64_t)head * a.group + r % a.group) * a.q.head_stride;
+                struct __attribute__((packed, aligned(sizeof(E)))) Four { E v[4]; };
+#pragma unroll
+                for (int c = 0; c < L::KS; c++)
+#pragma unroll
+                    for (int h = 0; h < 8; h += 4) {
+                        const bool there = real && column(c) + h < a.c.d;
+                        const Four y = *reinterpret_cast<const Four *>(q + (there ? column(c) + h : 0));
+#pragma unroll
+                        for (int e = 0; e < 4; e++) raw[c].v[h + e] = there ? y.v[e] : (E)0;
+                    }
+            } else {  // by way of LDS, where nothing is summed now
+                E *rows = reinterpret_cast<E *>(&sums[0][0][0]);
+                stage_queries<R, DP, kStride>(a, token0, head, row0, row0 + nrows, rows, threadIdx.x, 256);
+                __syncthreads();
+#pragma unroll
+                for (int c = 0; c < L::KS; c++) raw[c] = *reinterpret_cast<const Queries8<E> *>(rows + (at_lane & 15) * kStride + column(c));
+                __syncthreads();
+            }
+            const bool half = a.dtype == BIFEAT_F16;
+            float big = 0.f;
+#pragma unroll
+            for (int c = 0; c < L::KS; c++) {
+                float x[8];
+                floats_of(raw[c], half, x);
+                big = largest_finite(big, x);
+            }
+#pragma unroll
+            for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
+            const float up = power_to(big, 14);
+            f = a.scale * kLog2e * (kUnit<NP> / up);
+#pragma unroll
+            for (int c = 0; c < L::KS; c++) {
+                float x[8];
+                floats_of(raw[c], half, x);
+                qsum += query_operand<BITS, NP>(x, up, q[0][c], q[NP - 1][c]);
+            }
+            qsum += __shfl_xor(qsum, 16);
+            qsum += __shfl_xor(qsum, 32);
+            qsum *= f / kUnit<NP>;
+        }
+        const float slope = MODE && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
+        const float cap = a.softcap * kLog2e;
+
+        float top = kNothing, total = 0.f, mins = 0.f;  // mins: what is not in the products with the codes
+        float4v o[L::VT];
+#pragma unroll
+        for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
         auto step = [&](bool whole, int base, bool more, int next) {
             wave_sync();
@@ -275,9 +300,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             }
         };
 
-        if (v.len > 0) {
-            load_keys(0);
-            load_values();
+        if (v.len > 0)
             for (int u = 0; u < units; u++) {
                 const int base = base_of(u);
                 const bool more = u + 1 < units;
@@ -291,9 +314,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 }
                 if (more) load_values();
             }
-        }
 
         // ---- the four waves' parts joined
+        const int at_lane = (int)here((uint32_t)lane), row16 = at_lane & 15, quarter = at_lane >> 4;
         total += __shfl_xor(total, 16);
         total += __shfl_xor(total, 32);
         mins += __shfl_xor(mins, 16);
@@ -302,15 +325,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         for (int t = 0; t < L::VT; t++) {
             const float back = kUnit<NP> * (BITS == 4 && (t & 1) ? 0.0625f : 1.f);
 #pragma unroll
-            for (int i = 0; i < 4; i++) sums[wave][n16][(4 * g + i) * L::VT + t] = fmaf(o[t][i], back, mins);
+            for (int i = 0; i < 4; i++) sums[wave][row16][(4 * quarter + i) * L::VT + t] = fmaf(o[t][i], back, mins);
         }
-        if (g == 0) {
-            tops[wave][n16] = top;
-            totals[wave][n16] = total;
+        if (quarter == 0) {
+            tops[wave][row16] = top;
+            totals[wave][row16] = total;
         }
         __syncthreads();
         {
-            const int r = threadIdx.x >> 4, c0 = threadIdx.x & 15;
+            const int me = (int)here(threadIdx.x), r = me >> 4, c0 = me & 15;
             const float t0 = tops[0][r], t1 = tops[1][r], t2 = tops[2][r], t3 = tops[3][r];
             const float now = fmaxf(fmaxf(t0, t1), fmaxf(t2, t3));
             const float e0 = __builtin_amdgcn_exp2f(t0 - now), e1 = __builtin_amdgcn_exp2f(t1 - now);
