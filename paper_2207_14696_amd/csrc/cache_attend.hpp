@@ -12,9 +12,6 @@
 
 #include "cache.hpp"
 
-#ifndef BF_NT
-#define BF_NT 0
-#endif
 namespace bf {
 
 constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel for few rows
@@ -255,24 +252,26 @@ template <int NP> constexpr float kUnit = NP == 2 ? 1.f : 16777216.f;
 
 // Loads from a head's block of a page, whose address all lanes share: a descriptor in scalar registers, a 32-bit offset a lane
 // and one for all, where 64-bit addresses would take two vector registers and three vector instructions a load.  (The
-// hardware gives zeros past the block's end.)
-__device__ inline __amdgpu_buffer_rsrc_t block_buffer(const CachePages &c, int page, int head) {
-    return __builtin_amdgcn_make_buffer_rsrc(c.block(page, head), 0, (int)c.head_bytes, 0x00027000);
+// hardware gives zeros past the block's end, without a fetch: past any, if the block is not wanted.)
+__device__ inline __amdgpu_buffer_rsrc_t block_buffer(const CachePages &c, int page, int head, bool wanted = true) {
+    return __builtin_amdgcn_make_buffer_rsrc(c.block(page, head), 0, wanted ? (int)c.head_bytes : 0, 0x00027000);
 }
-template <int N>
+// STREAMED: not kept in the caches
+template <int N, bool STREAMED>
 __device__ inline void load_bytes(__amdgpu_buffer_rsrc_t r, uint32_t each, uint32_t all, uint32_t *w) {
+    constexpr int kPolicy = STREAMED ? 2 : 0;
     if constexpr (N == 16) {
-        const auto q = __builtin_amdgcn_raw_buffer_load_b128(r, each, all, BF_NT);
+        const auto q = __builtin_amdgcn_raw_buffer_load_b128(r, each, all, kPolicy);
         w[0] = q[0], w[1] = q[1], w[2] = q[2], w[3] = q[3];
     } else if constexpr (N == 8) {
-        const auto q = __builtin_amdgcn_raw_buffer_load_b64(r, each, all, BF_NT);
+        const auto q = __builtin_amdgcn_raw_buffer_load_b64(r, each, all, kPolicy);
         w[0] = q[0], w[1] = q[1];
     } else if constexpr (N == 4) {
-        w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, each, all, BF_NT);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(r, each, all, kPolicy);
     } else if constexpr (N == 2) {
-        w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, each, all, BF_NT);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b16(r, each, all, kPolicy);
     } else {
-        w[0] = __builtin_amdgcn_raw_buffer_load_b8(r, each, all, BF_NT);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b8(r, each, all, kPolicy);
     }
 }
 // x, which nothing that is made of it is to leave this place: mask bits tested ahead of a branch that seldom needs them cost 16 of

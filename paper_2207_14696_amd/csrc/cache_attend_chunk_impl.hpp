@@ -91,14 +91,14 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 const auto b = buffer(kgroup);
                 const uint32_t all = slot(kgroup) * rb;
 #pragma unroll
-                for (int i = 0; i < S::KB / S::KL; i++) load_bytes<S::KL>(b, koff[i], all, &kw[i * S::KL / 4]);
+                for (int i = 0; i < S::KB / S::KL; i++) load_bytes<S::KL, false>(b, koff[i], all, &kw[i * S::KL / 4]);
             }
 #pragma unroll
             for (int j = 0; j < 2; j++) {
                 const auto b = buffer(2 * vgroup + j);
                 const uint32_t all = (uint32_t)a.c.codes(1) + slot(2 * vgroup + j) * rb;
 #pragma unroll
-                for (int i = 0; i < 4; i++) load_bytes<S::VB>(b, voff, all + i * rb, vw[4 * j + i]);
+                for (int i = 0; i < 4; i++) load_bytes<S::VB, false>(b, voff, all + i * rb, vw[4 * j + i]);
             }
             const int page = __shfl(pages, at16 + fat / 16);
             const uint8_t *fp = a.c.block(page, head) + a.c.floats(wave / 2) + 4 * ((base + fat) & (a.c.ps() - 1));

@@ -72,31 +72,35 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         float4 fw;
         __amdgpu_buffer_rsrc_t block0, block1;  // of the step's two halves
         int slot0, slot1;
+        // Asked for without a branch, of no block where the item has no such unit: across a branch the compiler could not tell how
+        // many loads are on their way, and would wait for all of them where it needs the oldest (contexts of 131 072 tokens in 4
+        // bits 121 us, 117 so).  Past the caches: 64 answers 133 us, 120 so.
         auto load_keys = [&](int u) {
-            if (u - paged >= 32) {
+            const bool wanted = u < units;
+            if (wanted && u - paged >= 32) {
                 paged = u;
                 int j = u + (lane >> 1) < units ? base_of(u + (lane >> 1)) + 16 * (lane & 1) : 0;
                 j = j < v.len ? j : v.len - 1;
                 pages = table[j >> a.c.ps_log2];
             }
-            const int page0 = __builtin_amdgcn_readlane(pages, 2 * (u - paged)), page1 = __builtin_amdgcn_readlane(pages, 2 * (u - paged) + 1);
-            block0 = block_buffer(a.c, page0, head);
-            block1 = block_buffer(a.c, page1, head);
+            const int page0 = __builtin_amdgcn_readlane(pages, 2 * (u - paged) & 63), page1 = __builtin_amdgcn_readlane(pages, (2 * (u - paged) & 63) + 1);
+            block0 = block_buffer(a.c, page0, head, wanted);
+            block1 = block_buffer(a.c, page1, head, wanted);
             slot0 = base_of(u) & (a.c.ps() - 1);
             slot1 = (base_of(u) + 16) & (a.c.ps() - 1);
 #pragma unroll
-            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(block0, koff[i], slot0 * rb, &kw[0][i * L::KL / 4]);
+            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL, true>(block0, koff[i], slot0 * rb, &kw[0][i * L::KL / 4]);
 #pragma unroll
-            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL>(block1, koff[i], slot1 * rb, &kw[1][i * L::KL / 4]);
+            for (int i = 0; i < L::KB / L::KL; i++) load_bytes<L::KL, true>(block1, koff[i], slot1 * rb, &kw[1][i * L::KL / 4]);
             const uint8_t *fp = a.c.block(lane & 4 ? page1 : page0, head) + a.c.floats(0) + 4 * (lane & 4 ? slot1 : slot0);
             fw = *reinterpret_cast<const float4 *>(fp + foff);
         };
         auto load_values = [&] {  // of the step whose keys were asked for last
             const uint32_t at0 = (uint32_t)a.c.codes(1) + slot0 * rb, at1 = (uint32_t)a.c.codes(1) + slot1 * rb;
 #pragma unroll
-            for (int i = 0; i < 4; i++) load_bytes<L::VB>(block0, voff, at0 + i * rb, vw[i]);
+            for (int i = 0; i < 4; i++) load_bytes<L::VB, true>(block0, voff, at0 + i * rb, vw[i]);
 #pragma unroll
-            for (int i = 0; i < 4; i++) load_bytes<L::VB>(block1, voff, at1 + i * rb, vw[4 + i]);
+            for (int i = 0; i < 4; i++) load_bytes<L::VB, true>(block1, voff, at1 + i * rb, vw[4 + i]);
         };
 
         if (v.len > 0) {
@@ -169,7 +173,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
 #pragma unroll
         for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
-        auto step = [&](bool whole, int base, bool more, int next) {
+        auto step = [&](bool whole, int base, int next) {
             wave_sync();
             if (lane < 32) *reinterpret_cast<float4 *>(&params[wave][lane >> 3][4 * (lane & 7)]) = fw;
             wave_sync();
@@ -213,7 +217,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                     for (int p = 0; p < NP; p++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc[j], 0, 0, 0);
                 }
             }
-            if (more) load_keys(next);
+            load_keys(next);
             float p[8], pw[8], y[8];
             // scores less `ref`, -infinity where the row does not see the position
             auto score = [&](float ref) {
@@ -303,16 +307,15 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         if (v.len > 0)
             for (int u = 0; u < units; u++) {
                 const int base = base_of(u);
-                const bool more = u + 1 < units;
                 if (base < v.len) {  // (of the context's last positions some waves may have none)
                     // do all rows see all 32 positions?
                     const bool whole = base + 32 <= v.len && v.first >= 0 &&
                                        ((base + 31 <= v.first && (!a.window || base > v.last - a.window)) || base + 32 <= v.prefix);
-                    step(whole, base, more, u + 1);
-                } else if (more) {
+                    step(whole, base, u + 1);
+                } else {
                     load_keys(u + 1);
                 }
-                if (more) load_values();
+                load_values();
             }
 
         // ---- the four waves' parts joined
