@@ -12,7 +12,8 @@ constexpr int rows_workgroups(int dp) { return kCUs * (dp == 64 ? 3 : dp == 128 
 constexpr int chunk_workgroups(int dp, int np) { return kCUs * (dp == 256 && np == 2 ? 1 : 2); }
 
 // Joins the parts of the items that several workgroups have.  Blocks (w, y): the item that workgroup w goes on with, if it is the
-// first to go on with it; WAVES waves a query row, 16 lanes a part.  The parts' order in the sums is fixed by their number.
+// first to go on with it; WAVES waves a query row, 16 lanes a part.  The order of the sums is fixed by the parts' numbers.  A chain
+// of two fetches: where the parts are, then all of a part at once.
 template <int R, int DP, int WAVES>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPlan plan) {
     const int w = blockIdx.x;
@@ -23,47 +24,54 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPl
     // parts: of w - 1, which has its beginning, and of [w, w1]
     const int w1 = workgroup_of(first + b.units - 1, b.all, b.nw);
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, sub = lane & 15;
-    constexpr int kGroups = 4 * WAVES, kRows = 4 / WAVES;  // part groups a row, rows at a time
+    constexpr int kGroups = 4 * WAVES, kRows = 4 / WAVES, kC = DP / 64;  // part groups a row, rows at a time, float4s a lane
     const int group = (wave % WAVES) * 4 + lane / 16;
     __shared__ float tops[4], dens[4], part[WAVES > 1 ? 4 : 1][DP];
     const int64_t stride = R * (DP + 2);
-    const int left = (int)a.b.count(b.seq) * a.group - b.rt * R, rows = left < R ? left : R;
-    for (int r0 = blockIdx.y * kRows; r0 < rows; r0 += gridDim.y * kRows) {
-        const bool real = r0 + wave / WAVES < rows;
-        const int r = real ? r0 + wave / WAVES : rows - 1;
-        auto at = [&](int k) { return plan.partial + ((int64_t)k * 2 + (k == w - 1)) * stride; };
-        float top = kNothing;
-        for (int k = w - 1 + group * 16 + sub; k <= w1; k += kGroups * 16) top = fmaxf(top, at(k)[R * DP + r]);
+    for (int r0 = blockIdx.y * kRows; r0 < b.rows; r0 += gridDim.y * kRows) {
+        const bool real = r0 + wave / WAVES < b.rows;
+        const int r = real ? r0 + wave / WAVES : b.rows - 1;
+        float4 acc[kC];  // columns 64 c + 4 sub
+        float den = 0.f, top = kNothing;
 #pragma unroll
-        for (int m = 1; m < 64; m *= 2) top = fmaxf(top, __shfl_xor(top, m));
-        if constexpr (WAVES > 1) {
-            if (lane == 0) tops[wave] = top;
-            __syncthreads();
-            top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-        }
-        float4 acc[DP / 64];  // columns 64 c + 4 sub
-        float den = 0.f;
+        for (int c = 0; c < kC; c++) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto scale = [&](float by) {
+            den *= by;
 #pragma unroll
-        for (int c = 0; c < DP / 64; c++) acc[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int c = 0; c < kC; c++) acc[c].x *= by, acc[c].y *= by, acc[c].z *= by, acc[c].w *= by;
+        };
 #pragma unroll 2
         for (int k = w - 1 + group; k <= w1; k += kGroups) {
-            const float *x = at(k);
-            const float e = __builtin_amdgcn_exp2f(x[R * DP + r] - top);
-            den += e * x[R * DP + R + r];
+            const float *x = plan.partial + ((int64_t)k * 2 + (k == w - 1)) * stride;
+            const float its = x[R * DP + r], sum = x[R * DP + R + r];
+            float4 y[kC];
 #pragma unroll
-            for (int c = 0; c < DP / 64; c++) {
-                const float4 y = *reinterpret_cast<const float4 *>(x + r * DP + 64 * c + 4 * sub);
-                acc[c].x = fmaf(e, y.x, acc[c].x);
-                acc[c].y = fmaf(e, y.y, acc[c].y);
-                acc[c].z = fmaf(e, y.z, acc[c].z);
-                acc[c].w = fmaf(e, y.w, acc[c].w);
+            for (int c = 0; c < kC; c++) y[c] = *reinterpret_cast<const float4 *>(x + r * DP + 64 * c + 4 * sub);
+            const float now = fmaxf(top, its), e = __builtin_amdgcn_exp2f(its - now);
+            scale(__builtin_amdgcn_exp2f(top - now));
+            top = now;
+            den = fmaf(e, sum, den);
+#pragma unroll
+            for (int c = 0; c < kC; c++) {
+                acc[c].x = fmaf(e, y[c].x, acc[c].x);
+                acc[c].y = fmaf(e, y[c].y, acc[c].y);
+                acc[c].z = fmaf(e, y[c].z, acc[c].z);
+                acc[c].w = fmaf(e, y[c].w, acc[c].w);
             }
         }
+        float all = fmaxf(top, __shfl_xor(top, 16));
+        all = fmaxf(all, __shfl_xor(all, 32));
+        if constexpr (WAVES > 1) {
+            if (lane == 0) tops[wave] = all;
+            __syncthreads();
+            all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+        }
+        scale(__builtin_amdgcn_exp2f(top - all));
 #pragma unroll
         for (int m = 16; m < 64; m *= 2) {
             den += __shfl_xor(den, m);
 #pragma unroll
-            for (int c = 0; c < DP / 64; c++) {
+            for (int c = 0; c < kC; c++) {
                 acc[c].x += __shfl_xor(acc[c].x, m);
                 acc[c].y += __shfl_xor(acc[c].y, m);
                 acc[c].z += __shfl_xor(acc[c].z, m);
@@ -74,19 +82,19 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPl
             if (lane == 0) dens[wave] = den;
             if (lane < 16)
 #pragma unroll
-                for (int c = 0; c < DP / 64; c++) *reinterpret_cast<float4 *>(&part[wave][64 * c + 4 * sub]) = acc[c];
+                for (int c = 0; c < kC; c++) *reinterpret_cast<float4 *>(&part[wave][64 * c + 4 * sub]) = acc[c];
             __syncthreads();
             den = dens[0] + dens[1] + dens[2] + dens[3];
         }
         const int row = b.rt * R + r;
-        const int64_t dst = ((a.b.first(b.seq) + row / a.group) * ((int64_t)a.c.heads * a.group) + b.head * a.group + row % a.group) * a.c.d;
+        const int64_t dst = ((b.token + row / a.group) * ((int64_t)a.c.heads * a.group) + b.head * a.group + row % a.group) * a.c.d;
         const float inv = den != 0.f ? 1.f / den : 0.f;
         if constexpr (WAVES > 1) {
             if (tid < a.c.d) store_result(a, dst + tid, (part[0][tid] + part[1][tid] + part[2][tid] + part[3][tid]) * inv);
             __syncthreads();
         } else if (real && lane < 16) {
 #pragma unroll
-            for (int c = 0; c < DP / 64; c++) {
+            for (int c = 0; c < kC; c++) {
                 const int col = 64 * c + 4 * sub;
                 store_four(a, dst + col, a.c.d - col, make_float4(acc[c].x * inv, acc[c].y * inv, acc[c].z * inv, acc[c].w * inv));
             }

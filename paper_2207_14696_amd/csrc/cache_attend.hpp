@@ -40,6 +40,8 @@ struct PartOf {  // where a workgroup begins
     int unit, units;  // the first unit it has of the item, and the item's
     int nw;           // workgroups that have units (0: this one has none)
     int start, all;   // units before it, and of the call
+    int rows;         // of the item
+    int64_t token;    // the sequence's first of the call
 };
 struct AttendPlan {
     int items;       // per head; of a ragged batch with numbers left free (see first_item)
@@ -183,7 +185,8 @@ __device__ inline void locate(const AttendCall &a, const AttendPlan &p, int w, i
             const int rt = i - first_item<R>(a, s), u = view_of<R, TOK>(a, s, rt).units;
             if (left < u) {
                 sh[8] = s, sh[9] = rt, sh[10] = left;
-                p.begins[w] = {*head, s, rt, left, u, nw, *start, all};
+                const int rows = (int)a.b.count(s) * a.group - rt * R;
+                p.begins[w] = {*head, s, rt, left, u, nw, *start, all, rows < R ? rows : R, a.b.first(s)};
                 break;
             }
             left -= u;
