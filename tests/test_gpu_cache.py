@@ -508,3 +508,49 @@ def test_refusals_of_the_python_calls(bf, torch):
         with pytest.raises(bf.BifeatError) as e:
             call()
         assert e.value.status == bf.EINVAL
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+@pytest.mark.parametrize("n", [1, 40])
+def test_many_sequences(bf, torch, ragged, n):
+    # more sequences and items than a workgroup has threads; in the ragged batch some bring nothing
+    B, heads, d, ps = 700 if n == 1 else 300, 1, 32, 16
+    rng = np.random.default_rng(n)
+    lengths = [int(x) for x in rng.integers(n, n + 90, B)]
+    lengths[B // 2] = 900   # contexts are shared between workgroups
+    news = [n] * B if not ragged else [int(x) for x in rng.integers(0, n + 1, B)]
+    _attend_case(bf, torch, 8, heads, 2, d, ps, "f16", lengths, news, uniform=not ragged, seed=B)
+
+
+@pytest.mark.parametrize("dtype,bits,d", [("f16", 4, 64), ("bf16", 8, 256), ("f32", 8, 128)])
+@pytest.mark.parametrize("news", [[1, 1], [20, 20], [200, 90]])
+@pytest.mark.parametrize("opts", [dict(window=300, prefix=[130, 700]), dict(window=64, slopes=True), dict(window=1000, prefix=[1, 0], cap=20.0)])
+def test_attend_over_a_window_and_a_prefix_far_apart(bf, torch, news, opts, dtype, bits, d):
+    _attend_case(bf, torch, bits, 1, 2, d, 32, dtype, [2300, 1500], news, **opts)
+
+
+def test_every_row_of_a_call_may_see_nothing(bf, torch):
+    batch = Batch(torch, [0, 0], [3, 3], 16)
+    c = bf.PagedCache(8, 1, 64, 16)
+    pages = torch.full((batch.count, c.page_bytes), 255, dtype=torch.uint8, device="cuda")
+    q = torch.randn(6, 2, 64, device="cuda")
+    out = torch.full_like(q, 7.0)
+    c.attend(pages, q, batch.d_tables, batch.d_lengths, out=out)
+    assert not out.any()
+    k = torch.randn(6, 1, 64, device="cuda")
+    c.write(pages, k, k, batch.d_tables, batch.d_lengths)
+    assert (pages == 255).all()
+    assert not any(x.any() for x in c.read(pages, batch.d_tables, batch.d_lengths, 6))
+
+
+def test_the_example(bf, torch):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "cached_answers.py")
+    spec = importlib.util.spec_from_file_location("cached_answers", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    off = {bits: example.answer(bits, prompts=(70, 33, 5), tokens=6, chunk=32) for bits in (4, 8)}
+    # logits against those without a cache: a value's level is 1 / 255 or 1 / 15 of its row's range, of which half is the most
+    # that it is off by; two layers' worth, relative to the logits' size
+    assert off[8] < 0.03 and off[8] < off[4] < 0.4
