@@ -24,9 +24,10 @@ struct RowLanes {
     static constexpr int VW = VB < 4 ? 1 : VB / 4;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); MODE: 1: scores are biased by
-// distance, 2: capped (and biased)
-template <int BITS, int DP, int NP, int MODE>
+// NP: fp16 pieces of a query element (2 for 32-bit queries); WP: of a weight.  One is enough where the result is rounded to
+// bf16 (2^-9; a weight's one piece 2^-12, the second costs 8 % of long contexts in 4 bits); an fp16 result would be 1.6 times as far off
+// with one, and the second costs it 1 %.  MODE: 1: scores are biased by distance, 2: capped (and biased)
+template <int BITS, int DP, int NP, int WP, int MODE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
     using L = RowLanes<BITS, DP>;
     constexpr int R = kRowsR, TOK = kRowsTok;
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 weigh();
             }
             // ---- weights
-            half8 w[NP];
+            half8 w[WP];
             if (whole) {
 #pragma unroll
                 for (int e = 0; e < 8; e++) mins = fmaf(p[e], vm[e], mins);
@@ -278,12 +279,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             for (int e = 0; e < 8; e++) {
                 total += p[e];
                 w[0][e] = (_Float16)pw[e];
-                if constexpr (NP == 2) w[NP - 1][e] = (_Float16)(pw[e] - (float)w[0][e]);
+                if constexpr (WP == 2) w[WP - 1][e] = (_Float16)(pw[e] - (float)w[0][e]);
             }
             if constexpr (NP == 1)
 #pragma unroll
-                for (int e = 0; e < 8; e += 2)
-                    mins = __builtin_amdgcn_fdot2(half2v{w[0][e], w[0][e + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins, false);
+                for (int p = 0; p < WP; p++)
+#pragma unroll
+                    for (int e = 0; e < 8; e += 2)
+                        mins = __builtin_amdgcn_fdot2(half2v{w[p][e], w[p][e + 1]}, half2v{(_Float16)-kMiddle, (_Float16)-kMiddle}, mins, false);
             // ---- values: lane (n16, g) has columns [n16 DP/16, ...) of eight positions
 #pragma unroll
             for (int t = 0; t < L::VT; t++) {
@@ -299,7 +302,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 }
                 if constexpr (NP == 2) val = centred(val, all_of(BITS == 8 || (t & 1) ? 1152.f : 1032.f));
 #pragma unroll
-                for (int p = 0; p < NP; p++)
+                for (int p = 0; p < WP; p++)
                     o[t] = __builtin_amdgcn_mfma_f32_16x16x32_f16(val, w[p], o[t], 0, 0, 0);
             }
         };
