@@ -87,13 +87,19 @@ __device__ inline void load8_any(const T *p, int left, float (&x)[8]) {
         for (int i = 0; i < 8; i++) x[i] = i < left ? to_float(p[i]) : 0.f;
     }
 }
-template <typename T>
+// STREAMED: not kept in the caches
+template <bool STREAMED, typename T>
 __device__ inline void store8_any(T *p, int left, const float (&x)[8]) {
     if (left >= 8) {
         Eight<T> e;
 #pragma unroll
         for (int i = 0; i < 8; i++) e.v[i] = from_float<T>(x[i]);
-        *reinterpret_cast<Eight<T> *>(p) = e;
+        if constexpr (STREAMED) {
+            typedef uint32_t Words __attribute__((ext_vector_type(2 * sizeof(T)), aligned(sizeof(T))));
+            __builtin_nontemporal_store(__builtin_bit_cast(Words, e), reinterpret_cast<Words *>(p));
+        } else {
+            *reinterpret_cast<Eight<T> *>(p) = e;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 8; i++)
