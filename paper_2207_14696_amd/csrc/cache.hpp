@@ -18,7 +18,7 @@ struct bifeat_cache {
 namespace bf {
 
 int record_hip_error(hipError_t e, const char *what);
-int take_block(void **out);  // a zeroed device block of 1 KB from a pool, and back
+int take_block(void **out);  // a device block of 1 KB from a pool, its bytes as the last use left them, and back
 void give_block(void *blk);
 
 // The pages as the kernels see them.
@@ -87,22 +87,22 @@ __device__ inline void load8_any(const T *p, int left, float (&x)[8]) {
         for (int i = 0; i < 8; i++) x[i] = i < left ? to_float(p[i]) : 0.f;
     }
 }
-// STREAMED: not kept in the caches
-template <bool STREAMED, typename T>
-__device__ inline void store8_any(T *p, int left, const float (&x)[8]) {
-    if (left >= 8) {
-        Eight<T> e;
+// N columns next to each other, of which the row has `left`.  STREAMED: not kept in the caches
+template <int N, bool STREAMED, typename T>
+__device__ inline void store_any(T *p, int left, const float *x) {
+    if (left >= N) {
+        struct Columns {
+            T v[N];
+        } e;
 #pragma unroll
-        for (int i = 0; i < 8; i++) e.v[i] = from_float<T>(x[i]);
-        if constexpr (STREAMED) {
-            typedef uint32_t Words __attribute__((ext_vector_type(2 * sizeof(T)), aligned(sizeof(T))));
-            __builtin_nontemporal_store(__builtin_bit_cast(Words, e), reinterpret_cast<Words *>(p));
-        } else {
-            *reinterpret_cast<Eight<T> *>(p) = e;
-        }
+        for (int i = 0; i < N; i++) e.v[i] = from_float<T>(x[i]);
+        typedef uint32_t Words __attribute__((ext_vector_type(N * sizeof(T) / 4), aligned(sizeof(T))));
+        const Words w = __builtin_bit_cast(Words, e);
+        if constexpr (STREAMED) __builtin_nontemporal_store(w, reinterpret_cast<Words *>(p));
+        else *reinterpret_cast<Words *>(p) = w;
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; i++)
+        for (int i = 0; i < N; i++)
             if (i < left) p[i] = from_float<T>(x[i]);
     }
 }

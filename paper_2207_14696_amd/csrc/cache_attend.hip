@@ -102,14 +102,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPl
     }
 }
 
-// rows: the most that an item has
-template <int R>
+// rows: the most that an item has.  Four waves a row where an item of 16 rows may have 48 parts or more (one sequence of 8192, 4 rows
+// on 8 heads of 128, 64 parts: 16.7 us, with one wave 17.2), one where it has fewer (8 such sequences of 2048: 23.5 and 20.6).
+template <int R, int WAVES>
 void launch_join(const AttendCall &a, const AttendPlan &p, int dp, int rows) {
-    constexpr int kWaves = R == 16 ? 4 : 1;
-    const dim3 grid(p.nw, std::min(16, (rows * kWaves + 3) / 4));
-    if (dp == 64) attend_join_kernel<R, 64, kWaves><<<grid, 256, 0, a.s>>>(a, p);
-    else if (dp == 128) attend_join_kernel<R, 128, kWaves><<<grid, 256, 0, a.s>>>(a, p);
-    else attend_join_kernel<R, 256, kWaves><<<grid, 256, 0, a.s>>>(a, p);
+    const dim3 grid(p.nw, std::min(16, (rows * WAVES + 3) / 4));
+    if (dp == 64) attend_join_kernel<R, 64, WAVES><<<grid, 256, 0, a.s>>>(a, p);
+    else if (dp == 128) attend_join_kernel<R, 128, WAVES><<<grid, 256, 0, a.s>>>(a, p);
+    else attend_join_kernel<R, 256, WAVES><<<grid, 256, 0, a.s>>>(a, p);
 }
 
 // numbers of a head's items, an upper bound where the batch is ragged
@@ -144,24 +144,40 @@ bool ensure_partial(bifeat_cache *h, hipStream_t s) {
 
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     const int dp = a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256, bits = h->spec.bits;
-    const bool chunk = a.b.tokens * a.group > (int64_t)32 * a.b.B;
     const int np = a.dtype == BIFEAT_F32 ? 2 : 1;
+    const int64_t width = a.b.width << a.c.ps_log2;
+    auto units_of = [&](int R, int tok) { return (int64_t)items_of(a, R) * a.c.heads * ((width + tok - 1) / tok); };
+    // The kernel for many rows makes operands once for 64 or 128 rows; that for few, for 16, starts and joins sooner.  Few: up to 64
+    // rows of 64 columns a sequence and head on average (64 sequences of 4096, 12 heads: 294 us, the other kernel 300; 128
+    // rows 577 and 310), 32 of 128 (8 heads: 193 and 207; 48 rows 286 and 235), 16 of 256 (4 heads: 20 rows 195 and 161; 32 where a
+    // window leaves an unknown part of the context: 20 rows, 1024 positions seen 47 and 64).  And any number where the units
+    // come to 10 a workgroup or fewer: 64 rows of 8 sequences of 2048 on 8 heads of 128 (10) 40 and 53, 256 rows of one of 512 (1)
+    // 15 and 30, 256 rows of 8 of 1024 (17) 67 and 58.  Not for 32-bit queries, whose operands cost twice (385 rows of three of
+    // 1001, 2 units: 32 and 29.5).
+    const int few = dp == 64 ? 64 : dp == 256 && !a.window ? 16 : 32;
+    const bool chunk = a.b.tokens * a.group > (int64_t)few * a.b.B &&
+                       (np == 2 || units_of(kRowsR, kRowsTok) > 10 * rows_workgroups(dp));
     const int R = chunk ? 64 * chunk_tiles(dp, np) : kRowsR, tok = !chunk ? kRowsTok : dp == 256 ? 32 : 64;
+    const int most = chunk ? chunk_workgroups(dp, np) : rows_workgroups(dp);
     AttendPlan p;
     p.items = items_of(a, R);
-    const int64_t most = ((a.b.width << a.c.ps_log2) + tok - 1) / tok, all = (int64_t)p.items * a.c.heads;
-    // contexts of a few units, and calls that find no workspace: an item a workgroup, nothing to join (nor beyond 2^31 units)
-    const bool split = most > 4 && all * most <= INT32_MAX && ensure_partial(h, a.s);
+    const int64_t all = (int64_t)p.items * a.c.heads, units = units_of(R, tok);
+    // An item a workgroup and nothing to join: where the workgroups all run at once and have 6 units or fewer (2 of the kernel for
+    // many rows); 4 rows of 8 sequences on 8 heads of 128: at 512 positions 13.6 us, dealt evenly and joined 16.0; at
+    // 1024 19.3 and 16.3.  And calls that find no workspace, or have 2^31 units or more.
+    const bool small = width <= (chunk ? 128 : 6 * kRowsTok) && all <= most;
+    const bool split = !small && units <= INT32_MAX && ensure_partial(h, a.s);
     p.partial = split ? h->d_partial : nullptr;
     p.begins = split ? reinterpret_cast<PartOf *>(h->d_partial + kPartialFloats) : nullptr;
-    p.nw = (int)(split ? std::min<int64_t>(all * most, chunk ? chunk_workgroups(dp, np) : rows_workgroups(dp)) : all);
+    p.least = !chunk ? 2 : np == 2 ? 1 : 4;
+    p.nw = split ? workgroups_of(units, p.least, most) : (int)all;
     const int rows = a.b.indptr ? R : std::min(R, a.b.n * a.group);
     if (chunk) {
         if (hipError_t e = launch_attend_chunk(a, p, bits, dp)) return e;
-        if (split) R == 128 ? launch_join<128>(a, p, dp, rows) : launch_join<64>(a, p, dp, rows);
+        if (split) R == 128 ? launch_join<128, 1>(a, p, dp, rows) : launch_join<64, 1>(a, p, dp, rows);
     } else {
         launch_attend_rows(a, p, bits, dp);
-        if (split) launch_join<kRowsR>(a, p, dp, rows);
+        if (split) p.nw < (int64_t)48 * a.b.B * a.c.heads ? launch_join<kRowsR, 1>(a, p, dp, rows) : launch_join<kRowsR, 4>(a, p, dp, rows);
     }
     return hipGetLastError();
 }

@@ -46,10 +46,20 @@ struct PartOf {  // where a workgroup begins
 struct AttendPlan {
     int items;       // per head; of a ragged batch with numbers left free (see first_item)
     int nw;
+    int least;       // units that a workgroup has at least (see workgroups_of)
     // null: a workgroup has one item, all of it (contexts are short, or there is no workspace)
     float *partial;  // [nw][2]: of an item begun before / not ended by a workgroup sums [R][DP], reference [R], sum of weights [R]
     PartOf *begins;  // [nw]
 };
+
+// Workgroups of a call with `all` units: as many as run at a time (most), fewer where each would have less than `least` units;
+// least 4: 2 will do where units are fewer than 512.  What workgroups leave to be joined costs more than a few units one after another:
+// 16 rows of each of 8 sequences of 1024 on 8 heads of 128 (512 units) took 30 us by a unit each, 22 by two; 64 rows (1024 units,
+// kernel for many) 47 by two, 39 by four; 64 rows of one of 512 (64 units) 26.5 by one, 26.7 by two, 31 by four.
+__host__ __device__ inline int workgroups_of(int64_t all, int least, int most) {
+    const int64_t n = least < 4 ? all / least : all < 512 ? all / 2 : all < 1024 ? 256 : all / 4;
+    return n > most ? most : n > 1 ? (int)n : all > 0;
+}
 
 // `all` units over nw workgroups, nw <= all: the first all % nw have one more than the others
 __device__ inline int start_of(int w, int all, int nw) { return w * (all / nw) + (w < all % nw ? w : all % nw); }
@@ -167,7 +177,7 @@ __device__ inline void locate(const AttendCall &a, const AttendPlan &p, int w, i
         total += sh[k];
     }
     total = __builtin_amdgcn_readfirstlane(total);
-    const int all = total * a.c.heads, nw = all < p.nw ? all : p.nw;  // (none has nothing between two that have)
+    const int all = total * a.c.heads, nw = workgroups_of(all, p.least, p.nw);  // (none has nothing between two that have)
     if (w >= nw) {
         *start = *end = 0;
         if (tid == 0) p.begins[w].nw = 0;

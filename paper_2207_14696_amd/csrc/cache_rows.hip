@@ -137,35 +137,38 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, Cac
 }
 
 // Bound by the bytes of the result, twice (fp32: four times) the codes'.  STREAMED past the caches where they would not hold it:
-// 149 000 tokens of 8 heads of 128 in 8 bits to bf16 (610 MB written, 320 read) 257 us, 167 so; 26 MB 13 us, 11 so.
+// 149 000 tokens of 8 heads of 128 in 8 bits to bf16 (610 MB written, 320 read) 257 us, 167 so (5.6 TB/s); 26 MB 13 us, 11 so.
+// 65 536 tokens to fp32 (537 MB written) 143 us, 104 so; with a lane's eight columns next to each other, half a line a store, 257.
 template <typename T, int BITS, int LPR, bool STREAMED>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CachePages c, CacheBatch b, T *k, T *v, int per) {
     __shared__ Places places;
     const int64_t t0 = (int64_t)blockIdx.x * per;
     const int count = b.tokens - t0 < per ? (int)(b.tokens - t0) : per;
     find_places(c, b, t0, count, places);
-    const int sub = threadIdx.x % LPR, col = 8 * sub, rows = count * 2 * c.heads;
+    // a lane's columns: eight next to each other, in fp32 four and four, so that each store of a row's lanes fills whole lines
+    constexpr int kSets = sizeof(T) == 4 ? 2 : 1, kCols = 8 / kSets, kBytes = kCols * BITS / 8, kWords = (kBytes + 3) / 4;
+    const int sub = threadIdx.x % LPR, col = kCols * sub, rows = count * 2 * c.heads;
     if (col >= c.d) return;
     constexpr int kAhead = 8;  // rows in flight
     for (int r0 = threadIdx.x / LPR; r0 < rows; r0 += kAhead * (kThreads / LPR)) {
-        uint32_t w[kAhead][BITS / 4];
+        uint32_t w[kAhead][kSets][kWords];
         float scale[kAhead], mn[kAhead];
 #pragma unroll
         for (int i = 0; i < kAhead; i++) {
             const int r = r0 + i * (kThreads / LPR), token = r % count, hw = r / count, which = hw >= c.heads, head = hw - which * c.heads;
             scale[i] = mn[i] = 0.f;
 #pragma unroll
-            for (int e = 0; e < BITS / 4; e++) w[i][e] = 0;
+            for (int g = 0; g < kSets; g++)
+#pragma unroll
+                for (int e = 0; e < kWords; e++) w[i][g][e] = 0;
             if (r < rows && places.page[token] >= 0) {
                 const uint8_t *block = c.pages + places.page[token] + head * c.head_bytes;
                 const int slot = places.slot[token];
                 const uint8_t *codes = block + c.codes(which) + slot * c.rb;
-                if constexpr (BITS == 8) {
-                    const uint2 u = *reinterpret_cast<const uint2 *>(codes + 8 * sub);
-                    w[i][0] = u.x, w[i][BITS / 4 - 1] = u.y;
-                } else {
-                    w[i][0] = *reinterpret_cast<const uint32_t *>(codes + 4 * sub);
-                }
+#pragma unroll
+                for (int g = 0; g < kSets; g++)
+                    if (g == 0 || col + g * kCols * LPR < c.d)
+                        __builtin_memcpy(w[i][g], __builtin_assume_aligned(codes + kBytes * (sub + g * LPR), kBytes), kBytes);
                 const float *f = reinterpret_cast<const float *>(block + c.floats(which)) + slot;
                 scale[i] = f[0], mn[i] = f[c.ps()];
             }
@@ -174,13 +177,18 @@ __global__ __launch_bounds__(kThreads) void cache_read_kernel(CachePages c, Cach
         for (int i = 0; i < kAhead; i++) {
             const int r = r0 + i * (kThreads / LPR), token = r % count, hw = r / count, which = hw >= c.heads, head = hw - which * c.heads;
             if (r >= rows) break;
-            float x[8];
+            T *row = (which ? v : k) + ((t0 + token) * c.heads + head) * c.d;
 #pragma unroll
-            for (int e = 0; e < 8; e++) {
-                const uint32_t q = BITS == 8 ? w[i][e / 4 % (BITS / 4)] >> 8 * (e & 3) & 255 : w[i][0] >> 4 * e & 15;
-                x[e] = fmaf((float)q, scale[i], mn[i]);
+            for (int g = 0; g < kSets; g++) {
+                float x[kCols];
+#pragma unroll
+                for (int e = 0; e < kCols; e++) {
+                    const uint32_t q = w[i][g][e * BITS / 32] >> e * BITS % 32 & ((1u << BITS) - 1);
+                    x[e] = fmaf((float)q, scale[i], mn[i]);
+                }
+                const int at = col + g * kCols * LPR;
+                if (g == 0 || at < c.d) store_any<kCols, STREAMED>(row + at, c.d - at, x);
             }
-            store8_any<STREAMED>((which ? v : k) + ((t0 + token) * c.heads + head) * c.d + col, c.d - col, x);
         }
     }
 }
@@ -204,8 +212,12 @@ __global__ void cache_check_zero_kernel(int32_t *bad) { *bad = 0; }
 
 int lanes_per_row(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
-// tokens a workgroup: up to 16, whose places are looked up at once, where that leaves 2048 workgroups
-int tokens_per(const CacheBatch &b) { return (int)std::max<int64_t>(1, std::min<int64_t>(kTokens, b.tokens / 2048)); }
+// Tokens a workgroup: up to 16, whose places are looked up at once, where that leaves so many workgroups.  8 heads of 128 in 8 bits, bf16:
+// written with 2048 so 8192 tokens take 19 us (with 512: 27, with 8192: 25), 2048 8.4 (7.7, 8.4); read with 1024 4096 take 6.0
+// (with 2048: 9.3), 8192 to fp32 14.3 (with 512: 16.3).
+int tokens_per(const CacheBatch &b, int workgroups) {
+    return (int)std::max<int64_t>(1, std::min<int64_t>(kTokens, b.tokens / workgroups));
+}
 unsigned row_blocks(const CacheBatch &b, int per) { return (unsigned)((b.tokens + per - 1) / per); }
 
 }  // namespace
@@ -217,7 +229,7 @@ unsigned row_blocks(const CacheBatch &b, int per) { return (unsigned)((b.tokens 
 
 hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const HeadRows &k, const HeadRows &v, int bits, int dtype,
                               hipStream_t s) {
-    const int lpr = lanes_per_row(c.d), per = tokens_per(b);
+    const int lpr = lanes_per_row(c.d), per = tokens_per(b, 2048);
     const unsigned grid = row_blocks(b, per);
 #define BF_GO(T, LPR)                                                                     \
     if (bits == 8) cache_write_kernel<T, 8, LPR><<<grid, kThreads, 0, s>>>(c, b, k, v, per);   \
@@ -229,7 +241,7 @@ hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const He
 }
 
 hipError_t launch_cache_read(const CachePages &c, const CacheBatch &b, void *k, void *v, int bits, int dtype, hipStream_t s) {
-    const int lpr = lanes_per_row(c.d), per = tokens_per(b);
+    const int lpr = lanes_per_row(c.d), per = tokens_per(b, 1024);
     const unsigned grid = row_blocks(b, per);
     const bool stream = b.tokens * 2 * c.heads * c.d * (dtype == BIFEAT_F32 ? 4 : 2) > (16 << 20);
 #define BF_GO(T, LPR)                                                                                                             \
