@@ -402,8 +402,9 @@ int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *in
  * Queries of BIFEAT_F16 and BIFEAT_BF16 enter the matrix cores as fp16 (scaled by a
  * power of two per tile of rows: exact but for bf16 columns 2^-29 of a tile's largest),
  * codes as they are; products are summed in fp32, softmax and its sums are fp32, weights
- * are rounded to fp16 before they meet the values' codes.  BIFEAT_F32: queries and
- * weights enter as two fp16 pieces each (22 bits). */
+ * are rounded to fp16 before they meet the values' codes (BIFEAT_F16 with few rows: to two
+ * fp16 pieces).  BIFEAT_F32: queries and weights enter as two fp16 pieces each (22 bits).
+ * Which kernel runs, and so the rounding, depends on the call's sizes (not on its data). */
 typedef struct {
     int32_t bits;      /* 4 or 8 */
     int32_t heads;     /* cached heads, 1..1024 */

