@@ -102,8 +102,8 @@ __device__ inline void write_row(const CachePages &c, const float (&x)[8], bool 
     }
 }
 
-// Bound by the bytes of k and v and of the codes: 65 536 tokens of 8 heads of 128, bf16 to 8 bits (268 MB read, 143 written) 121 us,
-// 3.4 TB/s; fp32 (537 MB read) 157, 4.3 TB/s.  A row's codes are 128 bytes of a page, its two floats 8 more, elsewhere in it.
+// Bound by the bytes of k and v and of the codes: 65 536 tokens of 8 heads of 128, bf16 to 8 bits (268 MB read, 143 written) 112 us,
+// 3.7 TB/s; fp32 (537 MB read) 153, 4.4 TB/s.  A row's codes are 128 bytes of a page, its two floats 8 more, elsewhere in it.
 template <typename T, int BITS, int LPR>
 __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, CacheBatch b, HeadRows k, HeadRows v, int per) {
     __shared__ Places places;
@@ -111,29 +111,19 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, Cac
     const int count = b.tokens - t0 < per ? (int)(b.tokens - t0) : per;
     find_places(c, b, t0, count, places);
     const int sub = threadIdx.x % LPR, col = 8 * sub, rows = count * 2 * c.heads;
-    constexpr int kAhead = 2, kStep = kThreads / LPR;  // rows in flight
-    // (a wave's rows are taken together, those past the end as zeros that are not stored)
-    for (int r0 = threadIdx.x / 64 * (64 / LPR); r0 < rows; r0 += kAhead * kStep) {
-        float xs[kAhead][8];
-        bool reals[kAhead];
+    // (a wave's rows are taken together, those past the end as zeros that are not stored; a row at a time: with two on their way
+    // fewer waves fit, and 65 536 tokens took 121 us where they now take 112)
+    for (int r0 = threadIdx.x / 64 * (64 / LPR); r0 < rows; r0 += kThreads / LPR) {
+        const int r = r0 + threadIdx.x % 64 / LPR, token = r % count, hw = r / count, which = hw >= c.heads, head = hw - which * c.heads;
+        const bool real = r < rows && places.page[token] >= 0;
+        float x[8];
 #pragma unroll
-        for (int i = 0; i < kAhead; i++) {
-            const int r = r0 + i * kStep + threadIdx.x % 64 / LPR, token = r % count, hw = r / count, which = hw >= c.heads;
-            reals[i] = r < rows && places.page[token] >= 0;
-#pragma unroll
-            for (int e = 0; e < 8; e++) xs[i][e] = 0.f;
-            if (reals[i]) {
-                const HeadRows &h = which ? v : k;
-                load8_any(static_cast<const T *>(h.data) + (t0 + token) * h.token_stride + (hw - which * c.heads) * h.head_stride + col,
-                          c.d - col, xs[i]);
-            }
+        for (int e = 0; e < 8; e++) x[e] = 0.f;
+        if (real) {
+            const HeadRows &h = which ? v : k;
+            load8_any(static_cast<const T *>(h.data) + (t0 + token) * h.token_stride + head * h.head_stride + col, c.d - col, x);
         }
-#pragma unroll
-        for (int i = 0; i < kAhead; i++) {
-            const int r = r0 + i * kStep + threadIdx.x % 64 / LPR, token = r % count, hw = r / count, which = hw >= c.heads;
-            write_row<BITS, LPR>(c, xs[i], reals[i], c.pages + places.page[token] + (hw - which * c.heads) * c.head_bytes, which,
-                                 places.slot[token]);
-        }
+        write_row<BITS, LPR>(c, x, real, c.pages + places.page[token] + head * c.head_bytes, which, places.slot[token]);
     }
 }
 
@@ -214,8 +204,8 @@ __global__ void cache_check_zero_kernel(int32_t *bad) { *bad = 0; }
 int lanes_per_row(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
 // Tokens a workgroup: up to 16, whose places are looked up at once, where that leaves so many workgroups.  8 heads of 128 in 8 bits, bf16:
-// written with 2048 so 8192 tokens take 19 us (with 512: 27, with 8192: 25), 2048 8.4 (7.7, 8.4); read with 1024 4096 take 6.0
-// (with 2048: 9.3), 8192 to fp32 14.3 (with 512: 16.3).
+// written with 2048 8192 tokens take 17.7 us, 32 768 56 (with 8192: 20.5 and 53); read with 1024 4096 take 6.0 (with 2048: 9.3),
+// 8192 to fp32 14.3 (with 512: 16.3).
 int tokens_per(const CacheBatch &b, int workgroups) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(kTokens, b.tokens / workgroups));
 }
