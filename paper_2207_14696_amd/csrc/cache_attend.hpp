@@ -20,10 +20,15 @@ constexpr int kRowsR = 16, kRowsTok = 128;    // items and units of the kernel f
 // that the lanes outside the branch got their values back wrong.  Two tiles where sums and queries leave room for it.
 constexpr int chunk_tiles(int dp, int np) { return dp == 64 || (dp == 128 && np == 1) ? 2 : 1; }
 constexpr float kLog2e = 1.4426950408889634f;
-// A row's weights are p = 2^(x - top), and fp16 gets p * s: `top`, a whole number, follows the largest x + log2(s), so that
-// scales of values of any size fit.  It may lag (products up to 2^15) and is brought up for all lanes of a row together, to leave them 2^8.  Rows
-// of one value (s = 0) count with the least scale, which leaves p within 2^105; their codes are 0.
-constexpr float kLeastScale = 8.077935669463161e-28f;  // 2^-90
+// A row's weights are p = 2^(x - top), and fp16 gets p * s: `top`, a whole number, follows the largest x + log2(size), with the
+// scale s of the position's values for its size.  It may lag (p * size up to 2^15) and is brought up for all lanes of a row together, to
+// leave them 2^8.  A scale below 2^-80 (0 where the values are one) would let p grow without bound, and p * mn with it: such a position's
+// size is 2^-80, or its values' by 2^24 where that is more, so that p stays within 2^95 and p * mn within 2^39, which leaves 2^30 positions
+// room.  Steps that have one are sent down the seldom taken branch that brings `top` up; nothing else is asked of the others.  From 2^-80 on
+// scales need no such care: written values of which two differ have s > mn 2^-32.
+constexpr float kLeastScale = 8.271806125530277e-25f;  // 2^-80
+// (of the middle code's value, which is within 2^7 s of mn)
+__device__ inline float size_of(float s, float middle) { return s < kLeastScale ? fmaxf(fabsf(middle) * 5.9604644775390625e-8f, kLeastScale) : s; }
 constexpr float kNothing = -1e30f;  // running maximum where nothing was seen: below any score, and finite
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));

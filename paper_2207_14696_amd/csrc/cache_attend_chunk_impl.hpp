@@ -58,7 +58,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
     const int vo = (n16 * S::VP + vpart) * S::VB;
     const uint32_t voff = 4 * g * rb + (vo < rb ? vo : 0);
     // wave w brings array w of the floats in LDS, a position a lane: key scale times f, key offset (NP == 2: the middle
-    // code's value), value scale, value of the middle code
+    // code's value), value scale (1 behind the last position), value of the middle code
     const int fat = lane % TOK;
 
     while (cur < end) {
@@ -138,8 +138,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 values[buf][vgroup * S::VT + vpart * (S::VT / S::VP) + t][lane] = __builtin_bit_cast(uint4, val);
             }
             const bool there = base_of(u) + fat < v.len;  // what no token was written to may hold anything
-            float x = there ? fscale : 0.f;
-            if (wave >= 2) x = fmaxf(x, kLeastScale);
+            float x = there ? fscale : wave == 2 ? 1.f : 0.f;
             if (wave == 0) x *= f;
             if (wave & 1) x = fmaf(x, wave == 3 || NP == 2 ? kMiddle : 0.f, there ? fmin : 0.f);
             if (lane < TOK) params[buf][wave][fat] = x;
@@ -278,8 +277,10 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                         for (int i = 0; i < 4; i++) y[i] = bits >> i & 1 ? y[i] : -INFINITY;
                     }
                 };
+                // infinite where a value's size (see size_of) is not its scale.  (2 % of 2048 tokens over 32 768, as much as a flag a tile)
+                const float sized = fminf(fminf(vs[0], vs[1]), fminf(vs[2], vs[3])) < kLeastScale ? INFINITY : 0.f;
                 auto weigh = [&] {
-                    float most = 0.f;
+                    float most = sized;
 #pragma unroll
                     for (int n = 0; n < NT; n++) {
                         float y[4];
@@ -299,7 +300,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                         float y[4], now = kNothing;
                         score(n, 0.f, y);
 #pragma unroll
-                        for (int i = 0; i < 4; i++) now = fmaxf(now, y[i] + __builtin_amdgcn_logf(vs[i]));
+                        for (int i = 0; i < 4; i++) now = fmaxf(now, y[i] + __builtin_amdgcn_logf(size_of(vs[i], vm[i])));
                         now = fmaxf(now, __shfl_xor(now, 16));
                         now = fmaxf(now, __shfl_xor(now, 32));
                         now = fmaxf(top[n], ceilf(now) - 8.f);  // (whole numbers: what is kept is kept exactly)

@@ -177,6 +177,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         for (int t = 0; t < L::VT; t++) o[t] = float4v{0.f, 0.f, 0.f, 0.f};
 
         auto step = [&](bool whole, int base, int next) {
+            const bool sized = __any((lane >> 3 & 3) == 2 && fminf(fminf(fw.x, fw.y), fminf(fw.z, fw.w)) < kLeastScale);  // (see size_of)
             wave_sync();
             if (lane < 32) *reinterpret_cast<float4 *>(&params[wave][lane >> 3][4 * (lane & 7)]) = fw;
             wave_sync();
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                     const int e = 4 * j + i;
                     ks[e] = (&p[0].x)[i];
                     km[e] = NP == 2 ? fmaf(ks[e], kMiddle, (&p[1].x)[i]) : (&p[1].x)[i];
-                    vs[e] = fmaxf((&p[2].x)[i], kLeastScale);
+                    vs[e] = (&p[2].x)[i];
                     vm[e] = fmaf(vs[e], kMiddle, (&p[3].x)[i]);
                 }
             }
@@ -248,11 +249,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 }
                 return most;
             };
-            if (__any(weigh() > 32768.f)) {
+            if (__any(weigh() > 32768.f) || sized) {
                 float now = kNothing;
                 score(0.f);
 #pragma unroll
-                for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(vs[e]));
+                for (int e = 0; e < 8; e++) now = fmaxf(now, y[e] + __builtin_amdgcn_logf(size_of(vs[e], vm[e])));
                 now = fmaxf(now, __shfl_xor(now, 16));
                 now = fmaxf(now, __shfl_xor(now, 32));
                 now = fmaxf(top, ceilf(now) - 8.f);  // (whole numbers: what is kept is kept exactly)

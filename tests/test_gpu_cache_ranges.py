@@ -1,0 +1,119 @@
+"""Attention over the paged cache at the ends of what it accepts, against its definition in 64 bits on what the pages hold: both kernels,
+contexts that one workgroup has and that several share."""
+import numpy as np
+import pytest
+
+import cache_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+TYPES = ["f32", "f16", "bf16"]
+HALF_ULP = {"f32": 2.0 ** -24, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+# relative rounding of a weight before it meets the values' codes
+WEIGHT = {"f32": 2.0 ** -21, "f16": 2.0 ** -11, "bf16": 2.0 ** -11}
+# new tokens, context, and whether the page table is far wider than it (which brings the kernel for many rows)
+FORMS = {"few rows": (2, 300, False), "few rows, shared": (2, 1500, False), "many rows": (80, 120, False), "many rows, shared": (80, 700, True)}
+
+
+@pytest.fixture(scope="module")
+def bf():
+    import paper_2207_14696_amd as m
+    m.load_library()
+    return m
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch as t
+    return t
+
+
+def _dtype(torch, name):
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def _decoded(raw, table, length, bits, heads, d, ps):
+    """Keys and values [length, heads, d] in 64 bits, from the documented layout."""
+    rb = ref.row_bytes(d, bits)
+    blocks = raw[table].reshape(-1, heads, ps * (2 * rb + 16))
+    floats = np.ascontiguousarray(blocks[:, :, 2 * ps * rb:]).view(np.float32).reshape(-1, heads, 4, ps).astype(np.float64)
+    out = []
+    for which in (0, 1):
+        codes = blocks[:, :, which * ps * rb:(which + 1) * ps * rb].reshape(-1, heads, ps, rb)
+        if bits == 4:
+            codes = np.stack([codes & 15, codes >> 4], -1).reshape(*codes.shape[:3], 2 * rb)
+        x = floats[:, :, 2 * which + 1, :, None] + codes[..., :d].astype(np.float64) * floats[:, :, 2 * which, :, None]
+        out.append(x.transpose(0, 2, 1, 3).reshape(-1, heads, d)[:length])
+    return out
+
+
+class Context:
+    """One sequence of `length` cached tokens, the last n of which ask; keys and values [length, heads, d] in 32 bits."""
+
+    def __init__(self, bf, torch, bits, keys, values, n, ps=64, wide=False):
+        self.torch, self.bits, self.n, self.ps = torch, bits, n, ps
+        self.length, self.heads, self.d = keys.shape
+        self.c = bf.PagedCache(bits, self.heads, self.d, ps)
+        held = -(-self.length // ps)
+        table = np.random.default_rng(0).permutation(held + 2)[:held].astype(np.int32)
+        self.tables = torch.full((1, 2 ** 20 // ps if wide else held), -7, dtype=torch.int32, device="cuda")
+        self.tables[0, :held] = torch.from_numpy(table).cuda()
+        self.lengths = torch.tensor([self.length], dtype=torch.int64, device="cuda")
+        self.pages = self.c.new_pages(held + 2)
+        self.c.write(self.pages, torch.from_numpy(keys.astype(np.float32)).cuda(), torch.from_numpy(values.astype(np.float32)).cuda(),
+                     self.tables, self.lengths)
+        self.keys, self.values = _decoded(self.pages.cpu().numpy(), table, self.length, bits, self.heads, self.d, ps)
+
+    def check(self, q, dtype, scale=None, cap=0.0, scores=2.0 ** -19, weights=None):
+        """q [n, query heads, d], rounded to dtype here; against the definition, to `scores` (of the largest sum of |q| |k|: products and sums in 32
+        bits, which a weight and the weights' sum are off by) and `weights` (twice a weight's own rounding), both of the head's largest
+        value, and the result's rounding."""
+        torch, group = self.torch, q.shape[1] // self.heads
+        scale = 1.0 / np.sqrt(self.d) if scale is None else scale
+        weights = 2 * WEIGHT[dtype] if weights is None else weights
+        tq = torch.from_numpy(q.astype(np.float32)).cuda().to(_dtype(torch, dtype))
+        got = self.c.attend(self.pages, tq, self.tables, self.lengths, scale=scale, softcap=cap).float().cpu().numpy().astype(np.float64)
+        hq = tq.float().cpu().numpy().astype(np.float64)
+        # (the definition takes the softcap as a 32-bit number, as the entry point does)
+        want = ref.attend(hq, self.keys, self.values, len(q), self.length, scale, float(np.float32(cap)))
+        assert np.isfinite(got).all()
+        live = max(0, len(q) - self.length)   # (the first of those that see something)
+        for h in range(q.shape[1]):
+            k, v = self.keys[:, h // group], self.values[:, h // group]
+            biggest = (np.abs(hq[live:, h]) @ np.abs(k).T).max() * abs(scale)
+            bound = np.abs(v).max() * (scores * biggest + weights) + HALF_ULP[dtype] * np.abs(want[:, h]) + (2.0 ** -25 if dtype == "f16" else 0)
+            err = np.abs(got[:, h] - want[:, h])
+            assert (err <= bound).all(), (h, (err / np.maximum(bound, 1e-300)).max(), np.argwhere(err > bound)[:3])
+        return got, want
+
+
+def _normal(seed, *shape):
+    return np.random.default_rng(seed).standard_normal(shape)
+
+
+# ------------------------------------------------------------------ values of any size
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,constant", [("f16", 8192.0), ("f16", 60000.0), ("bf16", 1e7), ("f32", -1e7), ("bf16", 3e38), ("f32", 3e38), ("f32", 1e-20),
+                                            ("f32", 1e-35), ("f16", 0.0)])
+@pytest.mark.parametrize("bits,d,mixed", [(8, 64, False), (4, 1, False), (4, 100, True), (8, 256, True), (4, 128, False)])
+def test_attend_over_value_rows_of_one_value(bf, torch, form, bits, d, mixed, dtype, constant):
+    # rows whose columns are all alike have scale 0: all of a head's, or every other one beside ordinary rows
+    n, m, wide = FORMS[form]
+    values = np.full((m, 2, d), constant)
+    if mixed:
+        values[::2] = _normal(1, -(-m // 2), 2, d)
+    if d > 1:
+        values[:, 1] *= np.linspace(0.5, 1, m)[:, None]   # another value in each row of the second head
+    context = Context(bf, torch, bits, _normal(2, m, 2, d), values, n, wide=wide)
+    context.check(_normal(3, n, 4, d), dtype)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,size", [("bf16", 1e-25), ("f32", 1e-27), ("bf16", 1e-29), ("f32", 1e-29), ("f32", 1e-20), ("f32", 1e30), ("bf16", 1e37)])
+@pytest.mark.parametrize("bits,d", [(8, 64), (4, 128), (8, 256)])
+def test_attend_over_values_very_small_and_very_large(bf, torch, form, bits, d, dtype, size):
+    n, m, wide = FORMS[form]
+    context = Context(bf, torch, bits, _normal(2, m, 2, d), size * _normal(1, m, 2, d), n, wide=wide)
+    # (weights of the smallest values are fp16 numbers below the normal ones: to 2^-9 and better)
+    context.check(_normal(3, n, 4, d), dtype, weights=2 * max(WEIGHT[dtype], 2.0 ** -9) if size < 1e-28 else None)
