@@ -26,8 +26,7 @@ struct ChunkShape {
     static constexpr int KEYS = TOK / 16 * KS, VALUES = TOK / 32 * VT;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries); MODE: 1: scores are biased by
-// distance, 2: capped (and biased)
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries)
 template <int BITS, int DP, int NP, int NT, int MODE>
 __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chunk_kernel(AttendCall a, AttendPlan plan) {
     using S = ChunkShape<BITS, DP, NT>;
@@ -197,7 +196,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
             }
             __syncthreads();
         }
-        const float cap = a.softcap * kLog2e;
+        const Cap cap = cap_of(a);
         // first and last position of the wave's queries
         const int wend = wrow0 + 16 * NT < row0 + nrows ? wrow0 + 16 * NT : row0 + nrows;
         const int wfirst = v.len - v.n + wrow0 / a.group, wlast = v.len - v.n + (wend - 1) / a.group;
@@ -258,18 +257,20 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 float p[NT][4], pw[NT][4];
                 // scores less `ref`, -infinity where the row does not see the position
                 auto score = [&](int n, float ref, float(&y)[4]) {
-                    if constexpr (MODE == 0) {
+                    if constexpr (MODE == kPlain) {
 #pragma unroll
                         for (int i = 0; i < 4; i++) y[i] = fmaf(ks[i], acc[n][j][i], fmaf(km[i], qsum[n], -ref));
-                    } else if constexpr (MODE == 1) {
+                    } else if constexpr (MODE == kBiased) {
                         const float from = fmaf(slope[n], (float)(at4 - pos[n]), -ref);
 #pragma unroll
                         for (int i = 0; i < 4; i++) y[i] = fmaf(ks[i], acc[n][j][i], fmaf(km[i], qsum[n], fmaf(slope[n], (float)i, from)));
                     } else {
                         const float from = fmaf(slope[n], (float)(at4 - pos[n]), -ref);
 #pragma unroll
-                        for (int i = 0; i < 4; i++)
-                            y[i] = capped(fmaf(ks[i], acc[n][j][i], km[i] * qsum[n]), cap) + fmaf(slope[n], (float)i, from);
+                        for (int i = 0; i < 4; i++) y[i] = fmaf(ks[i], acc[n][j][i], km[i] * qsum[n]);
+                        cap_all<MODE == kCappedFirst>(y, cap);
+#pragma unroll
+                        for (int i = 0; i < 4; i++) y[i] += fmaf(slope[n], (float)i, from);
                     }
                     if (!whole) {
                         const uint32_t bits = here(seen[n]);

@@ -8,9 +8,12 @@ template <int BITS, int DP, int NP>
 hipError_t attend_chunk_one(const AttendCall &a, const AttendPlan &p) {
     constexpr int kNT = chunk_tiles(DP, NP);
     constexpr size_t lds = chunk_lds<BITS, DP, kNT>();
-    auto kernel = a.softcap > 0.f ? attend_chunk_kernel<BITS, DP, NP, kNT, 2>
-                  : a.slopes      ? attend_chunk_kernel<BITS, DP, NP, kNT, 1>
-                                  : attend_chunk_kernel<BITS, DP, NP, kNT, 0>;
+    const int mode = mode_of(a);
+    auto kernel = mode == kCapped  ? attend_chunk_kernel<BITS, DP, NP, kNT, kCapped>
+                  : mode == kBiased ? attend_chunk_kernel<BITS, DP, NP, kNT, kBiased>
+                                    : attend_chunk_kernel<BITS, DP, NP, kNT, kPlain>;
+    if constexpr (NP == 1)
+        if (mode == kCappedFirst) kernel = attend_chunk_kernel<BITS, DP, NP, kNT, kCappedFirst>;
     if (lds > 64 * 1024) {  // (what a launch may have without being asked)
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
     }

@@ -6,9 +6,12 @@ namespace {
 
 template <int BITS, int DP, int NP, int WP>
 void by_mode(const AttendCall &a, const AttendPlan &p) {
-    auto kernel = a.softcap > 0.f ? attend_rows_kernel<BITS, DP, NP, WP, 2>
-                  : a.slopes      ? attend_rows_kernel<BITS, DP, NP, WP, 1>
-                                  : attend_rows_kernel<BITS, DP, NP, WP, 0>;
+    const int mode = mode_of(a);
+    auto kernel = mode == kCapped  ? attend_rows_kernel<BITS, DP, NP, WP, kCapped>
+                  : mode == kBiased ? attend_rows_kernel<BITS, DP, NP, WP, kBiased>
+                                    : attend_rows_kernel<BITS, DP, NP, WP, kPlain>;
+    if constexpr (NP == 1)
+        if (mode == kCappedFirst) kernel = attend_rows_kernel<BITS, DP, NP, WP, kCappedFirst>;
     kernel<<<p.nw, 256, 0, a.s>>>(a, p);
 }
 

@@ -28,7 +28,7 @@ struct RowLanes {
 
 // NP: fp16 pieces of a query element (2 for 32-bit queries); WP: of a weight.  One is enough where the result is rounded to
 // bf16 (2^-9; a weight's one piece 2^-12, the second costs 8 % of long contexts in 4 bits); an fp16 result would be 1.6 times as far off
-// with one, and the second costs it 1 %.  MODE: 1: scores are biased by distance, 2: capped (and biased)
+// with one, and the second costs it 1 %.
 template <int BITS, int DP, int NP, int WP, int MODE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
     using L = RowLanes<BITS, DP>;
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             qsum *= f / kUnit<NP>;
         }
         const float slope = MODE && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
-        const float cap = a.softcap * kLog2e;
+        const Cap cap = cap_of(a);
 
         float top = kNothing, total = 0.f, mins = 0.f;  // mins: what is not in the products with the codes
         float4v o[L::VT];
@@ -226,11 +226,16 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             // scores less `ref`, -infinity where the row does not see the position
             auto score = [&](float ref) {
                 const float from = MODE ? fmaf(slope, (float)(base + 4 * g - pos), -ref) : -ref;
+                if constexpr (MODE >= kCappedFirst) {
+#pragma unroll
+                    for (int e = 0; e < 8; e++) y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum);
+                    cap_all<MODE == kCappedFirst>(y, cap);
+                }
 #pragma unroll
                 for (int e = 0; e < 8; e++) {
                     const float bias = MODE ? fmaf(slope, (float)(16 * (e / 4) + e % 4), from) : from;
-                    if constexpr (MODE < 2) y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, bias));
-                    else y[e] = capped(fmaf(ks[e], f * acc[e / 4][e % 4], km[e] * qsum), cap) + bias;
+                    if constexpr (MODE < kCappedFirst) y[e] = fmaf(ks[e], f * acc[e / 4][e % 4], fmaf(km[e], qsum, bias));
+                    else y[e] += bias;
                 }
                 if (!whole) {
                     const uint32_t bits = here(seen);

@@ -117,3 +117,27 @@ def test_attend_over_values_very_small_and_very_large(bf, torch, form, bits, d, 
     context = Context(bf, torch, bits, _normal(2, m, 2, d), size * _normal(1, m, 2, d), n, wide=wide)
     # (weights of the smallest values are fp16 numbers below the normal ones: to 2^-9 and better)
     context.check(_normal(3, n, 4, d), dtype, weights=2 * max(WEIGHT[dtype], 2.0 ** -9) if size < 1e-28 else None)
+
+
+# ------------------------------------------------------------------ caps of any size
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("cap", [1e-38, 1e-30, 0.02, 5.0, 30.0, 50.0, 1e3, 1e4, 1e6, 1e9, 1e30, 3e38])
+@pytest.mark.parametrize("dtype,bits,d", [("f32", 8, 64), ("f32", 4, 128), ("f16", 4, 64), ("bf16", 8, 256)])
+def test_attend_with_caps_of_any_size(bf, torch, form, cap, dtype, bits, d):
+    n, m, wide = FORMS[form]
+    context = Context(bf, torch, bits, _normal(2, m, 2, d), _normal(1, m, 2, d), n, wide=wide)
+    # scores of a standard deviation of 4; the cap's own error, a few 2^-24 of the score, is within what the sums are allowed
+    context.check(4 * _normal(3, n, 4, d), dtype, cap=cap)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("cap", [0.0, 30.0, 50.0, 1e3])
+@pytest.mark.parametrize("bits,d", [(8, 64), (4, 64), (8, 100), (4, 128), (8, 256)])
+def test_32_bit_queries_keep_32_bits(bf, torch, form, cap, bits, d):
+    # a query's pieces are off by 2^-23 of it, sums of products by a few 2^-24 of them, weights by 2^-23, in directions of their own: of scores of
+    # a standard deviation of 2 that is below 2^-20 in the mean, and of the result no more than twice as much
+    n, m, wide = FORMS[form]
+    context = Context(bf, torch, bits, _normal(2, m, 2, d), _normal(1, m, 2, d), n, wide=wide)
+    got, want = context.check(2 * _normal(3, n, 4, d), "f32", cap=cap)
+    assert np.linalg.norm(got - want) <= 2.0 ** -19 * np.linalg.norm(want)
