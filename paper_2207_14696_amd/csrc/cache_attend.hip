@@ -147,7 +147,8 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     const int dp = a.c.d <= 64 ? 64 : a.c.d <= 128 ? 128 : 256, bits = h->spec.bits;
     const int np = a.dtype == BIFEAT_F32 ? 2 : 1;
     const int64_t width = a.b.width << a.c.ps_log2;
-    auto units_of = [&](int R, int tok) { return (int64_t)items_of(a, R) * a.c.heads * ((width + tok - 1) / tok); };
+    // (an item has one unit at least, also over tables that have no room: its zeros)
+    auto units_of = [&](int R, int tok) { return (int64_t)items_of(a, R) * a.c.heads * std::max<int64_t>(1, (width + tok - 1) / tok); };
     // The kernel for many rows makes operands once for 64 or 128 rows; that for few, for 16, starts and joins sooner.  Few: up to 64
     // rows of 64 columns a sequence and head on average (64 sequences of 4096, 12 heads: 294 us, the other kernel 300; 128
     // rows 577 and 310), 32 of 128 (8 heads: 193 and 207; 48 rows 286 and 235), 16 of 256 (4 heads: 20 rows 195 and 161; 32 where a

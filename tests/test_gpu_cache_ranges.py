@@ -141,3 +141,21 @@ def test_32_bit_queries_keep_32_bits(bf, torch, form, cap, bits, d):
     context = Context(bf, torch, bits, _normal(2, m, 2, d), _normal(1, m, 2, d), n, wide=wide)
     got, want = context.check(2 * _normal(3, n, 4, d), "f32", cap=cap)
     assert np.linalg.norm(got - want) <= 2.0 ** -19 * np.linalg.norm(want)
+
+
+# ------------------------------------------------------------------ nothing to see
+
+@pytest.mark.parametrize("d,n,ragged", [(64, 1, False), (256, 1, False), (128, 3, True), (64, 100, False), (256, 40, True)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_tables_without_room_leave_zeros(bf, torch, d, n, ragged, dtype):
+    B, heads = 300, 8    # more items than run at a time
+    c = bf.PagedCache(8, heads, d, 16)
+    tables, lengths = torch.empty(B, 0, dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int64, device="cuda")
+    indptr = n * torch.arange(B + 1, device="cuda") if ragged else None
+    out = torch.full((B * n, heads, d), 7.0, device="cuda", dtype=_dtype(torch, dtype))
+    q = torch.randn(B * n, heads, d, device="cuda").to(out.dtype)
+    pages = c.new_pages(1)
+    c.attend(pages, q, tables, lengths, indptr, out=out)
+    assert not out.any()
+    c.write(pages, q, q, tables, lengths, indptr)
+    assert not any(x.any() for x in c.read(pages, tables, lengths, B * n, indptr))
