@@ -350,6 +350,7 @@ __device__ inline void floats_of(const Queries8<E> &q, bool half, float (&x)[8])
         else x[i] = half ? to_float(Half16{q.v[i]}) : to_float(Brain16{q.v[i]});
     }
 }
+// (only of queries that see something: the others may hold anything)
 __device__ inline float largest_finite(float most, const float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);

@@ -164,13 +164,17 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
             const bool half = a.dtype == BIFEAT_F16;
             float big = 0.f;
 #pragma unroll
-            for (int n = 0; n < NT; n++)
+            for (int n = 0; n < NT; n++) {
+                float its = 0.f;
 #pragma unroll
                 for (int c = 0; c < S::KS; c++) {
                     float x[8];
                     floats_of(*reinterpret_cast<const Queries8<E> *>(own + 16 * n * kStride + 8 * c), half, x);
-                    big = largest_finite(big, x);
+                    its = largest_finite(its, x);
                 }
+                const int row = wrow0 + 16 * n + (at_lane & 15);
+                if (v.len - v.n + row / a.group >= 0) big = fmaxf(big, its);
+            }
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
             if (lane == 0) tops[wave] = any_row ? big : 0.f;

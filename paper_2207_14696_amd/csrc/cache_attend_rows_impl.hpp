@@ -154,6 +154,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                 floats_of(raw[c], half, x);
                 big = largest_finite(big, x);
             }
+            if (pos < 0) big = 0.f;
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
             const float up = power_to(big, 14);

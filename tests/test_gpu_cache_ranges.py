@@ -159,3 +159,15 @@ def test_tables_without_room_leave_zeros(bf, torch, d, n, ragged, dtype):
     assert not out.any()
     c.write(pages, q, q, tables, lengths, indptr)
     assert not any(x.any() for x in c.read(pages, tables, lengths, B * n, indptr))
+
+
+@pytest.mark.parametrize("n,m,wide", [(6, 3, False), (80, 70, True), (80, 70, False)])
+@pytest.mark.parametrize("dtype,garbage", [("bf16", 1e30), ("f32", 1e30), ("f16", 65504.0), ("f32", 3e38), ("bf16", float("nan"))])
+@pytest.mark.parametrize("bits,d", [(8, 64), (4, 100), (8, 256)])
+def test_queries_before_the_beginning_may_hold_anything(bf, torch, n, m, wide, dtype, garbage, bits, d):
+    context = Context(bf, torch, bits, _normal(2, m, 2, d), _normal(1, m, 2, d), n, wide=wide)
+    q = _normal(3, n, 4, d)
+    q[:n - m] = garbage
+    with np.errstate(invalid="ignore"):
+        got, _ = context.check(q, dtype)
+    assert not got[:n - m].any()
