@@ -469,7 +469,8 @@ int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_ca
 /* The three calls only enqueue kernels on `stream`.  tokens = 0 is a no-op.  `dtype`
  * (BIFEAT_F32, _F16, _BF16) is the type of k and v, of the arrays read into, of q and out.
  * k, v outputs of read: DEVICE [tokens][heads][head_dim]; out: DEVICE
- * [tokens][query_heads][head_dim]; query_heads a multiple of heads.  Calls on one handle
+ * [tokens][query_heads][head_dim]; query_heads a multiple of heads, sequences * heads at
+ * most 2^30 for attend (BIFEAT_EINVAL).  Calls on one handle
  * that overlap in time share attend's workspace and must not. */
 int bifeat_cache_write(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
                        const bifeat_head_rows *k, const bifeat_head_rows *v, int32_t dtype, void *stream);

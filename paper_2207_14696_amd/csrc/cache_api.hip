@@ -144,6 +144,7 @@ int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages
                         void *stream) {
     if (!c || query_heads < 1 || query_heads > 65536 || query_heads % c->spec.heads) return BIFEAT_EINVAL;
     if (int rc = common(c, pages, num_pages, batch, query_heads, dtype)) return rc;
+    if (batch->sequences > (1 << 30) / c->spec.heads) return BIFEAT_EINVAL;  // (items, which empty sequences have numbers for too, are ints)
     if (!options || !isfinite(options->scale) || !(options->softcap >= 0.f) || !isfinite(options->softcap) || options->window < 0 ||
         (uintptr_t)options->prefix % 8 || (uintptr_t)options->slopes % 4)
         return BIFEAT_EINVAL;

@@ -113,7 +113,7 @@ void launch_join(const AttendCall &a, const AttendPlan &p, int dp, int rows) {
     else attend_join_kernel<R, 256, WAVES><<<grid, 256, 0, a.s>>>(a, p);
 }
 
-// numbers of a head's items, an upper bound where the batch is ragged
+// numbers of a head's items, an upper bound where the batch is ragged (times heads within an int: see bifeat_cache_attend)
 int items_of(const AttendCall &a, int R) {
     if (a.b.indptr) return (int)(a.b.tokens * a.group / R) + a.b.B;
     return a.b.B * ((a.b.n * a.group + R - 1) / R);
@@ -172,7 +172,7 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     p.partial = split ? h->d_partial : nullptr;
     p.begins = split ? reinterpret_cast<PartOf *>(h->d_partial + kPartialFloats) : nullptr;
     p.least = !chunk ? 2 : np == 2 ? 1 : 4;
-    p.nw = split ? workgroups_of(units, p.least, most) : (int)all;
+    p.nw = split ? workgroups_of(units, p.least, most) : (int)all;  // (bifeat_cache_attend has seen to it that they fit an int)
     const int rows = a.b.indptr ? R : std::min(R, a.b.n * a.group);
     if (chunk) {
         if (hipError_t e = launch_attend_chunk(a, p, bits, dp)) return e;

@@ -155,12 +155,14 @@ template <int R, int TOK>
 __device__ inline void locate(const AttendCall &a, const AttendPlan &p, int w, int *start, int *end, int *head, Place *at, int *sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
     if (!p.partial) {
+        w += (int)(gridDim.x * blockIdx.y);  // (see grid_of)
+        *start = *end = 0;
+        if (w >= p.items * a.c.heads) return;
         const int item = w % p.items;
         at->seq = uniform(sequence_of_item<R>(a, item));
         at->rt = uniform(item - first_item<R>(a, at->seq));
         at->unit = 0;
         *head = w / p.items;
-        *start = 0;
         *end = uniform(view_of<R, TOK>(a, at->seq, at->rt).units);
         return;
     }
@@ -468,6 +470,12 @@ __device__ inline void cap_all(float (&x)[N], const Cap &c) {
     if (__any(!(most < 0.6f)))
 #pragma unroll
         for (int i = 0; i < N; i++) x[i] = fabsf(u[i]) < 0.6f ? x[i] : first(u[i]);
+}
+
+// p.nw workgroups, in rows: a launch has fewer than 2^32 threads along an axis, 2^24 workgroups
+inline dim3 grid_of(const AttendPlan &p) {
+    const unsigned x = p.nw < 1 << 23 ? p.nw : 1 << 23;
+    return dim3(x, (p.nw + x - 1) / x);
 }
 
 void launch_attend_rows(const AttendCall &a, const AttendPlan &p, int bits, int dp);

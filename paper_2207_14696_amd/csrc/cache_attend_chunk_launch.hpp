@@ -17,7 +17,7 @@ hipError_t attend_chunk_one(const AttendCall &a, const AttendPlan &p) {
     if (lds > 64 * 1024) {  // (what a launch may have without being asked)
         if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds)) return e;
     }
-    kernel<<<p.nw, 256, lds, a.s>>>(a, p);
+    kernel<<<grid_of(p), 256, lds, a.s>>>(a, p);
     return hipSuccess;
 }
 

@@ -12,7 +12,7 @@ void by_mode(const AttendCall &a, const AttendPlan &p) {
                                     : attend_rows_kernel<BITS, DP, NP, WP, kPlain>;
     if constexpr (NP == 1)
         if (mode == kCappedFirst) kernel = attend_rows_kernel<BITS, DP, NP, WP, kCappedFirst>;
-    kernel<<<p.nw, 256, 0, a.s>>>(a, p);
+    kernel<<<grid_of(p), 256, 0, a.s>>>(a, p);
 }
 
 template <int BITS, int DP>

@@ -119,6 +119,22 @@ def test_reference_attention_is_softmax_attention():
     assert np.allclose(ref.attend(q, k, v, n, m, 0.4, window=1), np.repeat(v[m - n:], G, 1))
 
 
+def test_attend_refuses_more_items_than_it_can_number(bf):
+    from paper_2207_14696_amd.binding import _CAttendOptions, _CCacheBatch, _CHeadRows
+    lib = bf.load_library()
+    for heads in (1, 2, 1024):
+        c = bf.PagedCache(8, heads, 64, 16)
+
+        def attend(sequences, tokens):
+            b = _CCacheBatch(tables=16, table_width=4, lengths=16, indptr=16, sequences=sequences, tokens=tokens)
+            return lib.bifeat_cache_attend(c._h, 16, 9, C.byref(b), C.byref(_CHeadRows(16, 64, 64)), heads, 0,
+                                           C.byref(_CAttendOptions(1.0, 0.0, 0, None, None)), 16, None)
+
+        for tokens in (0, 1):
+            assert attend(2 ** 30 // heads + 1, tokens) == -1
+        assert attend(2 ** 30 // heads, 0) == 0
+
+
 def _kernels_of(library):
     """(name, vector registers spilled) of the kernels in the library's code objects, from the notes that the compiler left."""
     import re

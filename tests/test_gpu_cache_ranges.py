@@ -171,3 +171,21 @@ def test_queries_before_the_beginning_may_hold_anything(bf, torch, n, m, wide, d
     with np.errstate(invalid="ignore"):
         got, _ = context.check(q, dtype)
     assert not got[:n - m].any()
+
+
+def test_more_workgroups_than_a_launch_has_along_an_axis(bf, torch):
+    # 2.1 million sequences of 8 heads, whose page tables have room for more units than are dealt: a workgroup each.  All look at the
+    # same token, and answer with its values.
+    B, heads, d, ps = 2 ** 21 + 3, 8, 8, 1024
+    c = bf.PagedCache(8, heads, d, ps)
+    tables = torch.zeros(B, 16, dtype=torch.int32, device="cuda")
+    lengths = torch.ones(B, dtype=torch.int64, device="cuda")
+    pages = c.new_pages(1)
+    k = torch.randn(1, heads, d, device="cuda")
+    c.write(pages, k, k, tables[:1], lengths[:1])
+    values = c.read(pages, tables[:1], lengths[:1], 1, dtype=torch.bfloat16)[1]
+    q = torch.randn(B, heads, d, device="cuda", dtype=torch.bfloat16)
+    out = torch.full_like(q, 9.0)
+    c.attend(pages, q, tables, lengths, out=out)
+    # a weight of 1 in one fp16 piece; the result's rounding
+    assert (out - values).abs().max() <= 2.0 ** -7 * values.abs().max()
