@@ -412,8 +412,11 @@ typedef struct {
     int32_t page_size; /* tokens a page: 16, 32, 64, ... 1024 */
 } bifeat_cache_spec;
 
-/* Opaque: the spec, options, and the workspace of bifeat_cache_attend (device memory,
- * allocated by the first call that needs it, on the device current then). */
+/* Opaque: the spec, options, and the workspaces of bifeat_cache_attend (device memory,
+ * 68 MB each): one for each stream, allocated by the first call on it that needs one, and
+ * one for the calls that are captured, allocated with the first of those.  So calls on
+ * different streams may overlap, and threads may share a handle; graphs captured with one
+ * handle must not be replayed at the same time, nor after the handle is destroyed. */
 typedef struct bifeat_cache bifeat_cache;
 
 /* The sequences of one call and which of their tokens it is about: the last n_b of
@@ -459,9 +462,9 @@ int64_t bifeat_cache_page_bytes(const bifeat_cache *c);
 /* "validate" = 1: every call first checks its batch on the GPU, synchronises `stream` and
  * returns BIFEAT_EINVAL without launching anything else when the contract is broken. */
 int bifeat_cache_set_option(bifeat_cache *c, const char *name, int value);
-/* Allocates the workspace of bifeat_cache_attend ahead of time.  While a stream is
- * captured nothing is allocated: a call that finds no workspace then does not split
- * contexts over workgroups. */
+/* Allocates the workspaces of bifeat_cache_attend on `stream` and of captured calls ahead of
+ * time.  While a stream is captured nothing is allocated: a call that finds no workspace
+ * then does not split contexts over workgroups. */
 int bifeat_cache_reserve(bifeat_cache *c, void *stream);
 /* The batch contract on its own: BIFEAT_OK or BIFEAT_EINVAL; synchronises `stream`. */
 int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_cache_batch *batch, void *stream);
@@ -470,8 +473,8 @@ int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_ca
  * (BIFEAT_F32, _F16, _BF16) is the type of k and v, of the arrays read into, of q and out.
  * k, v outputs of read: DEVICE [tokens][heads][head_dim]; out: DEVICE
  * [tokens][query_heads][head_dim]; query_heads a multiple of heads, sequences * heads at
- * most 2^30 for attend (BIFEAT_EINVAL).  Calls on one handle
- * that overlap in time share attend's workspace and must not. */
+ * most 2^30 for attend (BIFEAT_EINVAL).  The arrays and pages are of the device that is
+ * current, which `stream` is of. */
 int bifeat_cache_write(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
                        const bifeat_head_rows *k, const bifeat_head_rows *v, int32_t dtype, void *stream);
 int bifeat_cache_read(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,

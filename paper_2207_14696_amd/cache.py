@@ -40,7 +40,11 @@ class PagedCache:
     All calls take a batch: ``tables`` int32 [B, width], the pages of each sequence; ``lengths`` int64
     [B], its tokens, the call's own among them; ``indptr`` int64 [B + 1] or None, which rows of the
     call's arrays are whose (None: as many for every sequence).  The call is about the last of each
-    sequence's tokens.  Work goes to the current stream; nothing is synchronised."""
+    sequence's tokens.  Work goes to the current stream; nothing is synchronised.
+
+    One object serves any streams and threads: ``attend`` has a workspace (68 MB) for each stream that it
+    is called on, and one for captured calls (``reserve``).  CUDA graphs captured with one object must not be
+    replayed at the same time, nor outlive it.  All tensors are of the current device."""
 
     def __init__(self, bits: int, heads: int, head_dim: int, page_size: int = 64):
         self._lib = load_library()
@@ -71,11 +75,14 @@ class PagedCache:
         _check(self._lib.bifeat_cache_set_option(self._h, name.encode(), int(value)))
 
     def reserve(self) -> None:
-        """The workspace of ``attend`` ahead of time (before a stream capture)."""
+        """The workspaces of ``attend`` on the current stream and of captured calls ahead of time (before a capture)."""
         _check(self._lib.bifeat_cache_reserve(self._h, _stream()))
 
-    def _pages(self, pages):
+    def _pages(self, pages, *others):
         import torch
+        if not pages.is_cuda or pages.device.index != torch.cuda.current_device() or \
+                any(t is not None and t.device != pages.device for t in others):
+            raise ValueError("pages and the other tensors must be on the current CUDA device")
         if pages.dim() != 2 or pages.shape[1] != self.page_bytes:
             raise ValueError(f"pages must be [pages, {self.page_bytes}]")
         return _dev_ptr(pages, (torch.uint8,)), pages.shape[0]
@@ -95,7 +102,7 @@ class PagedCache:
         """``bifeat_cache_check``: whether the batch is one that the calls may be given."""
         if tokens is None:
             tokens = int(indptr[-1]) if indptr is not None else tables.shape[0]
-        rc = self._lib.bifeat_cache_check(self._h, self._pages(pages)[1], C.byref(self._batch(tables, lengths, indptr, tokens)),
+        rc = self._lib.bifeat_cache_check(self._h, self._pages(pages, tables, lengths, indptr)[1], C.byref(self._batch(tables, lengths, indptr, tokens)),
                                           _stream())
         if rc == EINVAL:
             return False
@@ -111,7 +118,7 @@ class PagedCache:
         rows = [_head_rows(t, self.heads, self.head_dim, name) for t, name in ((k, "k"), (v, "v"))]
         if k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must be alike")
-        ptr, count = self._pages(pages)
+        ptr, count = self._pages(pages, k, v, tables, lengths, indptr)
         _check(self._lib.bifeat_cache_write(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, k.shape[0])),
                                             C.byref(rows[0]), C.byref(rows[1]), _type(k.dtype), _stream()))
 
@@ -131,7 +138,7 @@ class PagedCache:
             out = (torch.empty(shape, dtype=dtype, device=pages.device), torch.empty(shape, dtype=dtype, device=pages.device))
         elif any(t.shape != shape for t in out) or out[0].dtype != out[1].dtype or dtype not in (None, out[0].dtype):
             raise ValueError("out must be two [tokens, heads, head_dim] of one dtype")
-        ptr, count = self._pages(pages)
+        ptr, count = self._pages(pages, *out, tables, lengths, indptr)
         _check(self._lib.bifeat_cache_read(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, tokens)),
                                            _dev_ptr(out[0]), _dev_ptr(out[1]), _type(out[0].dtype), _stream()))
         return out
@@ -163,7 +170,7 @@ class PagedCache:
             raise ValueError("prefix must be [B]")
         if slopes is not None and slopes.shape != (heads,):
             raise ValueError("slopes must be [query heads]")
-        ptr, count = self._pages(pages)
+        ptr, count = self._pages(pages, q, out, tables, lengths, indptr, prefix, slopes)
         options = _b._CAttendOptions(scale, softcap, window,
                                      _dev_ptr(prefix, (torch.int64,)), _dev_ptr(slopes, (torch.float32,)))
         _check(self._lib.bifeat_cache_attend(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, q.shape[0])),

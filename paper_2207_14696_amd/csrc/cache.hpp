@@ -1,6 +1,7 @@
 // The paged cache: what its translation units share.
 #pragma once
 
+#include <mutex>
 #include <type_traits>
 
 #include "common.hpp"
@@ -11,8 +12,17 @@ struct bifeat_cache {
     int64_t head_bytes = 0;  // bytes of a page's block of one head
     int64_t page_bytes = 0;
     int opt_validate = 0;
-    // what bifeat_cache_attend leaves of contexts that several workgroups share (see cache_attend.hpp)
-    float *d_partial = nullptr;
+    // what bifeat_cache_attend leaves of contexts that several workgroups share (see cache_attend.hpp): each stream has its own, so that calls on
+    // different streams do not meet, and captured calls have one, whichever stream they are replayed on
+    struct Workspace {
+        int device;
+        hipStream_t stream;
+        bool captured;  // of calls that are being captured; stream is of no account
+        float *partial;
+        Workspace *next;
+    };
+    Workspace *workspaces = nullptr;
+    std::mutex mutex;  // of the list, and of a call's kernel and join: threads that share a stream enqueue them in turn
 };
 
 namespace bf {
@@ -133,7 +143,7 @@ hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const He
 hipError_t launch_cache_read(const CachePages &c, const CacheBatch &b, void *k, void *v, int bits, int dtype, hipStream_t s);
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a);
 void launch_cache_check(const CacheBatch &b, int ps_log2, int64_t num_pages, int32_t *d_bad, hipStream_t s);
-// whether the workspace is there; allocates it unless `s` is being captured
-bool ensure_partial(bifeat_cache *h, hipStream_t s);
+// The workspace of calls on `s`, and that of captured calls; allocated unless `s` is being captured.  Null: there is none.  The handle's mutex is held.
+float *workspace_of(bifeat_cache *h, hipStream_t s);
 
 }  // namespace bf

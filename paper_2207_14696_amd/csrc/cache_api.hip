@@ -89,7 +89,11 @@ int bifeat_cache_create(const bifeat_cache_spec *spec, bifeat_cache **out) {
 
 void bifeat_cache_destroy(bifeat_cache *c) {
     if (!c) return;
-    if (c->d_partial) (void)hipFree(c->d_partial);
+    while (bifeat_cache::Workspace *w = c->workspaces) {
+        (void)hipFree(w->partial);
+        c->workspaces = w->next;
+        delete w;
+    }
     delete c;
 }
 
@@ -106,7 +110,8 @@ int bifeat_cache_set_option(bifeat_cache *c, const char *name, int value) {
 
 int bifeat_cache_reserve(bifeat_cache *c, void *stream) {
     if (!c) return BIFEAT_EINVAL;
-    return bf::ensure_partial(c, (hipStream_t)stream) ? BIFEAT_OK : bf::record_hip_error(hipErrorOutOfMemory, "bifeat_cache_reserve");
+    const std::lock_guard<std::mutex> lock(c->mutex);
+    return bf::workspace_of(c, (hipStream_t)stream) ? BIFEAT_OK : bf::record_hip_error(hipErrorOutOfMemory, "bifeat_cache_reserve");
 }
 
 int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_cache_batch *batch, void *stream) {

@@ -1,5 +1,6 @@
 // Attention over the paged cache: which kernel, how many workgroups, and the join of what several of them did of one item.
 #include <algorithm>
+#include <new>
 
 #include "cache_attend.hpp"
 
@@ -130,17 +131,33 @@ static hipError_t launch_attend_chunk(const AttendCall &a, const AttendPlan &p, 
     return bits == 8 ? attend_chunk_bits<8>(a, p, dp) : attend_chunk_bits<4>(a, p, dp);
 }
 
-bool ensure_partial(bifeat_cache *h, hipStream_t s) {
-    if (h->d_partial) return true;
+float *workspace_of(bifeat_cache *h, hipStream_t s) {
+    int device = 0;
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    if (hipStreamIsCapturing(s, &status) != hipSuccess || status != hipStreamCaptureStatusNone) return false;
-    void *p = nullptr;
-    if (hipMalloc(&p, sizeof(float) * kPartialFloats + sizeof(PartOf) * rows_workgroups(64)) != hipSuccess) {
+    if (hipGetDevice(&device) != hipSuccess || hipStreamIsCapturing(s, &status) != hipSuccess) {
         (void)hipGetLastError();
-        return false;
+        return nullptr;
     }
-    h->d_partial = (float *)p;
-    return true;
+    const bool capturing = status != hipStreamCaptureStatusNone;
+    auto find = [&](bool captured) -> float * {
+        for (bifeat_cache::Workspace *w = h->workspaces; w; w = w->next)
+            if (w->device == device && w->captured == captured && (captured || w->stream == s)) return w->partial;
+        return nullptr;
+    };
+    float *own = find(capturing);
+    if (own || capturing) return own;
+    for (const bool captured : {true, false}) {
+        if (find(captured)) continue;
+        auto *w = new (std::nothrow) bifeat_cache::Workspace{device, s, captured, nullptr, h->workspaces};
+        if (!w) return nullptr;
+        if (hipMalloc((void **)&w->partial, sizeof(float) * kPartialFloats + sizeof(PartOf) * rows_workgroups(64)) != hipSuccess) {
+            (void)hipGetLastError();
+            delete w;
+            return nullptr;
+        }
+        h->workspaces = w;
+    }
+    return find(false);
 }
 
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
@@ -168,9 +185,14 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     // many rows); 4 rows of 8 sequences on 8 heads of 128: at 512 positions 13.6 us, dealt evenly and joined 16.0; at
     // 1024 19.3 and 16.3.  And calls that find no workspace, or have 2^31 units or more.
     const bool small = width <= (chunk ? 128 : 6 * kRowsTok) && all <= most;
-    const bool split = !small && units <= INT32_MAX && ensure_partial(h, a.s);
-    p.partial = split ? h->d_partial : nullptr;
-    p.begins = split ? reinterpret_cast<PartOf *>(h->d_partial + kPartialFloats) : nullptr;
+    std::unique_lock<std::mutex> lock(h->mutex, std::defer_lock);
+    p.partial = nullptr;
+    if (!small && units <= INT32_MAX) {
+        lock.lock();
+        p.partial = workspace_of(h, a.s);
+    }
+    const bool split = p.partial;
+    p.begins = split ? reinterpret_cast<PartOf *>(p.partial + kPartialFloats) : nullptr;
     p.least = !chunk ? 2 : np == 2 ? 1 : 4;
     p.nw = split ? workgroups_of(units, p.least, most) : (int)all;  // (bifeat_cache_attend has seen to it that they fit an int)
     const int rows = a.b.indptr ? R : std::min(R, a.b.n * a.group);

@@ -31,11 +31,13 @@ using AggregateFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, c
 
 PyObject *g_device = nullptr, *g_stream = nullptr;  // torch._C._cuda_getDevice, ._cuda_getCurrentRawStream
 
-const at::Tensor *tensor(PyObject *o, at::ScalarType a, at::ScalarType b) {
+// `with`: of whose device it has to be
+const at::Tensor *tensor(PyObject *o, at::ScalarType a, at::ScalarType b, const at::Tensor *with = nullptr) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.dim() < 1 || t.layout() != at::kStrided) return nullptr;
     if (!t.unsafeGetTensorImpl()->has_storage() || !t.is_contiguous()) return nullptr;
+    if (with && t.device() != with->device()) return nullptr;
     return t.scalar_type() == a || t.scalar_type() == b ? &t : nullptr;
 }
 
@@ -44,10 +46,14 @@ bool watched() {
            torch::jit::tracer::isTracing();
 }
 
-// the current stream's handle, as binding.py asks for it; false with a Python error set
-bool stream(void **out) {
+// the current stream's handle, as binding.py asks for it; false with a Python error set, or where `on` is not on the current device
+bool stream(void **out, const at::Tensor *on = nullptr) {
     PyObject *device = PyObject_CallNoArgs(g_device);
     if (!device) return false;
+    if (on && PyLong_AsLong(device) != on->device().index()) {
+        Py_DECREF(device);
+        return false;
+    }
     PyObject *handle = PyObject_CallOneArg(g_stream, device);
     Py_DECREF(device);
     if (!handle) return false;
@@ -135,7 +141,7 @@ PyObject *aggregate(PyObject *, PyObject *const *a, Py_ssize_t n) {
 }
 
 // ---- the paged cache.  Each call begins with (address of the entry point, handle, page bytes, heads, head_dim), then pages,
-// and has tables, lengths, indptr (or None) in a row.
+// and has tables, lengths, indptr (or None) in a row.  All tensors are of the pages' device, and that is current.
 
 struct Cache {
     void *fn, *handle;
@@ -154,12 +160,12 @@ bool cache_of(PyObject *const *a, Cache *c) {
            !watched();
 }
 
-bool batch_of(PyObject *const *a, int64_t tokens, bifeat_cache_batch *b) {
-    const at::Tensor *tables = tensor(a[0], at::kInt, at::kInt), *lengths = tensor(a[1], at::kLong, at::kLong), *indptr = nullptr;
+bool batch_of(PyObject *const *a, const Cache &c, int64_t tokens, bifeat_cache_batch *b) {
+    const at::Tensor *tables = tensor(a[0], at::kInt, at::kInt, c.pages), *lengths = tensor(a[1], at::kLong, at::kLong, c.pages), *indptr = nullptr;
     if (!tables || !lengths || tables->dim() != 2 || lengths->dim() != 1 || lengths->size(0) != tables->size(0)) return false;
     const int64_t B = tables->size(0);
     if (a[2] != Py_None) {
-        indptr = tensor(a[2], at::kLong, at::kLong);
+        indptr = tensor(a[2], at::kLong, at::kLong, c.pages);
         if (!indptr || indptr->dim() != 1 || indptr->size(0) != B + 1) return false;
     }
     *b = {static_cast<const int32_t *>(tables->data_ptr()), tables->size(1), static_cast<const int64_t *>(lengths->data_ptr()),
@@ -168,11 +174,11 @@ bool batch_of(PyObject *const *a, int64_t tokens, bifeat_cache_batch *b) {
 }
 
 // [tokens, heads, head_dim] of one of the three types, columns next to each other
-const at::Tensor *head_rows(PyObject *o, int64_t d, bifeat_head_rows *r, int32_t *dtype) {
+const at::Tensor *head_rows(PyObject *o, const Cache &c, bifeat_head_rows *r, int32_t *dtype) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.dim() != 3 || t.layout() != at::kStrided || !t.unsafeGetTensorImpl()->has_storage() ||
-        t.size(2) != d || t.stride(2) != 1)
+        t.size(2) != c.d || t.stride(2) != 1 || t.device() != c.pages->device())
         return nullptr;
     const auto type = t.scalar_type();
     if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return nullptr;
@@ -191,9 +197,9 @@ PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
         int32_t dtype, other;
         void *s = nullptr;
         const at::Tensor *tk, *tv;
-        if (!cache_of(a, &c) || !(tk = head_rows(a[6], c.d, &k, &dtype)) || !(tv = head_rows(a[7], c.d, &v, &other)) || dtype != other ||
-            tk->size(1) != c.heads || tv->size(1) != c.heads || tk->size(0) != tv->size(0) || !batch_of(a + 8, tk->size(0), &b) ||
-            !stream(&s)) {
+        if (!cache_of(a, &c) || !(tk = head_rows(a[6], c, &k, &dtype)) || !(tv = head_rows(a[7], c, &v, &other)) || dtype != other ||
+            tk->size(1) != c.heads || tv->size(1) != c.heads || tk->size(0) != tv->size(0) || !batch_of(a + 8, c, tk->size(0), &b) ||
+            !stream(&s, c.pages)) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }
@@ -218,7 +224,7 @@ PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
         bifeat_cache_batch b;
         void *s = nullptr;
         const int64_t tokens = PyLong_AsLongLong(a[6]), dtype = PyLong_AsLongLong(a[7]);
-        if (PyErr_Occurred() || tokens < 0 || !cache_of(a, &c) || !batch_of(a + 8, tokens, &b) || !stream(&s)) {
+        if (PyErr_Occurred() || tokens < 0 || !cache_of(a, &c) || !batch_of(a + 8, c, tokens, &b) || !stream(&s, c.pages)) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }
@@ -260,10 +266,10 @@ PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         o.scale = (float)PyFloat_AsDouble(a[7]);
         o.softcap = (float)PyFloat_AsDouble(a[8]);
         o.window = PyLong_AsLongLong(a[9]);
-        if (PyErr_Occurred() || !cache_of(a, &c) || !(tq = head_rows(a[6], c.d, &q, &dtype)) || !batch_of(a + 12, tq->size(0), &b) ||
-            (a[10] != Py_None && (!(prefix = tensor(a[10], at::kLong, at::kLong)) || prefix->dim() != 1 || prefix->size(0) != b.sequences)) ||
-            (a[11] != Py_None && (!(slopes = tensor(a[11], at::kFloat, at::kFloat)) || slopes->dim() != 1 || slopes->size(0) != tq->size(1))) ||
-            tq->size(1) > INT32_MAX || !stream(&s)) {
+        if (PyErr_Occurred() || !cache_of(a, &c) || !(tq = head_rows(a[6], c, &q, &dtype)) || !batch_of(a + 12, c, tq->size(0), &b) ||
+            (a[10] != Py_None && (!(prefix = tensor(a[10], at::kLong, at::kLong, c.pages)) || prefix->dim() != 1 || prefix->size(0) != b.sequences)) ||
+            (a[11] != Py_None && (!(slopes = tensor(a[11], at::kFloat, at::kFloat, c.pages)) || slopes->dim() != 1 || slopes->size(0) != tq->size(1))) ||
+            tq->size(1) > INT32_MAX || !stream(&s, c.pages)) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }
