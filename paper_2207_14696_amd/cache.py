@@ -5,6 +5,7 @@ it is built; what it leaves goes through ctypes, behind the checks here."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 from . import binding as _b
@@ -31,6 +32,23 @@ def _head_rows(t, heads: int, head_dim: int, name: str):
     if s[2] != 1 and head_dim != 1:
         raise ValueError(f"{name}: a head's columns must be contiguous")
     return _b._CHeadRows(t.data_ptr(), s[0], s[1])
+
+
+@functools.lru_cache(maxsize=None)
+def _without_backward():
+    """A function of autograd's graph around a call that has no backward pass: going back through it raises."""
+    import torch
+
+    class WithoutBackward(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, call):
+            return call()
+
+        @staticmethod
+        def backward(ctx, grad):
+            raise NotImplementedError("PagedCache.attend has no backward pass: the keys and values behind it are codes")
+
+    return WithoutBackward
 
 
 class PagedCache:
@@ -110,7 +128,7 @@ class PagedCache:
         return True
 
     def write(self, pages, k, v, tables, lengths, indptr=None) -> None:
-        """Quantises k and v, [tokens, heads, head_dim], into the pages."""
+        """Quantises k and v, [tokens, heads, head_dim], into the pages.  No gradient passes through codes."""
         if calls := _b._calls or _b._load_calls():
             r = calls.cache_write(*self._write, pages, k, v, tables, lengths, indptr)
             if r is not None:
@@ -149,7 +167,8 @@ class PagedCache:
         what the cache holds of it, each up to itself.  ``scale`` of the products (1 / sqrt(head_dim));
         ``softcap`` c > 0: c * tanh(score / c); ``window`` w > 0: the last w positions only; ``prefix`` int64
         [B]: positions that all queries see; ``slopes`` float32 [query heads]: bias by distance.  Returns
-        [tokens, query heads, head_dim] of q's dtype."""
+        [tokens, query heads, head_dim] of q's dtype.  There is no backward pass: where q requires a gradient, going back
+        through the output raises, and ``out`` is refused."""
         scale = self._scale if scale is None else scale
         if out is None and (calls := _b._calls or _b._load_calls()):
             r = calls.cache_attend(*self._attend, pages, q, scale, softcap, window, prefix, slopes, tables, lengths, indptr)
@@ -158,6 +177,11 @@ class PagedCache:
                     _check(r)
                 return r
         import torch
+        if q.requires_grad and torch.is_grad_enabled():
+            if out is not None:
+                raise ValueError("attend has no backward pass: no out where q requires a gradient")
+            args = (tables, lengths, indptr, scale, softcap, window, prefix, slopes)
+            return _without_backward().apply(q, lambda: self.attend(pages, q.detach(), *args))
         if q.dim() != 3:
             raise ValueError("q must be [tokens, query heads, head_dim]")
         heads = q.shape[1]

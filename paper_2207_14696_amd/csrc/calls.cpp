@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/autograd/generated/variable_factories.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -269,7 +270,7 @@ PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         if (PyErr_Occurred() || !cache_of(a, &c) || !(tq = head_rows(a[6], c, &q, &dtype)) || !batch_of(a + 12, c, tq->size(0), &b) ||
             (a[10] != Py_None && (!(prefix = tensor(a[10], at::kLong, at::kLong, c.pages)) || prefix->dim() != 1 || prefix->size(0) != b.sequences)) ||
             (a[11] != Py_None && (!(slopes = tensor(a[11], at::kFloat, at::kFloat, c.pages)) || slopes->dim() != 1 || slopes->size(0) != tq->size(1))) ||
-            tq->size(1) > INT32_MAX || !stream(&s, c.pages)) {
+            tq->size(1) > INT32_MAX || (tq->requires_grad() && c10::GradMode::is_enabled()) || !stream(&s, c.pages)) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }

@@ -282,3 +282,22 @@ def test_tensors_of_another_device_are_refused(bf, torch, monkeypatch):
     for call in calls:
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_attend_does_not_drop_a_gradient_silently(bf, torch, monkeypatch, native):
+    if not native:
+        import paper_2207_14696_amd.binding as binding
+        monkeypatch.setattr(binding, "_calls", False)
+    context = Context(bf, torch, 8, _normal(1, 40, 2, 64), _normal(2, 40, 2, 64), 3)
+    q = torch.from_numpy(_normal(3, 3, 4, 64)).float().cuda().requires_grad_()
+    args = (context.tables, context.lengths)
+    got = context.c.attend(context.pages, q, *args, window=20)
+    with torch.no_grad():
+        want = context.c.attend(context.pages, q, *args, window=20)
+    assert torch.equal(got, want) and got.requires_grad and not want.requires_grad
+    with pytest.raises(NotImplementedError):
+        got.sum().backward()
+    with pytest.raises(ValueError):
+        context.c.attend(context.pages, q, *args, out=torch.empty_like(want))
+    assert not context.c.attend(context.pages, q.detach(), *args).requires_grad
