@@ -4,8 +4,8 @@
 //     q . k_t = s_t (q . code_t) + mn_t sum(q)            sum_t p_t v_t = sum_t (p_t s_t) code_t + sum_t p_t mn_t
 // so that the matrix cores see whole numbers, which fp16 holds exactly, and nothing is decoded.  A code's bits are read as
 // an fp16 number as they stand: a subnormal, code * 2^-24, which the matrix cores of gfx950 multiply as it is (the factor is
-// taken out in 32 bits).  One byte permutation makes two operands of two 8-bit codes; of 4-bit codes a mask makes two, or
-// two times 16, which is taken out of the other factor or of the sum.
+// taken out in 32 bits).  One byte permutation makes two operands of two 8-bit codes; of 4-bit values' codes a mask makes two, or
+// two times 16, which is taken out of the sum; those of keys are all times 16 (see key_of4).
 // The values' codes are weighted about the middle of their range (c = mn + 2^(bits-1) s): what a weight's rounding to fp16
 // is off by then meets at most half a row's range.
 #pragma once
@@ -254,27 +254,29 @@ __device__ inline half8 operand(uint32_t a, uint32_t b, uint32_t c, uint32_t d) 
     return __builtin_bit_cast(half8, Words4{{a, b, c, d}});
 }
 
-// The same as whole numbers less their middle (4-bit codes' times 16 where they come so), for 32-bit queries: 1024 + code is
-// the code's bits beside 1024's, and 1024 + middle is taken off exactly.  Of subnormal operands the matrix cores lose the bits
-// that a normal number would have in place of their leading zeros (4-bit codes: 7 of 24), and sums of products of codes that
-// are all positive leave 2^-24 of the codes' common part.
+// Eight 4-bit codes of a key, all times 16: (0, 4), (1, 5), (2, 6), (3, 7).  Of subnormal operands the matrix cores lose the bits that a normal
+// number would have in place of their leading zeros; with every other pair as it stands, two instructions fewer, scores were off by 2^-21.4
+// of the sum of |q| |k| (root mean square), so by 2^-24, as of 8-bit codes (contexts of 131 072 in 4 bits 112.5 us, 115 so).
+__device__ inline half8 key_of4(uint32_t w) {
+    auto at = [](uint32_t x) { return x & 0x00f000f0u; };
+    return operand(at(w << 4), at(w), at(w >> 4), at(w >> 8));
+}
+
+// Codes as whole numbers less their middle (4-bit ones' times 16 where they come so), for 32-bit queries: 1024 + code is the code's bits beside
+// 1024's, and 1024 + middle is taken off exactly.  Sums of products of codes that are all positive leave 2^-24 of the codes' common part.
 __device__ inline half8 centred(half8 bits, half8 top) {
     Words4 w = __builtin_bit_cast(Words4, bits);
 #pragma unroll
     for (int i = 0; i < 4; i++) w.w[i] |= 0x64006400u;
     return __builtin_bit_cast(half8, w) - top;
 }
-// what `top` is for codes of BITS bits in a row, and for eight 4-bit codes as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16
 __device__ inline half8 all_of(float x) {
     const _Float16 m = (_Float16)x;
     return half8{m, m, m, m, m, m, m, m};
 }
-__device__ inline half8 centre4() {
-    const _Float16 m = (_Float16)1032.f, n = (_Float16)1152.f;
-    return half8{m, m, n, n, m, m, n, n};
-}
-// the unit of a product with a code: codes are subnormals, or (NP = 2) whole numbers
+// the unit of a product with a value's code: codes are subnormals, or (NP = 2) whole numbers; and with a key's, 4-bit ones times 16
 template <int NP> constexpr float kUnit = NP == 2 ? 1.f : 16777216.f;
+template <int BITS, int NP> constexpr float kKeyUnit = kUnit<NP> / (BITS == 4 ? 16 : 1);
 
 // Loads from a head's block of a page, whose address all lanes share: a descriptor in scalar registers, a 32-bit offset a lane
 // and one for all, where 64-bit addresses would take two vector registers and three vector instructions a load.  (The
@@ -358,8 +360,7 @@ __device__ inline float largest_finite(float most, const float (&x)[8]) {
     for (int i = 0; i < 8; i++) most = fmaxf(most, fabsf(x[i]) <= 3.402823466e38f ? fabsf(x[i]) : 0.f);
     return most;
 }
-// 8 columns as an operand beside 8 codes: of 4-bit codes, which come as (0, 4), (1, 5) * 16, (2, 6), (3, 7) * 16, the odd ones' are
-// a 16th.  Returns what they add up to.
+// 8 columns as an operand beside 8 codes, which of 4 bits come as 0, 4, 1, 5, 2, 6, 3, 7.  Returns what they add up to.
 template <int BITS, int NP>
 __device__ inline float query_operand(const float (&x)[8], float up, half8 &hi8, half8 &lo8) {
     float sum = 0.f;
@@ -369,9 +370,8 @@ __device__ inline float query_operand(const float (&x)[8], float up, half8 &hi8,
         const _Float16 hi = (_Float16)y, lo = NP == 2 ? (_Float16)(y - (float)hi) : (_Float16)0.f;
         sum += (float)hi + (float)lo;
         const int slot = BITS == 8 ? e : (e % 4) * 2 + e / 4;
-        const _Float16 down = BITS == 4 && (e & 1) ? (_Float16)0.0625f : (_Float16)1.f;
-        hi8[slot] = hi * down;
-        if constexpr (NP == 2) lo8[slot] = lo * down;
+        hi8[slot] = hi;
+        if constexpr (NP == 2) lo8[slot] = lo;
     }
     return sum;
 }

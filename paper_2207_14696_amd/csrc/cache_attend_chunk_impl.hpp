@@ -115,10 +115,9 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                     const uint32_t w0 = kw[2 * c], w1 = kw[2 * c + 1];
                     key = operand(bytes_of(w0, 0), bytes_of(w0, 2), bytes_of(w1, 0), bytes_of(w1, 2));
                 } else {
-                    const uint32_t w = kw[c], w8 = w >> 8;
-                    key = operand(w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u);
+                    key = key_of4(kw[c]);
                 }
-                if constexpr (NP == 2) key = centred(key, BITS == 8 ? all_of(1152.f) : centre4());
+                if constexpr (NP == 2) key = centred(key, all_of(1152.f));
                 keys[buf][kgroup * S::KS + kpart * (S::KS / S::KP) + c][lane] = __builtin_bit_cast(uint4, key);
             }
 #pragma unroll
@@ -180,7 +179,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
             if (lane == 0) tops[wave] = any_row ? big : 0.f;
             __syncthreads();
             const float up = power_to(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), 14);
-            f = a.scale * kLog2e * (kUnit<NP> / up);
+            f = a.scale * kLog2e * (kKeyUnit<BITS, NP> / up);
 #pragma unroll
             for (int n = 0; n < NT; n++) {
                 float sum = 0.f;
@@ -192,7 +191,7 @@ __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chun
                 }
                 sum += __shfl_xor(sum, 16);
                 sum += __shfl_xor(sum, 32);
-                qsum[n] = sum * (f / kUnit<NP>);
+                qsum[n] = sum * (f / kKeyUnit<BITS, NP>);
                 const int row = wrow0 + 16 * n + (at_lane & 15);
                 const bool real = row - row0 < nrows;
                 pos[n] = real ? v.len - v.n + row / a.group : -1;

@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
 #pragma unroll
             for (int m = 1; m < 64; m *= 2) big = fmaxf(big, __shfl_xor(big, m));
             const float up = power_to(big, 14);
-            f = a.scale * kLog2e * (kUnit<NP> / up);
+            f = a.scale * kLog2e * (kKeyUnit<BITS, NP> / up);
 #pragma unroll
             for (int c = 0; c < L::KS; c++) {
                 float x[8];
@@ -167,7 +167,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
             }
             qsum += __shfl_xor(qsum, 16);
             qsum += __shfl_xor(qsum, 32);
-            qsum *= f / kUnit<NP>;
+            qsum *= f / kKeyUnit<BITS, NP>;
         }
         const float slope = MODE && a.slopes ? a.slopes[real ? qh : 0] * kLog2e : 0.f;
         const Cap cap = cap_of(a);
@@ -214,10 +214,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
                         const uint32_t w0 = kw[j][2 * c], w1 = kw[j][2 * c + 1];
                         key = operand(bytes_of(w0, 0), bytes_of(w0, 2), bytes_of(w1, 0), bytes_of(w1, 2));
                     } else {
-                        const uint32_t w = kw[j][c], w8 = w >> 8;
-                        key = operand(w & 0x000f000fu, w & 0x00f000f0u, w8 & 0x000f000fu, w8 & 0x00f000f0u);
+                        key = key_of4(kw[j][c]);
                     }
-                    if constexpr (NP == 2) key = centred(key, BITS == 8 ? all_of(1152.f) : centre4());
+                    if constexpr (NP == 2) key = centred(key, all_of(1152.f));
 #pragma unroll
                     for (int p = 0; p < NP; p++) acc[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(key, q[p][c], acc[j], 0, 0, 0);
                 }

@@ -301,3 +301,44 @@ def test_attend_does_not_drop_a_gradient_silently(bf, torch, monkeypatch, native
     with pytest.raises(ValueError):
         context.c.attend(context.pages, q, *args, out=torch.empty_like(want))
     assert not context.c.attend(context.pages, q.detach(), *args).requires_grad
+
+
+# ------------------------------------------------------------------ large sums of products
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("bits,d", [(4, 64), (4, 128), (4, 256), (8, 64), (8, 128), (8, 256)])
+def test_scores_of_large_sums(bf, torch, bits, d, many):
+    """Two positions whose scores are nearly alike, of products that add up to tens of thousands: their weights' ratio shows the difference."""
+    rng, scale, n, ps = np.random.default_rng(d + bits), 256.0, 8192, 16
+    c = bf.PagedCache(bits, 1, d, ps)
+
+    def cached(keys, tables, lengths):
+        """The keys in the cache, as they stand there, beside values (1, 0, 0, ..), (0, 1, 0, ..), (1, 0, ..), .."""
+        k = torch.from_numpy(keys[:, None]).float().cuda()
+        v = torch.zeros_like(k)
+        v[0::2, :, 0], v[1::2, :, 1] = 1, 1
+        pages = c.new_pages(int(tables.max()) + 1)
+        c.write(pages, k, v, tables, lengths)
+        return pages, c.read(pages, tables, lengths, len(k))[0].double().cpu().numpy()[:, 0]
+
+    q = rng.standard_normal(d).astype(np.float16).astype(np.float64)
+    keys = rng.standard_normal((n, d))
+    _, stand = cached(keys, torch.arange(n // ps, dtype=torch.int32, device="cuda")[None], torch.tensor([n], device="cuda"))
+    pairs = np.argsort(stand @ q).reshape(-1, 2)[::4]
+    B, group, last = len(pairs), 40 if many else 1, 2 if many else 1
+    tables = torch.zeros(B, 2 ** 20 // ps if many else 1, dtype=torch.int32, device="cuda")
+    tables[:, 0] = torch.arange(B, device="cuda")
+    lengths = torch.full((B,), 2, dtype=torch.int64, device="cuda")
+    pages, k = cached(keys[pairs.reshape(-1)], tables, lengths)
+    k = k.reshape(B, 2, d)
+    tq = torch.from_numpy(q).half().cuda().expand(last * B, group, d)
+    out = c.attend(pages, tq, tables, lengths, scale=scale).double().cpu().numpy().reshape(B, last, group, d)[:, -1]
+    away = scale * (k[:, 0] - k[:, 1]) @ q
+    seen = np.abs(away) < 1
+    assert seen.sum() > 50
+    got = np.log(out[seen, :, 0] / out[seen, :, 1])
+    # Sums of products in 32 bits: 2^-22 of the sum of their sizes.  A weight is off by 2^-12 of it, which meets half its row's range, 1/2, in both
+    # columns: 2^-13 of their weights' sum 1 in each of two outputs of 1 / (1 + e) or more, 3.8 2^-11 in all; and the two results' 2^-11.
+    bound = 2.0 ** -22 * scale * (np.abs(k) @ np.abs(q)).max(-1)[seen] + 6 * 2.0 ** -11
+    err = np.abs(got - away[seen, None]).max(-1)
+    assert (err <= bound).all(), (err / bound).max()
