@@ -400,11 +400,18 @@ int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *in
  *   the output is sum_j softmax(x)_j v_j; a query that sees nothing gets zeros.
  *
  * Queries of BIFEAT_F16 and BIFEAT_BF16 enter the matrix cores as fp16 (scaled by a
- * power of two per tile of rows: exact but for bf16 columns 2^-29 of a tile's largest),
- * codes as they are; products are summed in fp32, softmax and its sums are fp32, weights
+ * power of two per tile of rows: exact but for columns below 2^-29 of the largest of the
+ * tile's queries that see something), codes as they are; products are summed in fp32
+ * (codes of few bits enter as subnormals, for which the matrix cores keep somewhat less:
+ * scores are within 2^-22 of the sum of |q| |k|), softmax and its sums are fp32, weights
  * are rounded to fp16 before they meet the values' codes (BIFEAT_F16 with few rows: to two
  * fp16 pieces).  BIFEAT_F32: queries and weights enter as two fp16 pieces each (22 bits).
- * Which kernel runs, and so the rounding, depends on the call's sizes (not on its data). */
+ * A capped score is within 2^-21 of itself (16-bit results up to a cap of 64: within 2^-22
+ * of the cap).  Of values of a range below 2^-72 sums keep 2^-106 a position.
+ * Which kernel runs, and so the rounding, depends on the call's sizes (not on its data):
+ * a context counts as long as its page table is wide.  A table no wider than the longest
+ * context makes short calls faster (a token over 300: 9.0 us, 16.3 by a table 4 times as
+ * wide; 64 rows of 8 sequences of 2048: 38 and 52). */
 typedef struct {
     int32_t bits;      /* 4 or 8 */
     int32_t heads;     /* cached heads, 1..1024 */

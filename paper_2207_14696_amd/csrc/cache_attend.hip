@@ -104,8 +104,9 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendCall a, AttendPl
     }
 }
 
-// rows: the most that an item has.  Four waves a row where an item of 16 rows may have 48 parts or more (one sequence of 8192, 4 rows
-// on 8 heads of 128, 64 parts: 16.7 us, with one wave 17.2), one where it has fewer (8 such sequences of 2048: 23.5 and 20.6).
+// rows: the most that an item has.  Four waves a row where an item of 16 rows may have 48 parts or more (one sequence of 12 288, 4 rows
+// on each of 8 heads of 128, 48 parts: the call 18.7 us, with one wave 20.0; of 65 536 on one head, 256 parts: 21.1 and 28.7), one where it has
+// fewer (8 sequences of 2048 on 8 heads, 8 parts: 19.1, with four 20.3; two of 8192, 32 parts: 20.1 and 20.7).
 template <int R, int WAVES>
 void launch_join(const AttendCall &a, const AttendPlan &p, int dp, int rows) {
     const dim3 grid(p.nw, std::min(16, (rows * WAVES + 3) / 4));
@@ -172,7 +173,9 @@ hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {
     // window leaves an unknown part of the context: 20 rows, 1024 positions seen 47 and 64).  And any number where the units
     // come to 10 a workgroup or fewer: 64 rows of 8 sequences of 2048 on 8 heads of 128 (10) 40 and 53, 256 rows of one of 512 (1)
     // 15 and 30, 256 rows of 8 of 1024 (17) 67 and 58.  Not for 32-bit queries, whose operands cost twice (385 rows of three of
-    // 1001, 2 units: 32 and 29.5).
+    // 1001, 2 units: 32 and 29.5).  Lengths are not known here: a context counts as long as its page table is wide (a token over 300 9.0 us, 16.3 by a table 4 times as wide), and
+    // rows are a mean over the batch (2048 rows over 16 384 beside 255 single tokens of 2048, 8 heads of 128: 873 us, in calls of their
+    // own 252 and 201).
     const int few = dp == 64 ? 64 : dp == 256 && !a.window ? 16 : 32;
     const bool chunk = a.b.tokens * a.group > (int64_t)few * a.b.B &&
                        (np == 2 || units_of(kRowsR, kRowsTok) > 10 * rows_workgroups(dp));

@@ -6,8 +6,7 @@
 // is on its way, into LDS in the very order in which the products take them (1 KB an operand, 16 bytes a lane, no conflict), and all
 // four waves read them there for rows of their own.  Scores are keys x queries as in the kernel for few rows, so that
 // weights need not be moved; NT tiles of 16 rows a wave share what is read.
-// 2048 tokens over 32 768, 32 heads on 8 of 128 in 8 bits: 1640 us with the join, 650 TFLOP/s; vector instructions are issued 56 % of
-// that time, matrix products 27 %.  A batch of 16 prompts and chunks, 12 heads of 64, bias by distance: 325 us, 185 TFLOP/s.
+// 2048 tokens over 32 768, 32 heads on 8 of 128 in 8 bits: 1664 us with the join, 640 TFLOP/s.
 #pragma once
 
 #include "cache_attend.hpp"
@@ -26,7 +25,8 @@ struct ChunkShape {
     static constexpr int KEYS = TOK / 16 * KS, VALUES = TOK / 32 * VT;
 };
 
-// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries)
+// NP: fp16 pieces of a query element and of a weight (2 for 32-bit queries; a second piece of 16-bit results' weights would add to the
+// vector instructions, which bound this kernel: fp16 results are off by 3.0e-4 with one, 2.1e-4 of it their own rounding).  MODE: see mode_of
 template <int BITS, int DP, int NP, int NT, int MODE>
 __global__ __launch_bounds__(256, DP == 256 && NP == 2 ? 1 : 2) void attend_chunk_kernel(AttendCall a, AttendPlan plan) {
     using S = ChunkShape<BITS, DP, NT>;

@@ -13,8 +13,6 @@
 
 namespace bf {
 
-
-
 template <int BITS, int DP>
 struct RowLanes {
     static constexpr int KB = DP / 4 * BITS / 8;   // bytes of a key that a lane reads (its quarter of the columns)
@@ -28,7 +26,7 @@ struct RowLanes {
 
 // NP: fp16 pieces of a query element (2 for 32-bit queries); WP: of a weight.  One is enough where the result is rounded to
 // bf16 (2^-9; a weight's one piece 2^-12, the second costs 8 % of long contexts in 4 bits); an fp16 result would be 1.6 times as far off
-// with one, and the second costs it 1 %.
+// with one, and the second costs it 1 %.  MODE: see mode_of.
 template <int BITS, int DP, int NP, int WP, int MODE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend_rows_kernel(AttendCall a, AttendPlan plan) {
     using L = RowLanes<BITS, DP>;
@@ -77,7 +75,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : DP == 128 ? 2 : 3) void attend
         int slot0, slot1;
         // Asked for without a branch, of no block where the item has no such unit: across a branch the compiler could not tell how
         // many loads are on their way, and would wait for all of them where it needs the oldest (contexts of 131 072 tokens in 4
-        // bits 121 us, 117 so).  Past the caches: 64 answers 133 us, 120 so.
+        // bits 121 us, 117 so).  Past the caches: 64 single tokens over up to 8192 130 us, 119 so; also where items share what they read, which is
+        // slower for caches that would hold it (64 rows of 8 sequences of 2048 34.7 us, 38.0 so; 32 x 5 tokens of 256 columns 44.2 and 47.2) and
+        // faster for larger ones (64 rows of 64 of 4096, 12 heads of 64: 321 and 289).
         auto load_keys = [&](int u) {
             const bool wanted = u < units;
             if (wanted && u - paged >= 32) {

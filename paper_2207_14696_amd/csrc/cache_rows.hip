@@ -127,8 +127,10 @@ __global__ __launch_bounds__(kThreads) void cache_write_kernel(CachePages c, Cac
     }
 }
 
-// Bound by the bytes of the result, twice (fp32: four times) the codes'.  STREAMED past the caches where they would not hold it:
-// 149 000 tokens of 8 heads of 128 in 8 bits to bf16 (610 MB written, 320 read) 257 us, 167 so (5.6 TB/s); 26 MB 13 us, 11 so.
+// Bound by the bytes of the result, twice (fp32: four times) the codes'.  STREAMED past the caches from 16 MB on:
+// 149 000 tokens of 8 heads of 128 in 8 bits to bf16 (610 MB written, 320 read) 257 us, 167 so (5.6 TB/s); 32 MB 10.5 us, 8.7 so; 256 MB 81.5 and
+// 63.  A program that goes through the result next gives some of that back: with k and v scaled in place after it, 32 MB 26.3 us, 28.3 so;
+// 256 MB 154 and 161.
 // 65 536 tokens to fp32 (537 MB written) 143 us, 104 so; with a lane's eight columns next to each other, half a line a store, 257.
 template <typename T, int BITS, int LPR, bool STREAMED>
 __global__ __launch_bounds__(kThreads) void cache_read_kernel(CachePages c, CacheBatch b, T *k, T *v, int per) {
