@@ -6,7 +6,7 @@
 // its way.  Scores are keys x queries (positions the rows of the 16 x 16 product), so that a lane ends up with
 // four positions of one query, which is how the second product wants its weights: nothing is moved between lanes.
 // 64 single tokens over up to 8192 positions, 32 heads on 8 of 128 in 8 bits (622 MB): 119 us, 5.2 TB/s; four over 131 072, 64 heads on 8,
-// 4 bits (604 MB): 115, 5.3 TB/s.  Of its waves' time 45 % waits for memory, 17 to 28 % issues vector instructions.
+// 4 bits (604 MB): 116, 5.2 TB/s.  Of its waves' time 40 to 44 % waits for memory, 17 to 29 % issues vector instructions.
 #pragma once
 
 #include "cache_attend.hpp"
