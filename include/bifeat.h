@@ -423,7 +423,8 @@ typedef struct {
  * 68 MB each): one for each stream, allocated by the first call on it that needs one, and
  * one for the calls that are captured, allocated with the first of those.  So calls on
  * different streams may overlap, and threads may share a handle; graphs captured with one
- * handle must not be replayed at the same time, nor after the handle is destroyed. */
+ * handle must not be replayed at the same time, nor after the handle is destroyed.  Of
+ * several streams in one capture the first that needs the workspace has it. */
 typedef struct bifeat_cache bifeat_cache;
 
 /* The sequences of one call and which of their tokens it is about: the last n_b of

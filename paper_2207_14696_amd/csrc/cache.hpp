@@ -13,11 +13,13 @@ struct bifeat_cache {
     int64_t page_bytes = 0;
     int opt_validate = 0;
     // what bifeat_cache_attend leaves of contexts that several workgroups share (see cache_attend.hpp): each stream has its own, so that calls on
-    // different streams do not meet, and captured calls have one, whichever stream they are replayed on
+    // different streams do not meet, and captured calls have one, whichever stream they are replayed on.  Streams of one capture may be branches
+    // that are replayed side by side: the first that asks has it
     struct Workspace {
         int device;
         hipStream_t stream;
-        bool captured;  // of calls that are being captured; stream is of no account
+        bool captured;
+        unsigned long long capture;  // the last that asked for it
         float *partial;
         Workspace *next;
     };
@@ -143,7 +145,7 @@ hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const He
 hipError_t launch_cache_read(const CachePages &c, const CacheBatch &b, void *k, void *v, int bits, int dtype, hipStream_t s);
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a);
 void launch_cache_check(const CacheBatch &b, int ps_log2, int64_t num_pages, int32_t *d_bad, hipStream_t s);
-// The workspace of calls on `s`, and that of captured calls; allocated unless `s` is being captured.  Null: there is none.  The handle's mutex is held.
+// The workspace of calls on `s`, or of captured calls; both are allocated unless `s` is being captured.  Null: there is none.  The handle's mutex is held.
 float *workspace_of(bifeat_cache *h, hipStream_t s);
 
 }  // namespace bf

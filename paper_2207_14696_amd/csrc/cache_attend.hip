@@ -135,21 +135,26 @@ static hipError_t launch_attend_chunk(const AttendCall &a, const AttendPlan &p, 
 float *workspace_of(bifeat_cache *h, hipStream_t s) {
     int device = 0;
     hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
-    if (hipGetDevice(&device) != hipSuccess || hipStreamIsCapturing(s, &status) != hipSuccess) {
+    unsigned long long capture = 0;
+    if (hipGetDevice(&device) != hipSuccess || hipStreamGetCaptureInfo(s, &status, &capture) != hipSuccess) {
         (void)hipGetLastError();
         return nullptr;
     }
     const bool capturing = status != hipStreamCaptureStatusNone;
-    auto find = [&](bool captured) -> float * {
-        for (bifeat_cache::Workspace *w = h->workspaces; w; w = w->next)
-            if (w->device == device && w->captured == captured && (captured || w->stream == s)) return w->partial;
-        return nullptr;
+    auto find = [&](bool captured) {
+        bifeat_cache::Workspace *w = h->workspaces;
+        while (w && !(w->device == device && w->captured == captured && (captured || w->stream == s))) w = w->next;
+        return w;
     };
-    float *own = find(capturing);
-    if (own || capturing) return own;
+    if (capturing) {
+        bifeat_cache::Workspace *w = find(true);
+        if (w && w->capture != capture) w->capture = capture, w->stream = s;
+        return w && w->stream == s ? w->partial : nullptr;
+    }
+    if (const bifeat_cache::Workspace *w = find(false)) return w->partial;
     for (const bool captured : {true, false}) {
         if (find(captured)) continue;
-        auto *w = new (std::nothrow) bifeat_cache::Workspace{device, s, captured, nullptr, h->workspaces};
+        auto *w = new (std::nothrow) bifeat_cache::Workspace{device, s, captured, 0, nullptr, h->workspaces};
         if (!w) return nullptr;
         if (hipMalloc((void **)&w->partial, sizeof(float) * kPartialFloats + sizeof(PartOf) * rows_workgroups(64)) != hipSuccess) {
             (void)hipGetLastError();
@@ -158,7 +163,7 @@ float *workspace_of(bifeat_cache *h, hipStream_t s) {
         }
         h->workspaces = w;
     }
-    return find(false);
+    return find(false)->partial;
 }
 
 hipError_t launch_cache_attend(bifeat_cache *h, const AttendCall &a) {

@@ -263,6 +263,29 @@ def test_a_replayed_graph_and_other_calls_do_not_meet(bf, torch):
         assert torch.equal(out, want) and all(torch.equal(x, want2) for x in got)
 
 
+def test_branches_of_a_graph_do_not_meet(bf, torch):
+    c = bf.PagedCache(8, 4, 64, 64)
+    contexts = _two_contexts(bf, torch, c)
+    outs, graph, side = [torch.zeros_like(x[1]) for x in contexts], torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        for stream, (pages, q, tables, lengths, _), out in zip((main, side), contexts, outs):
+            with torch.cuda.stream(stream):
+                c.attend(pages, q, tables, lengths, out=out)
+        main.wait_stream(side)
+    for _ in range(10):
+        for x, out in zip(contexts, outs):
+            x[1].copy_(torch.randn_like(x[1]))
+            out.zero_()
+        graph.replay()
+        wants = [c.attend(*x[:4]) for x in contexts]
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], wants[0])
+        # the second branch has no workspace, so that its context is not split: other sums; fp16's rounding of each, and of values below 4
+        assert (outs[1].float() - wants[1].float()).abs().max() <= 2 * 2.0 ** -11 * 4
+
+
 def test_tensors_of_another_device_are_refused(bf, torch, monkeypatch):
     c = bf.PagedCache(8, 2, 64, 16)
     pages, x = c.new_pages(2), torch.zeros(1, 2, 64, device="cuda")
