@@ -391,6 +391,13 @@ int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *in
  *   finite (columns all alike, or closer than L / FLT_MAX) scale = inv = 0.  A row that
  *   holds an infinity or a NaN, or whose range is not finite, gets scale = mn = NaN: it
  *   reads back as NaN and spoils the tokens that attend to it, but no others.
+ * append: write, of keys that are turned to their positions on the way, and the call's
+ *   queries turned with them.  Column pair i < pairs of a row of a token at position p is
+ *   (i, i + pairs), or (2 i, 2 i + 1) where interleaved; with a = p * frequencies[i] it becomes
+ *     (u, w) -> scale * (u cos a - w sin a),  scale * (u sin a + w cos a)
+ *   and the columns from 2 * pairs on stay.  All of it in 64 bits; a key's columns are then
+ *   rounded to fp32 and written as above, a query's to fp32 and to their type.  Values are
+ *   written as they are.  Queries before their sequence's beginning come out as zeros.
  * read: x' = mn + code * scale.
  * attend: query token i of sequence b is at position p = lengths[b] - n_b + i, query head
  *   h reads cached head h / (query_heads / heads).  It sees position j < lengths[b] if
@@ -463,6 +470,14 @@ typedef struct {
     const float *slopes;   /* DEVICE [query_heads]: bias by distance; or NULL */
 } bifeat_attend_options;
 
+/* How bifeat_cache_append turns rows by their position. */
+typedef struct {
+    const float *frequencies; /* DEVICE [pairs]: radians a position */
+    int32_t pairs;            /* 0..head_dim / 2 */
+    int32_t interleaved;      /* 1: a pair's columns lie next to each other */
+    double scale;             /* of the turned columns; usually 1 */
+} bifeat_turn;
+
 int bifeat_cache_create(const bifeat_cache_spec *spec, bifeat_cache **out);
 void bifeat_cache_destroy(bifeat_cache *c);
 /* Bytes of a page (a multiple of 16), or BIFEAT_EINVAL. */
@@ -477,19 +492,117 @@ int bifeat_cache_reserve(bifeat_cache *c, void *stream);
 /* The batch contract on its own: BIFEAT_OK or BIFEAT_EINVAL; synchronises `stream`. */
 int bifeat_cache_check(const bifeat_cache *c, int64_t num_pages, const bifeat_cache_batch *batch, void *stream);
 
-/* The three calls only enqueue kernels on `stream`.  tokens = 0 is a no-op.  `dtype`
+/* The four calls only enqueue kernels on `stream`.  tokens = 0 is a no-op.  `dtype`
  * (BIFEAT_F32, _F16, _BF16) is the type of k and v, of the arrays read into, of q and out.
+ * append: any number of query heads up to 65536, or 0 without q and out; out: DEVICE
+ * [tokens][query_heads][head_dim], which shares no memory with the other arrays.
  * k, v outputs of read: DEVICE [tokens][heads][head_dim]; out: DEVICE
  * [tokens][query_heads][head_dim]; query_heads a multiple of heads, sequences * heads at
  * most 2^30 for attend (BIFEAT_EINVAL).  The arrays and pages are of the device that is
  * current, which `stream` is of. */
 int bifeat_cache_write(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
                        const bifeat_head_rows *k, const bifeat_head_rows *v, int32_t dtype, void *stream);
+int bifeat_cache_append(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
+                        const bifeat_head_rows *q, int32_t query_heads, const bifeat_head_rows *k,
+                        const bifeat_head_rows *v, int32_t dtype, const bifeat_turn *turn, void *out, void *stream);
 int bifeat_cache_read(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
                       void *k, void *v, int32_t dtype, void *stream);
 int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch,
                         const bifeat_head_rows *q, int32_t query_heads, int32_t dtype,
                         const bifeat_attend_options *options, void *out, void *stream);
+
+/* ---- products with matrices in 4 bits
+ *
+ * A matrix of out_features rows (N) and in_features columns (K) is kept as 4-bit codes with a
+ * range of its own for each `group` columns of a row: weight = minimum + code * scale, scale
+ * and minimum in bfloat16.  Packed (DEVICE uint8 [experts][bifeat_linear_bytes()], 16-byte
+ * aligned): rows by 16, columns by 128, filled up with zeros;
+ *     codes   [rows / 16][columns / 128][lane 0..63][word 0..3], 32-bit words
+ *     levels  [rows / 16][columns / group][row 0..15], 32-bit words: scale low, minimum high half
+ * where word w of lane l of block (r, k) holds row 16 r + l % 16, columns 128 k + 32 w + 8 (l / 16) + c,
+ * c = 0..7, the code of c at bit 4 (c / 2 + 4 (c % 2)): as the matrix cores take it.
+ *
+ * pack: with mn, mx the least and largest of a group's weights, minimum = mn rounded down to
+ *   bfloat16, scale = (mx - minimum) / 15 rounded up to bfloat16, code = min(rne((w - minimum) / scale), 15)
+ *   (steps in fp32; scale 0: code 0), so that a weight is off by half a scale and fp32 roundings.  A
+ *   group that holds an infinity or a NaN, or whose range is not finite in bfloat16, gets scale =
+ *   minimum = NaN: its row of the matrix gives NaN, and no other.
+ * multiply: out[t][n] = sum_k x[t][k] weight[n][k], for rows x of any number.  16-bit x enter
+ *   the matrix cores as they are, 32-bit ones in three pieces that are them together, codes as
+ *   16 + code, all exact; sums are fp32: off by about 2^-20 of the sum of |x| scale 16 (fewer than
+ *   4096 columns), then rounded to x's type.  A row with an infinity or a NaN, or with a group whose sum
+ *   of |x| passes 2^122, gives infinities and NaN; other rows are as they were without it.
+ * experts: `experts` matrices of one size, and tokens with `choices` of them each.  out[t][j] =
+ *   x[t] or x[t][j] times matrix ids[t][j]; with weights the sum over j of weights[t][j] times
+ *   that (in fp32, j ascending).  An id outside [0, experts) names none: its product is zeros,
+ *   whatever x holds there, and it adds nothing.  Tokens may name one matrix twice.
+ * Results do not depend on the order in which anything ran.  There is no gradient. */
+typedef struct {
+    int32_t out_features, in_features; /* 1..2^20 */
+    int32_t group;                     /* columns that share a scale: 32, 64, 128 */
+    int32_t experts;                   /* matrices: 1..1024 */
+} bifeat_linear_spec;
+
+/* Bytes of one packed matrix (a multiple of 64), or BIFEAT_EINVAL. */
+int64_t bifeat_linear_bytes(const bifeat_linear_spec *spec);
+/* weight: DEVICE [experts][out_features][in_features] of dtype. */
+int bifeat_linear_pack(const bifeat_linear_spec *spec, const void *weight, int32_t dtype, uint8_t *packed, void *stream);
+/* The values that the codes stand for, fp32 [experts][out_features][in_features]. */
+int bifeat_linear_unpack(const bifeat_linear_spec *spec, const uint8_t *packed, float *weight, void *stream);
+/* x: DEVICE rows of in_features columns, `row_stride` elements apart (>= 0); out: DEVICE
+ * [rows][out_features], which shares no memory with x.  One matrix (experts = 1). */
+int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed, const void *x, int64_t row_stride, int64_t rows,
+                           int32_t dtype, void *out, void *stream);
+
+typedef struct {
+    const void *x;          /* DEVICE: row of token t and choice j at t * token_stride + j * choice_stride */
+    int64_t token_stride, choice_stride; /* elements, >= 0; choice_stride 0: a token's choices share its row */
+    const int32_t *ids;     /* DEVICE [tokens][choices] */
+    const float *weights;   /* DEVICE [tokens][choices], or NULL: no sum */
+    int64_t tokens;
+    int32_t choices;        /* 1..64 */
+} bifeat_expert_rows;
+
+/* Bytes of DEVICE memory that bifeat_linear_experts needs besides, 16-byte aligned and for
+ * the time of the call's kernels alone; or BIFEAT_EINVAL. */
+int64_t bifeat_linear_experts_workspace(const bifeat_linear_spec *spec, const bifeat_expert_rows *rows);
+/* out: DEVICE [tokens][choices][out_features], with weights [tokens][out_features]. */
+int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed, const bifeat_expert_rows *rows, int32_t dtype,
+                          void *out, void *workspace, int64_t workspace_bytes, void *stream);
+
+/* ---- routing to experts
+ *
+ * Of each token's logits x[0..experts): score = softmax(x) or 1 / (1 + exp(-x)), in 64 bits.
+ * Experts rank by x, or with a bias by score + bias; the larger first, of equal ones the lower
+ * number.  An expert whose logit is -infinity, or whose rank is that or NaN, is not to be had.  With groups > 1 the
+ * experts / groups neighbours of a group compete first: the top_groups groups of the largest
+ * group score are kept, which is their best expert's rank, or (group_two) the sum of their two best
+ * experts' score + bias, of the one where only one is to be had; of equal ones the lower number.
+ * ids: the `choices` best of what is left, best first, -1 where there are fewer.
+ * weights: their scores (without bias), over their sum where `renormalise` is set (0 where that is 0),
+ * times `scale`; 0 for id -1.  A NaN or +infinity among the softmax's logits, or a NaN among
+ * the sigmoid's, makes all the token's weights, and its logits' gradient, NaN.
+ * backward: the gradient of the logits from that of the weights, through score, sum and scale (the
+ * choice itself and the bias have none); what was not chosen gets zeros where score and
+ * sum do not reach it. */
+typedef struct {
+    int32_t experts;     /* 1..1024 */
+    int32_t choices;     /* 1..min(experts, 64) */
+    int32_t sigmoid;     /* 0: softmax */
+    int32_t groups, top_groups; /* groups: 1..64, divides experts; top_groups: 1..groups */
+    int32_t group_two;   /* 1: a group's score is the sum of its two best */
+    int32_t renormalise;
+    double scale;
+    const float *bias;   /* DEVICE [experts] or NULL */
+} bifeat_route_options;
+
+/* logits: DEVICE rows of `experts` columns of dtype, row_stride elements apart (>= 0).  ids: DEVICE
+ * int32 [tokens][choices], weights: DEVICE fp32 of that shape. */
+int bifeat_route(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens, const bifeat_route_options *options, int32_t *ids,
+                 float *weights, void *stream);
+/* grad_logits: DEVICE [tokens][experts] of dtype. */
+int bifeat_route_backward(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens, const bifeat_route_options *options,
+                          const int32_t *ids, const float *grad_weights, void *grad_logits, void *stream);
 
 const char *bifeat_strerror(int status);
 

@@ -10,8 +10,10 @@ from .binding import (Quantizer, Scheme, BifeatError, load_library, library_path
                       UNIFORM, LOG, VQ, VQ_L2, VQ_COSINE, F32, F16, BF16,
                       OK, EINVAL, ENOTFIT, EHIP, ENOTSUP, ELIMIT, FIT_AGAIN)
 from .cache import PagedCache
+from .linear import PackedLinear
+from .routing import route
 
 __all__ = ["Quantizer", "Scheme", "BifeatError", "load_library", "library_path",
-           "PagedCache", "aggregate_rows", "scale_profile", "check_lists",
+           "PagedCache", "PackedLinear", "route", "aggregate_rows", "scale_profile", "check_lists",
            "UNIFORM", "LOG", "VQ", "VQ_L2", "VQ_COSINE", "F32", "F16", "BF16",
            "OK", "EINVAL", "ENOTFIT", "EHIP", "ENOTSUP", "ELIMIT", "FIT_AGAIN"]

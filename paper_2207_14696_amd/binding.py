@@ -5,6 +5,7 @@ calls (``cache.py``) without ``out`` go through a native module (``csrc/calls.cp
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 import warnings
 from dataclasses import dataclass
@@ -48,6 +49,24 @@ class _CHeadRows(C.Structure):
 class _CAttendOptions(C.Structure):
     _fields_ = [("scale", C.c_float), ("softcap", C.c_float), ("window", C.c_int64),
                 ("prefix", C.c_void_p), ("slopes", C.c_void_p)]
+
+
+class _CTurn(C.Structure):
+    _fields_ = [("frequencies", C.c_void_p), ("pairs", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_double)]
+
+
+class _CLinearSpec(C.Structure):
+    _fields_ = [("out_features", C.c_int32), ("in_features", C.c_int32), ("group", C.c_int32), ("experts", C.c_int32)]
+
+
+class _CExpertRows(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("token_stride", C.c_int64), ("choice_stride", C.c_int64), ("ids", C.c_void_p),
+                ("weights", C.c_void_p), ("tokens", C.c_int64), ("choices", C.c_int32)]
+
+
+class _CRouteOptions(C.Structure):
+    _fields_ = [("experts", C.c_int32), ("choices", C.c_int32), ("sigmoid", C.c_int32), ("groups", C.c_int32), ("top_groups", C.c_int32),
+                ("group_two", C.c_int32), ("renormalise", C.c_int32), ("scale", C.c_double), ("bias", C.c_void_p)]
 
 
 @dataclass(frozen=True)
@@ -119,6 +138,18 @@ _SIGNATURES = {
                                     C.c_int32, C.c_void_p]),
     "bifeat_cache_attend": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.POINTER(_CHeadRows),
                                       C.c_int32, C.c_int32, C.POINTER(_CAttendOptions), C.c_void_p, C.c_void_p]),
+    "bifeat_cache_append": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int64, C.POINTER(_CCacheBatch), C.POINTER(_CHeadRows), C.c_int32,
+                                      C.POINTER(_CHeadRows), C.POINTER(_CHeadRows), C.c_int32, C.POINTER(_CTurn), C.c_void_p, C.c_void_p]),
+    "bifeat_linear_bytes": (C.c_int64, [C.POINTER(_CLinearSpec)]),
+    "bifeat_linear_pack": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
+    "bifeat_linear_unpack": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bifeat_linear_multiply": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]),
+    "bifeat_linear_experts_workspace": (C.c_int64, [C.POINTER(_CLinearSpec), C.POINTER(_CExpertRows)]),
+    "bifeat_linear_experts": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.POINTER(_CExpertRows), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
+                                        C.c_void_p]),
+    "bifeat_route": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.POINTER(_CRouteOptions), C.c_void_p, C.c_void_p, C.c_void_p]),
+    "bifeat_route_backward": (C.c_int, [C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.POINTER(_CRouteOptions), C.c_void_p, C.c_void_p, C.c_void_p,
+                                        C.c_void_p]),
     "bifeat_strerror": (C.c_char_p, [C.c_int]),
     "bifeat_set_option": (C.c_int, [C.c_void_p, C.c_char_p, C.c_int]),
 }
@@ -188,6 +219,41 @@ def _dev_ptr(t, dtypes=None) -> int:
     if dtypes is not None and t.dtype not in dtypes:
         raise ValueError(f"unexpected dtype {t.dtype}")
     return t.data_ptr()
+
+
+def _dtype_code(dtype) -> int:
+    import torch
+    if dtype == torch.float16:
+        return F16
+    if dtype == torch.bfloat16:
+        return BF16
+    if dtype == torch.float32:
+        return F32
+    raise ValueError(f"unexpected dtype {dtype}: float32, float16 or bfloat16")
+
+
+def _on_current_device(t, *others) -> None:
+    import torch
+    if not t.is_cuda or t.device.index != torch.cuda.current_device() or any(o is not None and o.device != t.device for o in others):
+        raise ValueError("all tensors must be on the current CUDA device")
+
+
+@functools.lru_cache(maxsize=None)
+def _without_backward():
+    """A function of autograd's graph around a call that has no backward pass: going back through it raises, and says why."""
+    import torch
+
+    class WithoutBackward(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, why, call, *tensors):
+            ctx.why = why
+            return call()
+
+        @staticmethod
+        def backward(ctx, grad):
+            raise NotImplementedError(ctx.why)
+
+    return WithoutBackward
 
 
 def _np_ptr(a):

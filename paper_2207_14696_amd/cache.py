@@ -5,22 +5,10 @@ it is built; what it leaves goes through ctypes, behind the checks here."""
 from __future__ import annotations
 
 import ctypes as C
-import functools
 import math
 
 from . import binding as _b
-from .binding import BF16, EINVAL, F16, F32, _check, _dev_ptr, _stream, load_library
-
-
-def _type(dtype) -> int:
-    import torch
-    if dtype == torch.float16:
-        return F16
-    if dtype == torch.bfloat16:
-        return BF16
-    if dtype == torch.float32:
-        return F32
-    raise ValueError(f"unexpected dtype {dtype}: float32, float16 or bfloat16")
+from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _stream, _without_backward, load_library
 
 
 def _head_rows(t, heads: int, head_dim: int, name: str):
@@ -32,23 +20,6 @@ def _head_rows(t, heads: int, head_dim: int, name: str):
     if s[2] != 1 and head_dim != 1:
         raise ValueError(f"{name}: a head's columns must be contiguous")
     return _b._CHeadRows(t.data_ptr(), s[0], s[1])
-
-
-@functools.lru_cache(maxsize=None)
-def _without_backward():
-    """A function of autograd's graph around a call that has no backward pass: going back through it raises."""
-    import torch
-
-    class WithoutBackward(torch.autograd.Function):
-        @staticmethod
-        def forward(ctx, q, call):
-            return call()
-
-        @staticmethod
-        def backward(ctx, grad):
-            raise NotImplementedError("PagedCache.attend has no backward pass: the keys and values behind it are codes")
-
-    return WithoutBackward
 
 
 class PagedCache:
@@ -140,14 +111,42 @@ class PagedCache:
             raise ValueError("k and v must be alike")
         ptr, count = self._pages(pages, k, v, tables, lengths, indptr)
         _check(self._lib.bifeat_cache_write(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, k.shape[0])),
-                                            C.byref(rows[0]), C.byref(rows[1]), _type(k.dtype), _stream()))
+                                            C.byref(rows[0]), C.byref(rows[1]), _dtype_code(k.dtype), _stream()))
+
+    def append(self, pages, q, k, v, frequencies, tables, lengths, indptr=None, interleaved: bool = False, scale: float = 1.0):
+        """``write`` of keys that are turned to their positions on the way; returns the queries, q [tokens, query heads, head_dim], turned
+        with them (None for q None).  ``frequencies`` float32 [pairs], pairs <= head_dim / 2: radians a position of the column pairs
+        (i, i + pairs), or (2 i, 2 i + 1) where ``interleaved``; columns from 2 * pairs on stay as they are.  ``scale``: of the turned
+        columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q requires one,
+        going back through the output raises."""
+        import torch
+        if q is not None and q.requires_grad and torch.is_grad_enabled():
+            return _without_backward().apply("PagedCache.append has no backward pass",
+                                             lambda: self.append(pages, q.detach(), k, v, frequencies, tables, lengths, indptr, interleaved, scale), q)
+        rows = [_head_rows(t, self.heads, self.head_dim, name) for t, name in ((k, "k"), (v, "v"))]
+        if k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must be alike")
+        if frequencies.dim() != 1:
+            raise ValueError("frequencies must be [pairs]")
+        out, heads, q_rows = None, 0, _b._CHeadRows(None, 0, 0)
+        if q is not None:
+            if q.dim() != 3 or q.shape[0] != k.shape[0] or q.dtype != k.dtype:
+                raise ValueError("q must be [tokens, query heads, head_dim] of k's tokens and type")
+            heads = q.shape[1]
+            q_rows = _head_rows(q, heads, self.head_dim, "q")
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        ptr, count = self._pages(pages, k, v, q, frequencies, tables, lengths, indptr)
+        turn = _b._CTurn(_dev_ptr(frequencies, (torch.float32,)), frequencies.shape[0], bool(interleaved), scale)
+        _check(self._lib.bifeat_cache_append(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, k.shape[0])), C.byref(q_rows), heads,
+                                             C.byref(rows[0]), C.byref(rows[1]), _dtype_code(k.dtype), C.byref(turn), _dev_ptr(out), _stream()))
+        return out
 
     def read(self, pages, tables, lengths, tokens: int, indptr=None, dtype=None, out=None):
         """Keys and values of the last tokens of each sequence, ``tokens`` in all, as they stand in
         the cache: two [tokens, heads, head_dim] of ``dtype`` (float32)."""
         import torch
         if out is None and (calls := _b._calls or _b._load_calls()):
-            r = calls.cache_read(*self._read, pages, tokens, _type(dtype or torch.float32), tables, lengths, indptr)
+            r = calls.cache_read(*self._read, pages, tokens, _dtype_code(dtype or torch.float32), tables, lengths, indptr)
             if r is not None:
                 if r.__class__ is int:
                     _check(r)
@@ -160,7 +159,7 @@ class PagedCache:
             raise ValueError("out must be two [tokens, heads, head_dim] of one dtype")
         ptr, count = self._pages(pages, *out, tables, lengths, indptr)
         _check(self._lib.bifeat_cache_read(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, tokens)),
-                                           _dev_ptr(out[0]), _dev_ptr(out[1]), _type(out[0].dtype), _stream()))
+                                           _dev_ptr(out[0]), _dev_ptr(out[1]), _dtype_code(out[0].dtype), _stream()))
         return out
 
     def attend(self, pages, q, tables, lengths, indptr=None, scale=None, softcap: float = 0.0, window: int = 0, prefix=None,
@@ -183,7 +182,8 @@ class PagedCache:
             if out is not None:
                 raise ValueError("attend has no backward pass: no out where q requires a gradient")
             args = (tables, lengths, indptr, scale, softcap, window, prefix, slopes)
-            return _without_backward().apply(q, lambda: self.attend(pages, q.detach(), *args))
+            return _without_backward().apply("PagedCache.attend has no backward pass: the keys and values behind it are codes",
+                                             lambda: self.attend(pages, q.detach(), *args), q)
         if q.dim() != 3:
             raise ValueError("q must be [tokens, query heads, head_dim]")
         heads = q.shape[1]
@@ -200,5 +200,5 @@ class PagedCache:
         options = _b._CAttendOptions(scale, softcap, window,
                                      _dev_ptr(prefix, (torch.int64,)), _dev_ptr(slopes, (torch.float32,)))
         _check(self._lib.bifeat_cache_attend(self._h, ptr, count, C.byref(self._batch(tables, lengths, indptr, q.shape[0])),
-                                             C.byref(rows), heads, _type(q.dtype), C.byref(options), _dev_ptr(out), _stream()))
+                                             C.byref(rows), heads, _dtype_code(q.dtype), C.byref(options), _dev_ptr(out), _stream()))
         return out

@@ -140,6 +140,20 @@ struct AttendCall {
     hipStream_t s;
 };
 
+struct AppendCall {
+    HeadRows q;
+    int query_heads;  // 0: no queries
+    HeadRows k, v;
+    int bits, dtype;
+    const float *frequencies;
+    int pairs;
+    bool interleaved;
+    double scale;
+    void *out;
+    hipStream_t s;
+};
+
+hipError_t launch_cache_append(const CachePages &c, const CacheBatch &b, const AppendCall &a);
 hipError_t launch_cache_write(const CachePages &c, const CacheBatch &b, const HeadRows &k, const HeadRows &v, int bits, int dtype,
                               hipStream_t s);
 hipError_t launch_cache_read(const CachePages &c, const CacheBatch &b, void *k, void *v, int bits, int dtype, hipStream_t s);

@@ -132,6 +132,26 @@ int bifeat_cache_write(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const
     return BIFEAT_OK;
 }
 
+int bifeat_cache_append(bifeat_cache *c, uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch, const bifeat_head_rows *q,
+                        int32_t query_heads, const bifeat_head_rows *k, const bifeat_head_rows *v, int32_t dtype,
+                        const bifeat_turn *turn, void *out, void *stream) {
+    if (!c || query_heads < 0 || query_heads > 65536) return BIFEAT_EINVAL;
+    if (int rc = common(c, pages, num_pages, batch, query_heads + 2 * c->spec.heads, dtype)) return rc;
+    if (!turn || turn->pairs < 0 || turn->pairs > c->spec.head_dim / 2 || (turn->interleaved != 0 && turn->interleaved != 1) ||
+        !isfinite(turn->scale) || (uintptr_t)turn->frequencies % 4)
+        return BIFEAT_EINVAL;
+    if (batch->tokens == 0) return BIFEAT_OK;
+    if (!rows_ok(k, dtype) || !rows_ok(v, dtype) || (turn->pairs > 0 && !turn->frequencies)) return BIFEAT_EINVAL;
+    if (query_heads > 0 && (!rows_ok(q, dtype) || !out || (uintptr_t)out % type_bytes(dtype))) return BIFEAT_EINVAL;
+    const bf::CacheBatch b = batch_of(batch);
+    if (c->opt_validate)
+        if (int rc = check(c, num_pages, b, (hipStream_t)stream)) return rc;
+    const bf::AppendCall a{query_heads ? rows_of(q) : bf::HeadRows{}, query_heads, rows_of(k), rows_of(v), c->spec.bits, dtype,
+                           turn->frequencies, turn->pairs, turn->interleaved != 0, turn->scale, out, (hipStream_t)stream};
+    BF_HIP(bf::launch_cache_append(pages_of(c, pages), b, a));
+    return BIFEAT_OK;
+}
+
 int bifeat_cache_read(bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch, void *k, void *v,
                       int32_t dtype, void *stream) {
     if (int rc = common(c, pages, num_pages, batch, c ? 2 * c->spec.heads : 1, dtype)) return rc;

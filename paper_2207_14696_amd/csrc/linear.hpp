@@ -1,0 +1,138 @@
+// Products with matrices in 4 bits: what their translation units share.
+//
+// With codes q, scale s and minimum m of each group g of a row's columns
+//   y = sum_g  s_g sum_{k in g} x_k q_k + m_g sum_{k in g} x_k
+//     = sum_g  s_g sum_{k in g} x_k (16 + q_k) + (m_g - 16 s_g) sum_{k in g} x_k.
+// 16 + q is a 16-bit float whose highest mantissa bits are q: two codes become two operands of a matrix product by a shift and one
+// bitwise instruction, exactly.  The products of a group are summed in fp32 by the matrix cores, the sum of x beside them (a product with
+// ones), and two fused multiply-adds a group bring them to the result's.  Neither a weight nor a partial sum is ever rounded to 16 bits.
+#pragma once
+
+#include "cache.hpp"
+
+namespace bf {
+
+struct Matrices {
+    const uint8_t *packed;
+    int64_t bytes;  // of one
+    int N, K;
+    int rows, blocks;  // of 16, and of 128 columns
+    int experts;
+    __host__ __device__ int64_t code_bytes() const { return (int64_t)rows * blocks * 1024; }
+};
+
+typedef float Sum4 __attribute__((ext_vector_type(4)));
+
+// ---- operands of the matrix products.  Pieces: how many of them are a row's value together
+template <typename T> struct Operand;
+template <> struct Operand<Half16> {
+    typedef _Float16 Eight __attribute__((ext_vector_type(8)));
+    static constexpr int kPieces = 1;
+    static constexpr uint32_t kMask = 0x03c003c0u, kSixteen = 0x4c004c00u, kOnes = 0x3c003c00u;
+    static constexpr int kShift[4] = {6, 2, -2, -6};
+    static __device__ Sum4 product(Eight a, Eight b, Sum4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+};
+template <> struct Operand<Brain16> {
+    typedef __bf16 Eight __attribute__((ext_vector_type(8)));
+    static constexpr int kPieces = 1;
+    static constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u, kOnes = 0x3f803f80u;
+    static constexpr int kShift[4] = {3, -1, -5, -9};
+    static __device__ Sum4 product(Eight a, Eight b, Sum4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+};
+// a 32-bit number is three bfloat16 together: 8 bits of it each
+template <> struct Operand<float> : Operand<Brain16> {
+    static constexpr int kPieces = 3;
+};
+
+// The eight codes of a word as 16 + code.
+template <typename T>
+__device__ inline typename Operand<T>::Eight sixteen_and_codes(uint32_t w) {
+    typedef Operand<T> O;
+    uint32_t __attribute__((ext_vector_type(4))) r;
+#pragma unroll
+    for (int j = 0; j < 4; j++) r[j] = ((O::kShift[j] > 0 ? w << (O::kShift[j] & 31) : w >> (-O::kShift[j] & 31)) & O::kMask) | O::kSixteen;
+    return __builtin_bit_cast(typename O::Eight, r);
+}
+template <typename T>
+__device__ inline typename Operand<T>::Eight ones() {
+    const uint32_t __attribute__((ext_vector_type(4))) r = {Operand<T>::kOnes, Operand<T>::kOnes, Operand<T>::kOnes, Operand<T>::kOnes};
+    return __builtin_bit_cast(typename Operand<T>::Eight, r);
+}
+
+// Eight columns of a row of x as they lie in memory, those from `left` on as zeros.
+template <typename T>
+struct Columns {
+    uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+__device__ inline Columns<T> load_columns(const T *p, int left) {
+    Columns<T> c;
+    if (left >= 8) {
+        const Eight<T> e = *reinterpret_cast<const Eight<T> *>(p);
+        __builtin_memcpy(c.w, &e, sizeof(c));
+    } else {
+        T v[8] = {};
+#pragma unroll
+        for (int i = 0; i < 8; i++)
+            if (i < left) v[i] = p[i];
+        __builtin_memcpy(c.w, v, sizeof(c));
+    }
+    return c;
+}
+// ... and as operands
+template <typename T>
+__device__ inline void to_operands(const Columns<T> &c, typename Operand<T>::Eight (&x)[Operand<T>::kPieces]) {
+    if constexpr (Operand<T>::kPieces == 1) {
+        x[0] = __builtin_bit_cast(typename Operand<T>::Eight, c);
+    } else {
+        uint32_t __attribute__((ext_vector_type(4))) r[3];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            // (what is left after the highest 8 bits, and after the next 8, is exact in 32 bits)
+            uint32_t piece[3][2];
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                float left = __builtin_bit_cast(float, c.w[2 * j + h]);
+#pragma unroll
+                for (int p = 0; p < 3; p++) {
+                    piece[p][h] = __builtin_bit_cast(uint32_t, left) & 0xffff0000u;
+                    left -= __builtin_bit_cast(float, piece[p][h]);
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 3; p++) r[p][j] = piece[p][0] >> 16 | piece[p][1];
+        }
+#pragma unroll
+        for (int p = 0; p < 3; p++) x[p] = __builtin_bit_cast(typename Operand<T>::Eight, r[p]);
+    }
+}
+
+// ---- the rows of a call
+struct XRows {
+    const void *x;
+    int64_t token_stride, choice_stride;
+    int choices;  // rows of a token (1 without experts)
+    int64_t count;
+    void *out;
+};
+
+// Where rows are dealt to experts, the pairs of a token and one of its choices lie in `order` expert by expert, and a tile is up to
+// kTile of one expert's.
+struct Tile {
+    int expert, first, count, unused;  // expert -1: pairs that name none
+};
+struct Deal {
+    const int *tiles_count;
+    const Tile *tiles;
+    const int *order;
+};
+
+hipError_t launch_linear_pack(const Matrices &m, int group, const void *weight, int dtype, uint8_t *packed, hipStream_t s);
+hipError_t launch_linear_unpack(const Matrices &m, int group, float *weight, hipStream_t s);
+// deal null: one matrix, rows as they are.  to_float: out is fp32 whatever the rows' type.
+hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
+hipError_t launch_linear_deal(const int *ids, int pairs, int experts, int tile, int *tiles_count, Tile *tiles, int *order, hipStream_t s);
+hipError_t launch_linear_join(const float *products, const int *ids, const float *weights, int64_t tokens, int choices, int experts, int N, int dtype, void *out,
+                              hipStream_t s);
+
+}  // namespace bf

@@ -1,0 +1,104 @@
+// Entry points of the products with matrices in 4 bits: argument checks, and dispatch to the kernels of linear_*.hip.
+#include <algorithm>
+
+#include "linear.hpp"
+
+#define BF_HIP(call)                                                   \
+    do {                                                               \
+        hipError_t e_ = (call);                                        \
+        if (e_ != hipSuccess) return bf::record_hip_error(e_, #call);  \
+    } while (0)
+
+namespace {
+
+bool spec_ok(const bifeat_linear_spec *s) {
+    return s && s->out_features >= 1 && s->out_features <= (1 << 20) && s->in_features >= 1 && s->in_features <= (1 << 20) &&
+           (s->group == 32 || s->group == 64 || s->group == 128) && s->experts >= 1 && s->experts <= 1024;
+}
+
+bool type_ok(int32_t d) { return d == BIFEAT_F32 || d == BIFEAT_F16 || d == BIFEAT_BF16; }
+bool data_ok(const void *p, int32_t dtype) { return p && (uintptr_t)p % (dtype == BIFEAT_F32 ? 4 : 2) == 0; }
+
+bf::Matrices matrices_of(const bifeat_linear_spec *s, const uint8_t *packed) {
+    const int rows = (s->out_features + 15) / 16, blocks = (s->in_features + 127) / 128;
+    return {packed, (int64_t)rows * blocks * (1024 + 64 * (128 / s->group)), s->out_features, s->in_features, rows, blocks, s->experts};
+}
+
+bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
+    return r && r->tokens >= 0 && r->choices >= 1 && r->choices <= 64 && r->token_stride >= 0 && r->choice_stride >= 0 &&
+           r->tokens <= (INT32_MAX - 64) / r->choices;
+}
+
+// The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, 32-bit products.
+struct Room {
+    int tile;
+    int64_t most_tiles, order, products, bytes;
+};
+Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
+    Room o;
+    const int64_t pairs = r->tokens * r->choices;
+    o.tile = 16;
+    o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
+    o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
+    o.products = o.order + (pairs + 3) / 4 * 16;
+    o.bytes = o.products + (r->weights ? pairs * s->out_features * 4 : 0);
+    return o;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t bifeat_linear_bytes(const bifeat_linear_spec *spec) { return spec_ok(spec) ? matrices_of(spec, nullptr).bytes : BIFEAT_EINVAL; }
+
+int bifeat_linear_pack(const bifeat_linear_spec *spec, const void *weight, int32_t dtype, uint8_t *packed, void *stream) {
+    if (!spec_ok(spec) || !type_ok(dtype) || !data_ok(weight, dtype) || !packed || (uintptr_t)packed % 16) return BIFEAT_EINVAL;
+    BF_HIP(bf::launch_linear_pack(matrices_of(spec, packed), spec->group, weight, dtype, packed, (hipStream_t)stream));
+    return BIFEAT_OK;
+}
+
+int bifeat_linear_unpack(const bifeat_linear_spec *spec, const uint8_t *packed, float *weight, void *stream) {
+    if (!spec_ok(spec) || !data_ok(weight, BIFEAT_F32) || !packed || (uintptr_t)packed % 16) return BIFEAT_EINVAL;
+    BF_HIP(bf::launch_linear_unpack(matrices_of(spec, packed), spec->group, weight, (hipStream_t)stream));
+    return BIFEAT_OK;
+}
+
+int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed, const void *x, int64_t row_stride, int64_t rows,
+                           int32_t dtype, void *out, void *stream) {
+    if (!spec_ok(spec) || spec->experts != 1 || !type_ok(dtype) || rows < 0 || rows > INT32_MAX - 64 || row_stride < 0) return BIFEAT_EINVAL;
+    if (rows == 0) return BIFEAT_OK;
+    if (!packed || (uintptr_t)packed % 16 || !data_ok(x, dtype) || !data_ok(out, dtype)) return BIFEAT_EINVAL;
+    BF_HIP(bf::launch_linear_few(matrices_of(spec, packed), spec->group, {x, row_stride, 0, 1, rows, out}, nullptr, 0, dtype, false,
+                                 (hipStream_t)stream));
+    return BIFEAT_OK;
+}
+
+int64_t bifeat_linear_experts_workspace(const bifeat_linear_spec *spec, const bifeat_expert_rows *rows) {
+    return spec_ok(spec) && rows_ok(spec, rows) ? room_of(spec, rows).bytes : (int64_t)BIFEAT_EINVAL;
+}
+
+int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed, const bifeat_expert_rows *r, int32_t dtype, void *out,
+                          void *workspace, int64_t workspace_bytes, void *stream) {
+    if (!spec_ok(spec) || !type_ok(dtype) || !rows_ok(spec, r)) return BIFEAT_EINVAL;
+    if (r->tokens == 0) return BIFEAT_OK;
+    if (!packed || (uintptr_t)packed % 16 || !data_ok(r->x, dtype) || !data_ok(out, dtype) || !r->ids || (uintptr_t)r->ids % 4 ||
+        (uintptr_t)r->weights % 4 || !workspace || (uintptr_t)workspace % 16)
+        return BIFEAT_EINVAL;
+    const Room room = room_of(spec, r);
+    if (workspace_bytes < room.bytes) return BIFEAT_EINVAL;
+    const bf::Matrices m = matrices_of(spec, packed);
+    const hipStream_t s = (hipStream_t)stream;
+    const int64_t pairs = r->tokens * r->choices;
+    uint8_t *w = static_cast<uint8_t *>(workspace);
+    int *tiles_count = reinterpret_cast<int *>(w), *order = reinterpret_cast<int *>(w + room.order);
+    bf::Tile *tiles = reinterpret_cast<bf::Tile *>(w + 16);
+    float *products = reinterpret_cast<float *>(w + room.products);
+    BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, tiles_count, tiles, order, s));
+    const bf::Deal deal{tiles_count, tiles, order};
+    const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out};
+    BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, r->weights != nullptr, s));
+    if (r->weights) BF_HIP(bf::launch_linear_join(products, r->ids, r->weights, r->tokens, r->choices, spec->experts, m.N, dtype, out, s));
+    return BIFEAT_OK;
+}
+
+}  // extern "C"
