@@ -528,10 +528,10 @@ int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages
  *   group that holds an infinity or a NaN, or whose range is not finite in bfloat16, gets scale =
  *   minimum = NaN: its row of the matrix gives NaN, and no other.
  * multiply: out[t][n] = sum_k x[t][k] weight[n][k], for rows x of any number.  16-bit x enter
- *   the matrix cores as they are, 32-bit ones in three pieces that are them together, codes as
- *   16 + code, all exact; sums are fp32: off by about 2^-20 of the sum of |x| scale 16 (fewer than
- *   4096 columns), then rounded to x's type.  A row with an infinity or a NaN, or with a group whose sum
- *   of |x| passes 2^122, gives infinities and NaN; other rows are as they were without it.
+ *   the matrix cores as they are, codes with them as 16 + code; 32-bit x in three pieces that are
+ *   them together, codes as they are: all exact.  Sums are fp32, then rounded to x's type.  A row of
+ *   x with an infinity or a NaN gives infinities and NaN, as may one with a group whose sum of
+ *   |x|, or that times 16 scales or the minimum, passes 2^122; other rows are as they were without it.
  * experts: `experts` matrices of one size, and tokens with `choices` of them each.  out[t][j] =
  *   x[t] or x[t][j] times matrix ids[t][j]; with weights the sum over j of weights[t][j] times
  *   that (in fp32, j ascending).  An id outside [0, experts) names none: its product is zeros,

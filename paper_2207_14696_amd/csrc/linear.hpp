@@ -4,7 +4,8 @@
 //   y = sum_g  s_g sum_{k in g} x_k q_k + m_g sum_{k in g} x_k
 //     = sum_g  s_g sum_{k in g} x_k (16 + q_k) + (m_g - 16 s_g) sum_{k in g} x_k.
 // 16 + q is a 16-bit float whose highest mantissa bits are q: two codes become two operands of a matrix product by a shift and one
-// bitwise instruction, exactly.  The products of a group are summed in fp32 by the matrix cores, the sum of x beside them (a product with
+// bitwise instruction, exactly.  With rows of 32 bits the codes are taken as they are (twice the instructions, beside three products): the 16 would
+// bring sums three times as large, and cost them 1.5 bits.  The products of a group are summed in fp32 by the matrix cores, the sum of x beside them (a product with
 // ones), and two fused multiply-adds a group bring them to the result's.  Neither a weight nor a partial sum is ever rounded to 16 bits.
 #pragma once
 
@@ -28,6 +29,7 @@ template <typename T> struct Operand;
 template <> struct Operand<Half16> {
     typedef _Float16 Eight __attribute__((ext_vector_type(8)));
     static constexpr int kPieces = 1;
+    static constexpr float kMore = 16.f;  // of a code's operand than the code
     static constexpr uint32_t kMask = 0x03c003c0u, kSixteen = 0x4c004c00u, kOnes = 0x3c003c00u;
     static constexpr int kShift[4] = {6, 2, -2, -6};
     static __device__ Sum4 product(Eight a, Eight b, Sum4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
@@ -35,6 +37,7 @@ template <> struct Operand<Half16> {
 template <> struct Operand<Brain16> {
     typedef __bf16 Eight __attribute__((ext_vector_type(8)));
     static constexpr int kPieces = 1;
+    static constexpr float kMore = 16.f;
     static constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u, kOnes = 0x3f803f80u;
     static constexpr int kShift[4] = {3, -1, -5, -9};
     static __device__ Sum4 product(Eight a, Eight b, Sum4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
@@ -42,13 +45,25 @@ template <> struct Operand<Brain16> {
 // a 32-bit number is three bfloat16 together: 8 bits of it each
 template <> struct Operand<float> : Operand<Brain16> {
     static constexpr int kPieces = 3;
+    static constexpr float kMore = 0.f;
 };
 
-// The eight codes of a word as 16 + code.
+// The eight codes of a word, each with kMore.
 template <typename T>
-__device__ inline typename Operand<T>::Eight sixteen_and_codes(uint32_t w) {
+__device__ inline typename Operand<T>::Eight code_operands(uint32_t w) {
     typedef Operand<T> O;
     uint32_t __attribute__((ext_vector_type(4))) r;
+    if constexpr (O::kMore == 0.f) {
+        // (a code is a 32-bit float of which bfloat16 is the upper half)
+        const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            const uint32_t from = j % 2 ? odd : even;  // nibble j, and the one 16 bits further
+            const float low = (float)(from >> 8 * (j / 2) & 0xffu), high = (float)(from >> (16 + 8 * (j / 2)) & 0xffu);
+            r[j] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, high), __builtin_bit_cast(uint32_t, low), 0x07060302u);
+        }
+        return __builtin_bit_cast(typename O::Eight, r);
+    }
 #pragma unroll
     for (int j = 0; j < 4; j++) r[j] = ((O::kShift[j] > 0 ? w << (O::kShift[j] & 31) : w >> (-O::kShift[j] & 31)) & O::kMask) | O::kSixteen;
     return __builtin_bit_cast(typename O::Eight, r);

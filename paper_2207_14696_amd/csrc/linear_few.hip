@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
             for (int w = 4 / GPB * g; w < 4 / GPB * (g + 1); w++) {
                 typename O::Eight a[R];
 #pragma unroll
-                for (int r = 0; r < R; r++) a[r] = sixteen_and_codes<T>(w == 0 ? codes[r].x : w == 1 ? codes[r].y : w == 2 ? codes[r].z : codes[r].w);
+                for (int r = 0; r < R; r++) a[r] = code_operands<T>(w == 0 ? codes[r].x : w == 1 ? codes[r].y : w == 2 ? codes[r].z : codes[r].w);
 #pragma unroll
                 for (int t = 0; t < TB; t++) {
                     typename O::Eight b[P];
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
                 for (int i = 0; i < 4; i++) {
                     const uint32_t word = i == 0 ? level[r][g].x : i == 1 ? level[r][g].y : i == 2 ? level[r][g].z : level[r][g].w;
                     const float scale = __builtin_bit_cast(float, word << 16), low = __builtin_bit_cast(float, word & 0xffff0000u);
-                    const float rest = fmaf(-16.f, scale, low);
+                    const float rest = fmaf(-O::kMore, scale, low);
 #pragma unroll
                     for (int t = 0; t < TB; t++) total[r][t][i] = fmaf(scale, sum[r][t][i], fmaf(rest, of_x[t][i], total[r][t][i]));
                 }

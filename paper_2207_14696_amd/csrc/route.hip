@@ -62,12 +62,12 @@ __device__ inline void scores_of(const T *row, const Options &o, int lane, doubl
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; i++) {
-        score[i] = lane + 64 * i < o.experts ? exp(x[i] - most) : 0.0;
+        score[i] = most == -INFINITY ? 0.0 : exp(x[i] - most);  // (all masked: no expert has a score)
         sum += score[i];
     }
     sum = wave_sum(sum);
 #pragma unroll
-    for (int i = 0; i < EPL; i++) score[i] /= sum;
+    for (int i = 0; i < EPL; i++) score[i] = sum != 0.0 ? score[i] / sum : 0.0;
 }
 
 template <typename T, int EPL>
