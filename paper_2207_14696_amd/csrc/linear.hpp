@@ -74,24 +74,49 @@ __device__ inline typename Operand<T>::Eight ones() {
     return __builtin_bit_cast(typename Operand<T>::Eight, r);
 }
 
-// Eight columns of a row of x as they lie in memory, those from `left` on as zeros.
+// Eight columns of a row of x as they lie in memory.
 template <typename T>
 struct Columns {
     uint32_t w[2 * sizeof(T)];
 };
 template <typename T>
-__device__ inline Columns<T> load_columns(const T *p, int left) {
+__device__ inline Columns<T> load_columns(const T *p) {
     Columns<T> c;
-    if (left >= 8) {
-        const Eight<T> e = *reinterpret_cast<const Eight<T> *>(p);
-        __builtin_memcpy(c.w, &e, sizeof(c));
-    } else {
-        T v[8] = {};
+    const Eight<T> e = *reinterpret_cast<const Eight<T> *>(p);
+    __builtin_memcpy(c.w, &e, sizeof(c));
+    return c;
+}
+// ... from column `at` of a row of K >= 8, those past the end as zeros: the row's last eight, moved down.
+template <typename T>
+__device__ inline Columns<T> load_last_columns(const T *row, int at, int K) {
+    const int from = at < K - 8 ? at : K - 8, past = at < K ? at - from : 8;
+    Columns<T> c = load_columns(row + from);
+    constexpr int kWords = 2 * sizeof(T), kPerWord = 4 / sizeof(T);
 #pragma unroll
-        for (int i = 0; i < 8; i++)
-            if (i < left) v[i] = p[i];
-        __builtin_memcpy(c.w, v, sizeof(c));
-    }
+    for (int by = kWords; by >= 1; by /= 2)
+#pragma unroll
+        for (int i = 0; i < kWords; i++) c.w[i] = past & (by * kPerWord) ? (i + by < kWords ? c.w[i + by < kWords ? i + by : 0] : 0u) : c.w[i];
+    if constexpr (kPerWord == 2)
+#pragma unroll
+        for (int i = 0; i < kWords; i++) c.w[i] = past & 1 ? c.w[i] >> 16 | (i + 1 < kWords ? c.w[i + 1 < kWords ? i + 1 : 0] << 16 : 0u) : c.w[i];
+    return c;
+}
+// ... of a row of K < 8 columns.
+template <typename T>
+__device__ inline Columns<T> load_short_columns(const T *row, int K) {
+    Columns<T> c;
+    T v[8] = {};
+#pragma unroll
+    for (int i = 0; i < 7; i++)
+        if (i < K) v[i] = row[i];
+    __builtin_memcpy(c.w, v, sizeof(c));
+    return c;
+}
+template <typename T>
+__device__ inline Columns<T> no_columns() {
+    Columns<T> c;
+#pragma unroll
+    for (uint32_t &w : c.w) w = 0;
     return c;
 }
 // ... and as operands
@@ -146,6 +171,9 @@ hipError_t launch_linear_pack(const Matrices &m, int group, const void *weight, 
 hipError_t launch_linear_unpack(const Matrices &m, int group, float *weight, hipStream_t s);
 // deal null: one matrix, rows as they are.  to_float: out is fp32 whatever the rows' type.
 hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
+// ... of K >= 8 columns, tiles of kManyRows
+constexpr int kManyRows = 128;
+hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
 hipError_t launch_linear_deal(const int *ids, int pairs, int experts, int tile, int *tiles_count, Tile *tiles, int *order, hipStream_t s);
 hipError_t launch_linear_join(const float *products, const int *ids, const float *weights, int64_t tokens, int choices, int experts, int N, int dtype, void *out,
                               hipStream_t s);

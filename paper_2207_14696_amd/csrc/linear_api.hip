@@ -37,7 +37,7 @@ struct Room {
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
     const int64_t pairs = r->tokens * r->choices;
-    o.tile = 16;
+    o.tile = pairs >= 32 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
     o.products = o.order + (pairs + 3) / 4 * 16;
@@ -68,8 +68,9 @@ int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed
     if (!spec_ok(spec) || spec->experts != 1 || !type_ok(dtype) || rows < 0 || rows > INT32_MAX - 64 || row_stride < 0) return BIFEAT_EINVAL;
     if (rows == 0) return BIFEAT_OK;
     if (!packed || (uintptr_t)packed % 16 || !data_ok(x, dtype) || !data_ok(out, dtype)) return BIFEAT_EINVAL;
-    BF_HIP(bf::launch_linear_few(matrices_of(spec, packed), spec->group, {x, row_stride, 0, 1, rows, out}, nullptr, 0, dtype, false,
-                                 (hipStream_t)stream));
+    const bf::XRows r{x, row_stride, 0, 1, rows, out};
+    const auto launch = rows > 64 && spec->in_features >= 8 ? bf::launch_linear_many : bf::launch_linear_few;
+    BF_HIP(launch(matrices_of(spec, packed), spec->group, r, nullptr, 0, dtype, false, (hipStream_t)stream));
     return BIFEAT_OK;
 }
 
@@ -96,7 +97,8 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, tiles_count, tiles, order, s));
     const bf::Deal deal{tiles_count, tiles, order};
     const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out};
-    BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, r->weights != nullptr, s));
+    const auto launch = room.tile == 16 ? bf::launch_linear_few : bf::launch_linear_many;
+    BF_HIP(launch(m, spec->group, x, &deal, (int)room.most_tiles, dtype, r->weights != nullptr, s));
     if (r->weights) BF_HIP(bf::launch_linear_join(products, r->ids, r->weights, r->tokens, r->choices, spec->experts, m.N, dtype, out, s));
     return BIFEAT_OK;
 }

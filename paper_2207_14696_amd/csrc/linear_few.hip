@@ -1,4 +1,6 @@
 // Products of few rows with matrices in 4 bits.
+#include <algorithm>
+
 #include "linear.hpp"
 
 namespace bf {
@@ -9,18 +11,19 @@ constexpr int kWaves = 8;
 // A workgroup takes R times 16 rows of the matrix and up to 16 TB rows of x; its waves take blocks of 128 columns in turn and add up what they have
 // in LDS at the end.  A lane's 16 bytes of a block are 32 codes of one row of the matrix, four operands as they are.
 template <typename T, int GPB, int TB, int R, bool DEALT, typename Out>
-__global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out) {
+__global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out, int tile0) {
     typedef Operand<T> O;
     constexpr int P = O::kPieces;
     __shared__ Sum4 part[kWaves][R * TB][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, quarter = lane / 16;
     const int row0 = blockIdx.x * R;
-    int64_t first = (int64_t)blockIdx.y * 16 * TB;
+    const int x_tile = tile0 + blockIdx.y;
+    int64_t first = (int64_t)x_tile * 16 * TB;
     int count;
     const uint8_t *packed = m.packed;
     if constexpr (DEALT) {
-        if ((int)blockIdx.y >= *deal.tiles_count) return;
-        const Tile t = deal.tiles[blockIdx.y];
+        if (x_tile >= *deal.tiles_count) return;
+        const Tile t = deal.tiles[x_tile];
         first = t.first;
         count = t.count;
         if (t.expert < 0) {
@@ -62,13 +65,15 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
                 level[r][g] = *reinterpret_cast<const uint4 *>(levels + (((int64_t)row * m.blocks + k) * GPB + g) * 16 + 4 * quarter);
         }
         Columns<T> columns[4][TB];
+        const auto load = [&](auto of) {
 #pragma unroll
-        for (int w = 0; w < 4; w++)
+            for (int w = 0; w < 4; w++)
 #pragma unroll
-            for (int t = 0; t < TB; t++) {
-                const int at = 128 * k + 32 * w + 8 * quarter;
-                columns[w][t] = load_columns(xr[t] + at, m.K - at);
-            }
+                for (int t = 0; t < TB; t++) columns[w][t] = of(xr[t], 128 * k + 32 * w + 8 * quarter);
+        };
+        if (128 * (k + 1) <= m.K) load([&](const T *row, int at) { return load_columns(row + at); });
+        else if (m.K >= 8) load([&](const T *row, int at) { return load_last_columns(row, at, m.K); });
+        else load([&](const T *row, int at) { return at == 0 ? load_short_columns(row, m.K) : no_columns<T>(); });
 #pragma unroll
         for (int g = 0; g < GPB; g++) {
             Sum4 sum[R][TB], of_x[TB];
@@ -130,7 +135,11 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
 template <typename T, typename Out, bool DEALT>
 void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int64_t tiles, hipStream_t s) {
     const auto launch = [&](auto kernel, int r, int64_t y) {
-        kernel<<<dim3((m.rows + r - 1) / r, (unsigned)y), 64 * kWaves, 0, s>>>(m, x, deal, (Out *)x.out);
+        const int row_tiles = (m.rows + r - 1) / r;
+        // (a launch has fewer than 2^32 threads, and a grid's second dimension than 2^16)
+        const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, (1 << 22) / row_tiles));
+        for (int64_t at = 0; at < y; at += most)
+            kernel<<<dim3(row_tiles, (unsigned)std::min(most, y - at)), 64 * kWaves, 0, s>>>(m, x, deal, (Out *)x.out, (int)at);
     };
     const bool wide = !DEALT && x.count > 16;
     const int64_t y = DEALT ? tiles : wide ? (x.count + 63) / 64 : (x.count + 15) / 16;
