@@ -395,9 +395,10 @@ int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *in
  *   queries turned with them.  Column pair i < pairs of a row of a token at position p is
  *   (i, i + pairs), or (2 i, 2 i + 1) where interleaved; with a = p * frequencies[i] it becomes
  *     (u, w) -> scale * (u cos a - w sin a),  scale * (u sin a + w cos a)
- *   and the columns from 2 * pairs on stay.  All of it in 64 bits; a key's columns are then
- *   rounded to fp32 and written as above, a query's to fp32 and to their type.  Values are
- *   written as they are.  Queries before their sequence's beginning come out as zeros.
+ *   and the columns from 2 * pairs on stay.  Angles, cosines and sines in 64 bits, as are the
+ *   turns of keys, which are then rounded to fp32 and written as above, and of 32-bit queries;
+ *   16-bit queries are turned in fp32 and rounded to their type.  Values are written as
+ *   they are.  Queries before their sequence's beginning come out as zeros.
  * read: x' = mn + code * scale.
  * attend: query token i of sequence b is at position p = lengths[b] - n_b + i, query head
  *   h reads cached head h / (query_heads / heads).  It sees position j < lengths[b] if

@@ -187,7 +187,7 @@ def _load_calls():
             from . import _calls as module
             _calls = module
         except ImportError as e:
-            warnings.warn(f"gather_dequant, gather_mean, gather_sum and the paged cache's calls go through ctypes, 5 us a call slower ({e}); "
+            warnings.warn(f"gather_dequant, gather_mean, gather_sum, the paged cache's calls, PackedLinear's and route go through ctypes, 5 us a call slower ({e}); "
                           "`python -m paper_2207_14696_amd.build` builds the native module", RuntimeWarning, stacklevel=3)
             _calls = False
     return _calls

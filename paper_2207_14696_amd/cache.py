@@ -47,13 +47,13 @@ class PagedCache:
         self._scale = 1.0 / math.sqrt(self.head_dim)
         # what the native module's calls begin with: entry point, handle, sizes
         rest = (h.value, self.page_bytes, self.heads, self.head_dim)
-        self._write, self._read, self._attend = (
+        self._write, self._read, self._attend, self._append = (
             (_b._address(fn),) + rest
-            for fn in (self._lib.bifeat_cache_write, self._lib.bifeat_cache_read, self._lib.bifeat_cache_attend))
+            for fn in (self._lib.bifeat_cache_write, self._lib.bifeat_cache_read, self._lib.bifeat_cache_attend, self._lib.bifeat_cache_append))
 
     def __del__(self):
         h, self._h = getattr(self, "_h", None), None
-        self._write = self._read = self._attend = (0,) * 5  # (no address of a destroyed object is left)
+        self._write = self._read = self._attend = self._append = (0,) * 5  # (no address of a destroyed object is left)
         if h:
             self._lib.bifeat_cache_destroy(h)
 
@@ -119,6 +119,12 @@ class PagedCache:
         (i, i + pairs), or (2 i, 2 i + 1) where ``interleaved``; columns from 2 * pairs on stay as they are.  ``scale``: of the turned
         columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q requires one,
         going back through the output raises."""
+        if calls := _b._calls or _b._load_calls():
+            r = calls.cache_append(*self._append, pages, q, k, v, frequencies, bool(interleaved), scale, tables, lengths, indptr)
+            if r is not None:
+                if r.__class__ is int:
+                    _check(r)
+                return None if r is True else r
         import torch
         if q is not None and q.requires_grad and torch.is_grad_enabled():
             return _without_backward().apply("PagedCache.append has no backward pass",

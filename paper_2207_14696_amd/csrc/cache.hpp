@@ -99,6 +99,36 @@ __device__ inline void load8_any(const T *p, int left, float (&x)[8]) {
         for (int i = 0; i < 8; i++) x[i] = i < left ? to_float(p[i]) : 0.f;
     }
 }
+// Eight columns of a row as they lie in memory.
+template <typename T>
+struct Columns {
+    uint32_t w[2 * sizeof(T)];
+};
+template <typename T>
+__device__ inline Columns<T> load_columns(const T *p) {
+    Columns<T> c;
+    const Eight<T> e = *reinterpret_cast<const Eight<T> *>(p);
+    __builtin_memcpy(c.w, &e, sizeof(c));
+    return c;
+}
+// ... of a row of K < 8 columns, the others as zeros.
+template <typename T>
+__device__ inline Columns<T> load_short_columns(const T *row, int K) {
+    Columns<T> c;
+    T v[8] = {};
+#pragma unroll
+    for (int i = 0; i < 7; i++)
+        if (i < K) v[i] = row[i];
+    __builtin_memcpy(c.w, v, sizeof(c));
+    return c;
+}
+template <typename T>
+__device__ inline Columns<T> no_columns() {
+    Columns<T> c;
+#pragma unroll
+    for (uint32_t &w : c.w) w = 0;
+    return c;
+}
 // N columns next to each other, of which the row has `left`.  STREAMED: not kept in the caches
 template <int N, bool STREAMED, typename T>
 __device__ inline void store_any(T *p, int left, const float *x) {

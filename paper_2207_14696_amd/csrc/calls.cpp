@@ -27,6 +27,11 @@ using DequantFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, int
 using CacheWriteFn = decltype(&bifeat_cache_write);
 using CacheReadFn = decltype(&bifeat_cache_read);
 using CacheAttendFn = decltype(&bifeat_cache_attend);
+using CacheAppendFn = decltype(&bifeat_cache_append);
+using LinearFn = decltype(&bifeat_linear_multiply);
+using ExpertsRoomFn = decltype(&bifeat_linear_experts_workspace);
+using ExpertsFn = decltype(&bifeat_linear_experts);
+using RouteFn = decltype(&bifeat_route);
 using AggregateFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, const void *, int64_t, int64_t, float *,
                             void *);
 
@@ -217,6 +222,47 @@ PyObject *cache_write(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
+// cache_append(..., pages, q (or None), k, v, frequencies, interleaved, scale, tables, lengths, indptr): the turned queries (or True), an
+// error status, or None
+PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 15) Py_RETURN_NONE;
+    try {
+        Cache c;
+        bifeat_head_rows q{}, k, v;
+        bifeat_cache_batch b;
+        int32_t dtype, other, third;
+        void *s = nullptr;
+        const at::Tensor *tq = nullptr, *tk, *tv, *f;
+        const bool queries = a[6] != Py_None;
+        const long interleaved = PyLong_AsLong(a[10]);
+        const double scale = PyFloat_AsDouble(a[11]);
+        if (PyErr_Occurred() || !cache_of(a, &c) || !(tk = head_rows(a[7], c, &k, &dtype)) || !(tv = head_rows(a[8], c, &v, &other)) || dtype != other ||
+            tk->size(1) != c.heads || tv->size(1) != c.heads || tk->size(0) != tv->size(0) ||
+            (queries && (!(tq = head_rows(a[6], c, &q, &third)) || third != dtype || tq->size(0) != tk->size(0) || tq->size(1) > INT32_MAX ||
+                         (tq->requires_grad() && c10::GradMode::is_enabled()))) ||
+            !(f = tensor(a[9], at::kFloat, at::kFloat, c.pages)) || f->dim() != 1 || f->size(0) > INT32_MAX || !batch_of(a + 12, c, tk->size(0), &b) ||
+            !stream(&s, c.pages)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const bifeat_turn turn{static_cast<const float *>(f->data_ptr()), (int32_t)f->size(0), interleaved != 0, scale};
+        const int64_t count = c.pages->size(0);
+        auto *p = static_cast<uint8_t *>(c.pages->data_ptr());
+        at::Tensor out;
+        int status;
+        {
+            Released interpreter;
+            if (queries) out = torch::empty(tq->sizes(), at::TensorOptions().dtype(tq->scalar_type()).device(tq->device()));
+            status = reinterpret_cast<CacheAppendFn>(c.fn)(static_cast<bifeat_cache *>(c.handle), p, count, &b, &q, queries ? (int32_t)tq->size(1) : 0, &k, &v,
+                                                           dtype, &turn, queries ? out.data_ptr() : nullptr, s);
+        }
+        if (status == 0 && !queries) Py_RETURN_TRUE;
+        return finish(status, out);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 // cache_read(..., pages, tokens, dtype, tables, lengths, indptr): (k, v), an error status, or None
 PyObject *cache_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
     if (n != 11) Py_RETURN_NONE;
@@ -292,12 +338,151 @@ PyObject *cache_attend(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
+// ---- products with matrices in 4 bits, and routing
+
+// rows of any of the three types whose last dimension's elements lie next to each other
+const at::Tensor *float_rows(PyObject *o, const at::Tensor *with, int32_t *dtype) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda() || t.dim() < 1 || t.layout() != at::kStrided || !t.unsafeGetTensorImpl()->has_storage() || t.stride(-1) != 1 ||
+        (with && t.device() != with->device()))
+        return nullptr;
+    const auto type = t.scalar_type();
+    if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return nullptr;
+    *dtype = type == at::kFloat ? BIFEAT_F32 : type == at::kHalf ? BIFEAT_F16 : BIFEAT_BF16;
+    return &t;
+}
+
+at::TensorOptions options_of(const at::Tensor &like, at::ScalarType type) { return at::TensorOptions().dtype(type).device(like.device()); }
+
+// linear_multiply(address of the entry point, out_features, in_features, group, bytes, packed, x): the output, an error status, or None
+PyObject *linear_multiply(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 7) Py_RETURN_NONE;
+    try {
+        auto fn = reinterpret_cast<LinearFn>(PyLong_AsVoidPtr(a[0]));
+        const bifeat_linear_spec spec{(int32_t)PyLong_AsLong(a[1]), (int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), 1};
+        const int64_t bytes = PyLong_AsLongLong(a[4]);
+        const at::Tensor *packed = tensor(a[5], at::kByte, at::kByte), *x;
+        int32_t dtype;
+        void *s = nullptr;
+        if (PyErr_Occurred() || !fn || !packed || packed->dim() != 1 || packed->size(0) != bytes || !(x = float_rows(a[6], packed, &dtype)) ||
+            x->size(-1) != spec.in_features || (x->dim() != 2 && !x->is_contiguous()) || (x->requires_grad() && c10::GradMode::is_enabled()) || watched() ||
+            !stream(&s, packed)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const int64_t rows = x->numel() / spec.in_features, stride = x->dim() == 2 ? x->stride(0) : spec.in_features;
+        const auto *p = static_cast<const uint8_t *>(packed->data_ptr());
+        at::Tensor out;
+        int status;
+        {
+            Released interpreter;
+            c10::DimVector shape(x->sizes().begin(), x->sizes().end());
+            shape.back() = spec.out_features;
+            out = torch::empty(shape, options_of(*x, x->scalar_type()));
+            status = fn(&spec, p, x->data_ptr(), stride, rows, dtype, out.data_ptr(), s);
+        }
+        return finish(status, out);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// linear_experts(address for the workspace's bytes, of the entry point, out_features, in_features, group, experts, bytes of one matrix, packed, x, ids,
+// weights or None): the output, an error status, or None
+PyObject *linear_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 11) Py_RETURN_NONE;
+    try {
+        auto room = reinterpret_cast<ExpertsRoomFn>(PyLong_AsVoidPtr(a[0]));
+        auto fn = reinterpret_cast<ExpertsFn>(PyLong_AsVoidPtr(a[1]));
+        const bifeat_linear_spec spec{(int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[4]), (int32_t)PyLong_AsLong(a[5])};
+        const int64_t bytes = PyLong_AsLongLong(a[6]);
+        const at::Tensor *packed = tensor(a[7], at::kByte, at::kByte), *x, *ids, *weights = nullptr;
+        int32_t dtype;
+        void *s = nullptr;
+        const bool summed = a[10] != Py_None;
+        if (PyErr_Occurred() || !room || !fn || !packed || packed->dim() != 2 || packed->size(0) != spec.experts || packed->size(1) != bytes ||
+            !(x = float_rows(a[8], packed, &dtype)) || !(ids = tensor(a[9], at::kInt, at::kInt, packed)) || ids->dim() != 2 || ids->size(1) > INT32_MAX ||
+            (x->dim() != 2 && x->dim() != 3) || x->size(0) != ids->size(0) || x->size(-1) != spec.in_features || (x->dim() == 3 && x->size(1) != ids->size(1)) ||
+            (summed && (!(weights = tensor(a[10], at::kFloat, at::kFloat, packed)) || weights->sizes() != ids->sizes())) ||
+            ((x->requires_grad() || (summed && weights->requires_grad())) && c10::GradMode::is_enabled()) || watched() || !stream(&s, packed)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const int64_t tokens = ids->size(0), choices = ids->size(1);
+        const bifeat_expert_rows rows{x->data_ptr(), x->stride(0), x->dim() == 3 ? x->stride(1) : 0, static_cast<const int32_t *>(ids->data_ptr()),
+                                      summed ? static_cast<const float *>(weights->data_ptr()) : nullptr, tokens, (int32_t)choices};
+        const int64_t need = room(&spec, &rows);
+        if (need < 0) return PyLong_FromLongLong(need);
+        const auto *p = static_cast<const uint8_t *>(packed->data_ptr());
+        at::Tensor out, work;
+        int status;
+        {
+            Released interpreter;
+            out = summed ? torch::empty({tokens, spec.out_features}, options_of(*x, x->scalar_type()))
+                         : torch::empty({tokens, choices, spec.out_features}, options_of(*x, x->scalar_type()));
+            if (need > 0) work = torch::empty({need}, options_of(*x, at::kByte));
+            status = fn(&spec, p, &rows, dtype, out.data_ptr(), need > 0 ? work.data_ptr() : nullptr, need, s);
+        }
+        return finish(status, out);
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
+// route(address of the entry point, logits, choices, sigmoid, bias or None, groups, top_groups, group_two, renormalise, scale): (ids, weights),
+// an error status, or None.  Logits without a gradient.
+PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    if (n != 10) Py_RETURN_NONE;
+    try {
+        auto fn = reinterpret_cast<RouteFn>(PyLong_AsVoidPtr(a[0]));
+        int32_t dtype;
+        void *s = nullptr;
+        const at::Tensor *x = float_rows(a[1], nullptr, &dtype), *bias = nullptr;
+        if (!fn || !x || x->size(-1) > INT32_MAX || (x->dim() != 2 && !x->is_contiguous())) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        const bool biased = a[4] != Py_None;
+        bifeat_route_options o{(int32_t)x->size(-1), (int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[5]),
+                               (int32_t)PyLong_AsLong(a[6]), (int32_t)PyLong_AsLong(a[7]), (int32_t)PyLong_AsLong(a[8]), PyFloat_AsDouble(a[9]), nullptr};
+        if (PyErr_Occurred() || o.experts < 1 || o.choices < 1 || (x->requires_grad() && c10::GradMode::is_enabled()) ||
+            (biased && (!(bias = tensor(a[4], at::kFloat, at::kFloat, x)) || bias->dim() != 1 || bias->size(0) != o.experts)) || watched() || !stream(&s, x)) {
+            PyErr_Clear();
+            Py_RETURN_NONE;
+        }
+        if (biased) o.bias = static_cast<const float *>(bias->data_ptr());
+        const int64_t tokens = x->numel() / o.experts, stride = x->dim() == 2 ? x->stride(0) : o.experts;
+        at::Tensor ids, weights;
+        int status;
+        {
+            Released interpreter;
+            c10::DimVector shape(x->sizes().begin(), x->sizes().end());
+            shape.back() = o.choices;
+            ids = torch::empty(shape, options_of(*x, at::kInt));
+            weights = torch::empty(shape, options_of(*x, at::kFloat));
+            status = fn(x->data_ptr(), stride, dtype, tokens, &o, static_cast<int32_t *>(ids.data_ptr()), static_cast<float *>(weights.data_ptr()), s);
+        }
+        if (status != 0) return PyLong_FromLong(status);
+        PyObject *pi = THPVariable_Wrap(ids), *pw = pi ? THPVariable_Wrap(weights) : nullptr, *both = pw ? PyTuple_Pack(2, pi, pw) : nullptr;
+        Py_XDECREF(pi);
+        Py_XDECREF(pw);
+        return both;
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+}
+
 PyMethodDef methods[] = {
     {"gather_dequant", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gather_dequant)), METH_FASTCALL, nullptr},
     {"aggregate", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(aggregate)), METH_FASTCALL, nullptr},
     {"cache_write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_write)), METH_FASTCALL, nullptr},
     {"cache_read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_read)), METH_FASTCALL, nullptr},
     {"cache_attend", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_attend)), METH_FASTCALL, nullptr},
+    {"cache_append", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_append)), METH_FASTCALL, nullptr},
+    {"linear_multiply", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_multiply)), METH_FASTCALL, nullptr},
+    {"linear_experts", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_experts)), METH_FASTCALL, nullptr},
+    {"route", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(route)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -74,19 +74,8 @@ __device__ inline typename Operand<T>::Eight ones() {
     return __builtin_bit_cast(typename Operand<T>::Eight, r);
 }
 
-// Eight columns of a row of x as they lie in memory.
-template <typename T>
-struct Columns {
-    uint32_t w[2 * sizeof(T)];
-};
-template <typename T>
-__device__ inline Columns<T> load_columns(const T *p) {
-    Columns<T> c;
-    const Eight<T> e = *reinterpret_cast<const Eight<T> *>(p);
-    __builtin_memcpy(c.w, &e, sizeof(c));
-    return c;
-}
-// ... from column `at` of a row of K >= 8, those past the end as zeros: the row's last eight, moved down.
+// Columns: eight of a row of x as they lie in memory (cache.hpp).
+// From column `at` of a row of K >= 8, those past the end as zeros: the row's last eight, moved down.
 template <typename T>
 __device__ inline Columns<T> load_last_columns(const T *row, int at, int K) {
     const int from = at < K - 8 ? at : K - 8, past = at < K ? at - from : 8;
@@ -99,24 +88,6 @@ __device__ inline Columns<T> load_last_columns(const T *row, int at, int K) {
     if constexpr (kPerWord == 2)
 #pragma unroll
         for (int i = 0; i < kWords; i++) c.w[i] = past & 1 ? c.w[i] >> 16 | (i + 1 < kWords ? c.w[i + 1 < kWords ? i + 1 : 0] << 16 : 0u) : c.w[i];
-    return c;
-}
-// ... of a row of K < 8 columns.
-template <typename T>
-__device__ inline Columns<T> load_short_columns(const T *row, int K) {
-    Columns<T> c;
-    T v[8] = {};
-#pragma unroll
-    for (int i = 0; i < 7; i++)
-        if (i < K) v[i] = row[i];
-    __builtin_memcpy(c.w, v, sizeof(c));
-    return c;
-}
-template <typename T>
-__device__ inline Columns<T> no_columns() {
-    Columns<T> c;
-#pragma unroll
-    for (uint32_t &w : c.w) w = 0;
     return c;
 }
 // ... and as operands

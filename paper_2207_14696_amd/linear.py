@@ -25,6 +25,11 @@ class PackedLinear:
             _check(EINVAL)
         self.out_features, self.in_features, self.group = int(out_features), int(in_features), int(group)
         self.experts = None if experts is None else int(experts)
+        # what the native module's calls begin with: entry points, sizes
+        sizes = (self.out_features, self.in_features, self.group)
+        self._multiply = (_b._address(self._lib.bifeat_linear_multiply), *sizes, self.bytes)
+        self._by_experts = (_b._address(self._lib.bifeat_linear_experts_workspace), _b._address(self._lib.bifeat_linear_experts), *sizes,
+                            self.experts, self.bytes)
 
     def _lead(self):
         return () if self.experts is None else (self.experts,)
@@ -59,6 +64,12 @@ class PackedLinear:
         """x [..., in_features] times the matrix's rows: [..., out_features] of x's type (float32, float16 or bfloat16).  Rows may lie any
         distance apart, their columns next to each other.  There is no backward pass: where x requires a gradient, going back
         through the output raises, and ``out`` is refused."""
+        if out is None and self.experts is None and (calls := _b._calls or _b._load_calls()):
+            r = calls.linear_multiply(*self._multiply, packed, x)
+            if r is not None:
+                if r.__class__ is int:
+                    _check(r)
+                return r
         import torch
         if self.experts is not None:
             raise ValueError("a layer of experts: multiply_experts")
@@ -88,6 +99,12 @@ class PackedLinear:
         [tokens, choices, out_features] of x's type, or with ``weights`` float32 [tokens, choices] their weighted sum,
         [tokens, out_features].  Takes memory for the time of the call: 4 bytes a pair of a token and a choice, with weights
         4 * out_features more.  No backward pass, as ``multiply``."""
+        if out is None and self.experts is not None and (calls := _b._calls or _b._load_calls()):
+            r = calls.linear_experts(*self._by_experts, packed, x, ids, weights)
+            if r is not None:
+                if r.__class__ is int:
+                    _check(r)
+                return r
         import torch
         if self.experts is None:
             raise ValueError("a layer of one matrix: multiply")

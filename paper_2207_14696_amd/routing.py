@@ -9,6 +9,14 @@ from . import binding as _b
 from .binding import _check, _dev_ptr, _dtype_code, _on_current_device, _stream, load_library
 
 
+_SCORES, _GROUP_SCORES = {"softmax": 0, "sigmoid": 1}, {"best": 0, "two": 1}
+
+
+@functools.lru_cache(maxsize=None)
+def _entry() -> int:
+    return _b._address(load_library().bifeat_route)
+
+
 def _rows(logits):
     rows = logits.reshape(-1, logits.shape[-1])
     return rows if rows.stride(1) == 1 or rows.shape[1] == 1 else rows.contiguous()
@@ -63,15 +71,21 @@ def route(logits, choices: int, score: str = "softmax", bias=None, groups: int =
     its "best" expert or (``group_score`` "two") the sum of its two best.  ``renormalise``: weights are shares of their sum.  ``scale``: of the
     weights.  An expert whose logit is -infinity is not chosen.  Weights have a gradient in the logits (once); the choice and
     the bias have none."""
+    if score in _SCORES and group_score in _GROUP_SCORES and (calls := _b._calls or _b._load_calls()):
+        r = calls.route(_entry(), logits, choices, _SCORES[score], bias, groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale)
+        if r is not None:
+            if r.__class__ is int:
+                _check(r)
+            return r
     import torch
-    if logits.dim() < 1 or score not in ("softmax", "sigmoid") or group_score not in ("best", "two"):
+    if logits.dim() < 1 or score not in _SCORES or group_score not in _GROUP_SCORES:
         raise ValueError('logits must be [..., experts], score "softmax" or "sigmoid", group_score "best" or "two"')
     experts = logits.shape[-1]
     if bias is not None:
         if bias.shape != (experts,):
             raise ValueError("bias must be [experts]")
         _on_current_device(logits, bias)
-    options = _b._CRouteOptions(experts, choices, score == "sigmoid", groups, top_groups, group_score == "two", bool(renormalise), scale,
+    options = _b._CRouteOptions(experts, choices, _SCORES[score], groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale,
                                 _dev_ptr(bias, (torch.float32,)))
     options.kept = bias     # (as long as a backward pass may need the options)
     if logits.requires_grad and torch.is_grad_enabled():

@@ -39,9 +39,12 @@ def _check(bf, torch, batch, bits, heads, group, d, ps, dtype, layout, pairs, in
     want_q = turn(_host(q), at, hf, interleaved, scale)
     want_q[at < 0] = 0.0
     assert got_q.dtype == q.dtype and got_q.shape == q.shape and got_q.is_contiguous()
-    # rounded to 32 bits, then to the type
+    # rounded to 32 bits, then to the type; queries of 16 bits in numbers of 32: cosine and sine rounded (2^-25 of them: they are below 1, times the
+    # scale), products (2^-24) and their sum (2^-24), so within 2^-22 of scale (|u| + |w|),
+    # which is at most twice the row's largest
     off = np.abs(_host(got_q) - want_q)
-    assert (off <= np.abs(want_q) * (HALF_ULP[dtype] + 2.0 ** -24 + 2.0 ** -40) + 2.0 ** -25 * (dtype == "f16") + 1e-13).all()
+    turned = 0.0 if dtype == "f32" else 2.0 ** -22 * scale * np.abs(_host(q)).max(-1, keepdims=True) * 2
+    assert (off <= (np.abs(want_q) + turned) * (HALF_ULP[dtype] + 2.0 ** -24 + 2.0 ** -40) + turned + 2.0 ** -25 * (dtype == "f16") + 1e-13).all()
     return c, pages
 
 
