@@ -12,12 +12,16 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/generated/variable_factories.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
 
 #include <cstdint>
 #include <string>
+#include <tuple>
+#include <utility>
 
 #include "bifeat.h"
 
@@ -32,6 +36,7 @@ using LinearFn = decltype(&bifeat_linear_multiply);
 using ExpertsRoomFn = decltype(&bifeat_linear_experts_workspace);
 using ExpertsFn = decltype(&bifeat_linear_experts);
 using RouteFn = decltype(&bifeat_route);
+using RouteBackwardFn = decltype(&bifeat_route_backward);
 using AggregateFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, const void *, int64_t, int64_t, float *,
                             void *);
 
@@ -430,40 +435,110 @@ PyObject *linear_experts(PyObject *, PyObject *const *a, Py_ssize_t n) {
     }
 }
 
-// route(address of the entry point, logits, choices, sigmoid, bias or None, groups, top_groups, group_two, renormalise, scale): (ids, weights),
-// an error status, or None.  Logits without a gradient.
+struct Routing {
+    RouteFn fn;
+    RouteBackwardFn back;
+    bifeat_route_options options;
+    int32_t dtype;
+    int64_t tokens, stride;
+    void *stream;
+    int status;
+};
+
+// ids and weights of the logits
+std::pair<at::Tensor, at::Tensor> routed(const at::Tensor &x, Routing &r) {
+    c10::DimVector shape(x.sizes().begin(), x.sizes().end());
+    shape.back() = r.options.choices;
+    at::Tensor ids = torch::empty(shape, options_of(x, at::kInt)), weights = torch::empty(shape, options_of(x, at::kFloat));
+    r.status = r.fn(x.data_ptr(), r.stride, r.dtype, r.tokens, &r.options, static_cast<int32_t *>(ids.data_ptr()), static_cast<float *>(weights.data_ptr()), r.stream);
+    return {ids, weights};
+}
+
+// Through Python's autograd function a call and its way back took 80 us of the host.
+struct RouteWithGradient : torch::autograd::Function<RouteWithGradient> {
+    static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const at::Tensor &x, Routing *r) {
+        auto [ids, weights] = routed(x, *r);
+        ctx->save_for_backward({x, ids});
+        ctx->mark_non_differentiable({ids});
+        const auto &o = r->options;
+        ctx->saved_data["back"] = static_cast<int64_t>(reinterpret_cast<intptr_t>(r->back));
+        ctx->saved_data["whole"] = std::vector<int64_t>{o.experts, o.choices, o.sigmoid, o.groups, o.top_groups, o.group_two, o.renormalise};
+        ctx->saved_data["scale"] = o.scale;
+        return {ids, weights};
+    }
+
+    static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, torch::autograd::variable_list grads) {
+        const auto saved = ctx->get_saved_variables();
+        const at::Tensor &x = saved[0], &ids = saved[1];
+        const auto whole = ctx->saved_data["whole"].toIntVector();
+        const bifeat_route_options o{(int32_t)whole[0], (int32_t)whole[1], (int32_t)whole[2], (int32_t)whole[3], (int32_t)whole[4],
+                                     (int32_t)whole[5], (int32_t)whole[6], ctx->saved_data["scale"].toDouble(), nullptr};
+        const bool again = c10::GradMode::is_enabled();
+        at::Tensor out;
+        {
+            const at::NoGradGuard no_grad;
+            const at::Tensor grad = grads[1].contiguous();
+            out = torch::empty(x.sizes(), options_of(x, x.scalar_type()));
+            void *s = nullptr;
+            bool there;
+            {
+                const PyGILState_STATE state = PyGILState_Ensure();
+                there = stream(&s, &x);
+                PyErr_Clear();
+                PyGILState_Release(state);
+            }
+            TORCH_CHECK(there && grad.device() == x.device(), "route: the logits are not on the current device");
+            const auto type = x.scalar_type();
+            const int status = reinterpret_cast<RouteBackwardFn>(static_cast<intptr_t>(ctx->saved_data["back"].toInt()))(
+                x.data_ptr(), x.dim() == 2 ? x.stride(0) : o.experts, type == at::kFloat ? BIFEAT_F32 : type == at::kHalf ? BIFEAT_F16 : BIFEAT_BF16,
+                x.numel() / o.experts, &o, static_cast<const int32_t *>(ids.data_ptr()), static_cast<const float *>(grad.data_ptr()), out.data_ptr(), s);
+            TORCH_CHECK(status == 0, "bifeat_route_backward: status ", status);
+        }
+        if (again) {  // (the gradient is no function of the graph: going back through it raises)
+            auto error = std::make_shared<torch::autograd::DelayedError>("route: weights have a gradient once, not a second derivative", 1);
+            out = (*error)({out.requires_grad_(true)})[0];
+        }
+        return {out, at::Tensor()};
+    }
+};
+
+// route(address of the entry point, and of its backward pass, logits, choices, sigmoid, bias or None, groups, top_groups, group_two, renormalise,
+// scale): (ids, weights), an error status, or None
 PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 10) Py_RETURN_NONE;
+    if (n != 11) Py_RETURN_NONE;
     try {
-        auto fn = reinterpret_cast<RouteFn>(PyLong_AsVoidPtr(a[0]));
-        int32_t dtype;
-        void *s = nullptr;
-        const at::Tensor *x = float_rows(a[1], nullptr, &dtype), *bias = nullptr;
-        if (!fn || !x || x->size(-1) > INT32_MAX || (x->dim() != 2 && !x->is_contiguous())) {
+        Routing r{};
+        r.fn = reinterpret_cast<RouteFn>(PyLong_AsVoidPtr(a[0]));
+        r.back = reinterpret_cast<RouteBackwardFn>(PyLong_AsVoidPtr(a[1]));
+        const at::Tensor *x = float_rows(a[2], nullptr, &r.dtype), *bias = nullptr;
+        if (!r.fn || !r.back || !x || x->size(-1) > INT32_MAX || (x->dim() != 2 && !x->is_contiguous())) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }
-        const bool biased = a[4] != Py_None;
-        bifeat_route_options o{(int32_t)x->size(-1), (int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[5]),
-                               (int32_t)PyLong_AsLong(a[6]), (int32_t)PyLong_AsLong(a[7]), (int32_t)PyLong_AsLong(a[8]), PyFloat_AsDouble(a[9]), nullptr};
-        if (PyErr_Occurred() || o.experts < 1 || o.choices < 1 || (x->requires_grad() && c10::GradMode::is_enabled()) ||
-            (biased && (!(bias = tensor(a[4], at::kFloat, at::kFloat, x)) || bias->dim() != 1 || bias->size(0) != o.experts)) || watched() || !stream(&s, x)) {
+        const bool biased = a[5] != Py_None;
+        auto &o = r.options;
+        o = {(int32_t)x->size(-1), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[4]), (int32_t)PyLong_AsLong(a[6]),
+             (int32_t)PyLong_AsLong(a[7]), (int32_t)PyLong_AsLong(a[8]), (int32_t)PyLong_AsLong(a[9]), PyFloat_AsDouble(a[10]), nullptr};
+        if (PyErr_Occurred() || o.experts < 1 || o.choices < 1 ||
+            (biased && (!(bias = tensor(a[5], at::kFloat, at::kFloat, x)) || bias->dim() != 1 || bias->size(0) != o.experts)) || watched() ||
+            !stream(&r.stream, x)) {
             PyErr_Clear();
             Py_RETURN_NONE;
         }
         if (biased) o.bias = static_cast<const float *>(bias->data_ptr());
-        const int64_t tokens = x->numel() / o.experts, stride = x->dim() == 2 ? x->stride(0) : o.experts;
+        r.tokens = x->numel() / o.experts;
+        r.stride = x->dim() == 2 ? x->stride(0) : o.experts;
         at::Tensor ids, weights;
-        int status;
         {
             Released interpreter;
-            c10::DimVector shape(x->sizes().begin(), x->sizes().end());
-            shape.back() = o.choices;
-            ids = torch::empty(shape, options_of(*x, at::kInt));
-            weights = torch::empty(shape, options_of(*x, at::kFloat));
-            status = fn(x->data_ptr(), stride, dtype, tokens, &o, static_cast<int32_t *>(ids.data_ptr()), static_cast<float *>(weights.data_ptr()), s);
+            if (x->requires_grad() && c10::GradMode::is_enabled()) {
+                auto both = RouteWithGradient::apply(*x, &r);
+                ids = both[0], weights = both[1];
+            } else {
+                std::tie(ids, weights) = routed(*x, r);
+            }
         }
-        if (status != 0) return PyLong_FromLong(status);
+        if (r.status != 0) return PyLong_FromLong(r.status);
         PyObject *pi = THPVariable_Wrap(ids), *pw = pi ? THPVariable_Wrap(weights) : nullptr, *both = pw ? PyTuple_Pack(2, pi, pw) : nullptr;
         Py_XDECREF(pi);
         Py_XDECREF(pw);

@@ -145,7 +145,10 @@ hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const
 // ... of K >= 8 columns, tiles of kManyRows
 constexpr int kManyRows = 128;
 hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
-hipError_t launch_linear_deal(const int *ids, int pairs, int experts, int tile, int *tiles_count, Tile *tiles, int *order, hipStream_t s);
+// Workgroups that deal pairs: several from 4096 on (one then takes longer than a launch more), 2048 or more each, 64 at most.
+inline int deal_parts(int64_t pairs) { return pairs < 4096 ? 1 : pairs < 64 * 2048 ? (int)(pairs / 2048) : 64; }
+// counts: deal_parts x (experts + 1)
+hipError_t launch_linear_deal(const int *ids, int pairs, int experts, int tile, int *counts, int *tiles_count, Tile *tiles, int *order, hipStream_t s);
 hipError_t launch_linear_join(const float *products, const int *ids, const float *weights, int64_t tokens, int choices, int experts, int N, int dtype, void *out,
                               hipStream_t s);
 

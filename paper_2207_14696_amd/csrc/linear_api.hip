@@ -29,10 +29,10 @@ bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
            r->tokens <= (INT32_MAX - 64) / r->choices;
 }
 
-// The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, 32-bit products.
+// The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, the parts' counts, 32-bit products.
 struct Room {
     int tile;
-    int64_t most_tiles, order, products, bytes;
+    int64_t most_tiles, order, counts, products, bytes;
 };
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
@@ -40,7 +40,9 @@ Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     o.tile = pairs >= 32 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
-    o.products = o.order + (pairs + 3) / 4 * 16;
+    o.counts = o.order + (pairs + 3) / 4 * 16;
+    const int parts = bf::deal_parts(pairs);
+    o.products = o.counts + (parts > 1 ? ((int64_t)parts * (s->experts + 1) + 3) / 4 * 16 : 0);
     o.bytes = o.products + (r->weights ? pairs * s->out_features * 4 : 0);
     return o;
 }
@@ -94,7 +96,7 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     int *tiles_count = reinterpret_cast<int *>(w), *order = reinterpret_cast<int *>(w + room.order);
     bf::Tile *tiles = reinterpret_cast<bf::Tile *>(w + 16);
     float *products = reinterpret_cast<float *>(w + room.products);
-    BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, tiles_count, tiles, order, s));
+    BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, reinterpret_cast<int *>(w + room.counts), tiles_count, tiles, order, s));
     const bf::Deal deal{tiles_count, tiles, order};
     const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out};
     const auto launch = room.tile == 16 ? bf::launch_linear_few : bf::launch_linear_many;

@@ -1,6 +1,8 @@
 // Tokens routed to experts: scores, ranks, the choice and its weights, and the logits' gradient.
 #include <math.h>
 
+#include <type_traits>
+
 #include "cache.hpp"
 
 #define BF_HIP(call)                                                   \
@@ -12,8 +14,9 @@
 namespace bf {
 namespace {
 
-// A wave takes a token; lane l has experts l, l + 64, ...  Scores, ranks and sums are 64-bit numbers: which of two experts is before the other may hang on the
-// last digits, and ranks in 32 bits would put another one first in 3 of 100 000 choices of 8 among 256.
+// A wave takes a token, a lane EPL neighbouring experts.  Where ranks are the logits alone, they are 32-bit numbers, and scores are needed of the chosen only.
+// Where scores count (a bias, sums of groups, softmax without shares) they and ranks are 64-bit numbers: which of two experts is before the other may hang
+// on the last digits, and ranks in 32 bits would put another one first in 3 of 100 000 choices of 8 among 256.
 constexpr int kTokensAtOnce = kThreads / 64;
 
 struct Options {
@@ -21,128 +24,259 @@ struct Options {
     bool sigmoid, two, renormalise;
     double scale;
     const float *bias;
+    int lanes_log2;  // of a group, where it is whole lanes and a power of two of them; else -1
 };
 
-__device__ inline double shuffled(double x, int by) { return __shfl_xor(x, by); }
-__device__ inline double wave_sum(double x) {
-#pragma unroll
-    for (int by = 32; by; by /= 2) x += shuffled(x, by);
+// ---- over a wave's lanes, without LDS: by moves within rows of 16, then from row to row; the result in the last lane
+template <int CTRL, int ROWS>
+__device__ inline uint32_t moved(uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ inline double moved(double x) {
+    const uint2 w = __builtin_bit_cast(uint2, x);
+    return __builtin_bit_cast(double, make_uint2(moved<CTRL, ROWS>(w.x), moved<CTRL, ROWS>(w.y)));
+}
+template <typename X, typename F>
+__device__ inline X over_wave(X x, F f) {
+    x = f(x, moved<0x111, 0xf>(x));  // the lane below
+    x = f(x, moved<0x112, 0xf>(x));  // two below, four, eight
+    x = f(x, moved<0x114, 0xf>(x));
+    x = f(x, moved<0x118, 0xf>(x));
+    x = f(x, moved<0x142, 0xa>(x));  // the last of the row below, in every other row
+    x = f(x, moved<0x143, 0xc>(x));  // the last of the lower half
     return x;
 }
-// the best of all lanes' ranks, of equal ones the lowest number, in all of them
-__device__ inline void wave_best(double &rank, int &number) {
-#pragma unroll
-    for (int by = 32; by; by /= 2) {
-        const double r = shuffled(rank, by);
-        const int n = __shfl_xor(number, by);
-        if (r > rank || (r == rank && n < number)) rank = r, number = n;
-    }
+__device__ inline uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
+__device__ inline double of_lane(double x, int lane) {
+    const uint2 w = __builtin_bit_cast(uint2, x);
+    return __builtin_bit_cast(double, make_uint2(of_lane(w.x, lane), of_lane(w.y, lane)));
+}
+__device__ inline uint32_t wave_most(uint32_t x) {
+    return of_lane(over_wave(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; }), 63);
+}
+__device__ inline double wave_sum(double x) {
+    return of_lane(over_wave(x, [](double a, double b) { return a + b; }), 63);
 }
 
-// A token's scores; true in `spoilt` where its weights are NaN.
+// ---- ranks as whole numbers in the same order; 0: not to be had
+__device__ inline uint32_t key_of(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x);
+    return x > -INFINITY ? (b & 0x80000000u ? ~b : b | 0x80000000u) : 0u;  // (a NaN is not)
+}
+__device__ inline uint64_t key_of(double x) {
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    return x > -INFINITY ? (b >> 63 ? ~b : b | 1ull << 63) : 0ull;
+}
+__device__ inline float of_key(uint32_t k) { return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k); }
+
+// (0 and -0 are equal)
+__device__ inline float plain_zero(float x) { return x == 0.f ? 0.f : x; }
+
+// The first lane that holds the largest key, and its upper 32 bits, the same in all lanes; 0 of them: no lane has one.
+__device__ inline int first_best(uint32_t key, uint32_t &most) {
+    most = wave_most(key);
+    return __builtin_ctzll(__ballot(key == most));
+}
+__device__ inline int first_best(uint64_t key, uint32_t &most) {
+    const uint32_t high = (uint32_t)(key >> 32);
+    most = wave_most(high);
+    uint64_t which = __ballot(high == most);
+    if (which & (which - 1)) {
+        const uint32_t low = high == most ? (uint32_t)key : 0u;
+        const uint32_t rest = wave_most(low);
+        which = __ballot(high == most && low == rest);
+    }
+    return __builtin_ctzll(which);
+}
+
+// A lane's logits, -infinity past the last expert; true in `spoilt` where the token's weights are NaN.
 template <typename T, int EPL>
-__device__ inline void scores_of(const T *row, const Options &o, int lane, double (&x)[EPL], double (&score)[EPL], bool &spoilt) {
-    double most = -INFINITY;
+__device__ inline void logits_of(const T *row, const Options &o, int lane, float (&x)[EPL], bool &spoilt) {
+    const int e0 = lane * EPL;
+    if (e0 + EPL <= o.experts) {
+        struct __attribute__((packed, aligned(sizeof(T)))) Logits {
+            T v[EPL];
+        };
+        const Logits l = *reinterpret_cast<const Logits *>(row + e0);
+#pragma unroll
+        for (int i = 0; i < EPL; i++) x[i] = to_float(l.v[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; i++) x[i] = e0 + i < o.experts ? to_float(row[e0 + i]) : -INFINITY;
+    }
     bool nan = false;
 #pragma unroll
     for (int i = 0; i < EPL; i++) {
-        const int e = lane + 64 * i;
-        x[i] = e < o.experts ? (double)to_float(row[e]) : -INFINITY;
+        x[i] = plain_zero(x[i]);
         nan |= x[i] != x[i] || (!o.sigmoid && x[i] == INFINITY);
-        most = fmax(most, x[i]);
     }
     spoilt = __ballot(nan) != 0;
+}
+
+__device__ inline double sigmoid(float x) { return 1.0 / (1.0 + exp(-(double)x)); }
+
+// All scores.
+template <int EPL>
+__device__ inline void scores_of(const float (&x)[EPL], const Options &o, double (&score)[EPL]) {
     if (o.sigmoid) {
 #pragma unroll
-        for (int i = 0; i < EPL; i++) score[i] = 1.0 / (1.0 + exp(-x[i]));
+        for (int i = 0; i < EPL; i++) score[i] = sigmoid(x[i]);
         return;
     }
+    uint32_t key = 0;
 #pragma unroll
-    for (int by = 32; by; by /= 2) most = fmax(most, shuffled(most, by));
+    for (int i = 0; i < EPL; i++) key = key_of(x[i]) > key ? key_of(x[i]) : key;
+    key = wave_most(key);
+    const double most = key ? (double)of_key(key) : 0.0;
     double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; i++) {
-        score[i] = most == -INFINITY ? 0.0 : exp(x[i] - most);  // (all masked: no expert has a score)
+        score[i] = exp((double)x[i] - most);
         sum += score[i];
     }
     sum = wave_sum(sum);
+    const double inverse = sum != 0.0 ? 1.0 / sum : 0.0;  // (all masked: no expert has a score)
 #pragma unroll
-    for (int i = 0; i < EPL; i++) score[i] = sum != 0.0 ? score[i] / sum : 0.0;
+    for (int i = 0; i < EPL; i++) score[i] *= inverse;
 }
 
-template <typename T, int EPL>
-__global__ __launch_bounds__(kThreads) void route_kernel(const T *logits, int64_t stride, int64_t tokens, Options o, int *ids, float *weights) {
-    extern __shared__ double ranks[];  // [token of the workgroup][expert], with groups
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-    const int64_t t = (int64_t)blockIdx.x * kTokensAtOnce + wave;
-    if (t >= tokens) return;
-    double x[EPL], score[EPL], rank[EPL];
-    bool spoilt;
-    scores_of<T, EPL>(logits + t * stride, o, lane, x, score, spoilt);
+// The experts that the kept groups do not hold are no longer to be had.  worth: what counts of an expert for its group.
+template <int EPL, typename Key>
+__device__ inline void keep_groups(const Options &o, int lane, double *room, Key (&key)[EPL], const double (&worth)[EPL]) {
+    const int per = o.experts / o.groups;
+    // (a group's worth is a key again: of its best expert, or of the sum of two)
+    if (o.lanes_log2 >= 0) {
+        const int lanes = 1 << o.lanes_log2;
+        Key of_group = 0;
+        if (!o.two) {
 #pragma unroll
-    for (int i = 0; i < EPL; i++) {
-        const int e = lane + 64 * i;
-        rank[i] = -INFINITY;
-        if (e < o.experts && x[i] > -INFINITY) {
-            const double r = o.bias ? score[i] + (double)o.bias[e] : x[i];
-            rank[i] = r == r ? r : -INFINITY;
+            for (int i = 0; i < EPL; i++) of_group = key[i] > of_group ? key[i] : of_group;
+            for (int by = 1; by < lanes; by *= 2) {
+                const Key other = __shfl_xor(of_group, by);
+                of_group = other > of_group ? other : of_group;
+            }
+        } else if constexpr (sizeof(Key) == 8) {
+            double best = -INFINITY, second = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < EPL; i++) {
+                const double w = key[i] ? worth[i] : -INFINITY;
+                second = fmax(second, fmin(best, w));
+                best = fmax(best, w);
+            }
+            for (int by = 1; by < lanes; by *= 2) {
+                const double b = __shfl_xor(best, by), s = __shfl_xor(second, by);
+                second = fmax(fmin(best, b), fmax(second, s));
+                best = fmax(best, b);
+            }
+            of_group = key_of(second > -INFINITY ? best + second : best);
         }
+        bool kept = false;
+        for (int j = 0; j < o.top_groups; j++) {
+            uint32_t most;
+            const int first = first_best(of_group, most);
+            if (most == 0) break;
+            if (lane >> o.lanes_log2 == first >> o.lanes_log2) kept = true, of_group = 0;
+        }
+#pragma unroll
+        for (int i = 0; i < EPL; i++) key[i] = kept ? key[i] : 0;
+        return;
     }
-    if (o.groups > 1) {
-        double *mine = ranks + wave * o.experts;
-        const int per = o.experts / o.groups;
+    // groups that lie across lanes, by way of LDS: a lane takes a group
+    if constexpr (sizeof(Key) == 8) {
 #pragma unroll
-        for (int i = 0; i < EPL; i++) {
-            const int e = lane + 64 * i;
-            if (e < o.experts) mine[e] = !o.two || o.bias || rank[i] == -INFINITY ? rank[i] : score[i];
-        }
+        for (int i = 0; i < EPL; i++)
+            if (lane * EPL + i < o.experts) room[lane * EPL + i] = key[i] ? worth[i] : -INFINITY;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup");
         double best = -INFINITY, second = -INFINITY;
         if (lane < o.groups)
             for (int i = 0; i < per; i++) {
-                const double r = mine[lane * per + i];
-                if (r > best) second = best, best = r;
-                else if (r > second) second = r;
+                const double w = room[lane * per + i];
+                second = fmax(second, fmin(best, w));
+                best = fmax(best, w);
             }
-        double of_group = o.two && second > -INFINITY ? best + second : best;
-        uint64_t kept = 0;
+        uint64_t of_group = key_of(o.two && second > -INFINITY ? best + second : best), kept = 0;
         for (int j = 0; j < o.top_groups; j++) {
-            double r = of_group;
-            int g = lane;
-            wave_best(r, g);
-            if (r == -INFINITY) break;
+            uint32_t most;
+            const int g = first_best(of_group, most);
+            if (most == 0) break;
             kept |= 1ull << g;
-            if (lane == g) of_group = -INFINITY;
+            if (lane == g) of_group = 0;
         }
+#pragma unroll
+        for (int i = 0; i < EPL; i++)
+            if (!(kept >> ((lane * EPL + i) / per & 63) & 1)) key[i] = 0;
+    }
+}
+
+// WIDE: ranks and scores are 64-bit numbers (see the top).
+template <typename T, int EPL, bool WIDE>
+__global__ __launch_bounds__(kThreads) void route_kernel(const T *logits, int64_t stride, int64_t tokens, Options o, int *ids, float *weights) {
+    typedef std::conditional_t<WIDE, uint64_t, uint32_t> Key;
+    extern __shared__ double ranks[];  // [token of the workgroup][expert], where groups lie across lanes
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t t = (int64_t)blockIdx.x * kTokensAtOnce + wave;
+    if (t >= tokens) return;
+    float x[EPL];
+    bool spoilt;
+    logits_of<T, EPL>(logits + t * stride, o, lane, x, spoilt);
+    Key key[EPL];
+    double score[EPL];
+    if constexpr (WIDE) {
+        double worth[EPL];
+        scores_of<EPL>(x, o, score);
 #pragma unroll
         for (int i = 0; i < EPL; i++) {
-            const int e = lane + 64 * i;
-            if (e < o.experts && !(kept >> (e / per) & 1)) rank[i] = -INFINITY;
+            const int e = lane * EPL + i;
+            const bool there = e < o.experts && x[i] > -INFINITY;
+            worth[i] = o.bias && there ? score[i] + (double)o.bias[e] : score[i];
+            const double rank = o.bias ? worth[i] : (double)x[i];
+            key[i] = there ? key_of(rank) : 0ull;
+            if (!o.bias && !o.two) worth[i] = rank;
         }
+        if (o.groups > 1) keep_groups<EPL>(o, lane, ranks + wave * o.experts, key, worth);
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; i++) key[i] = key_of(x[i]);  // (past the last expert: 0)
+        if (o.groups > 1) keep_groups<EPL>(o, lane, nullptr, key, score);
     }
-    int id = -1;           // the lane's choice, and its score
-    double chosen = 0.0, total = 0.0;
+    int id = -1;  // the lane's choice, and its score
+    double chosen = 0.0;
     for (int j = 0; j < o.choices; j++) {
-        double r = -INFINITY, its = 0.0;
-        int e = INT32_MAX;
+        Key best = 0;
+        int which = 0;
 #pragma unroll
         for (int i = 0; i < EPL; i++)
-            if (rank[i] > r) r = rank[i], e = lane + 64 * i;
-        wave_best(r, e);
-        if (r == -INFINITY) break;
+            if (key[i] > best) best = key[i], which = i;
+        uint32_t most;
+        const int first = first_best(best, most);
+        if (most == 0) break;
+        const int e = (int)of_lane((uint32_t)(lane * EPL + which), first);
+        double its = 0.0;
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int i = 0; i < EPL; i++) its = which == i ? score[i] : its;
+            its = of_lane(its, first);
+        } else {
+            its = (double)of_key(most);  // (the logit, for now)
+        }
 #pragma unroll
         for (int i = 0; i < EPL; i++)
-            if (e == lane + 64 * i) {
-                its = score[i];
-                rank[i] = -INFINITY;
-            }
-        its = __shfl(its, e % 64);
-        total += its;
+            if (lane == first && which == i) key[i] = 0;
         if (lane == j) id = e, chosen = its;
     }
+    if constexpr (!WIDE) {
+        // the first choice has the largest logit of all, so that shares of softmax scores are shares of exp(x - x_first)
+        const double most = of_lane(chosen, 0);
+        if (o.sigmoid) chosen = id < 0 ? 0.0 : sigmoid((float)chosen);
+        else chosen = id < 0 ? 0.0 : exp(chosen - most);
+    }
+    double w = o.scale * chosen;
+    if (o.renormalise) {
+        const double total = wave_sum(chosen);
+        w = total > 0.0 ? w / total : 0.0;
+    }
     if (lane < o.choices) {
-        double w = o.scale * chosen;
-        if (o.renormalise) w = total > 0.0 ? w / total : 0.0;
         ids[t * o.choices + lane] = id;
         weights[t * o.choices + lane] = spoilt ? NAN : id < 0 ? 0.f : (float)w;
     }
@@ -153,50 +287,94 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const T *logits, int64_
 //   softmax                  dx_i = c s_i ([i chosen] g_i - sum_j g_j s_j)
 //   sigmoid, renormalised    dx_i = c q_i (1 - s_i) (g_i - sum_j g_j q_j) for the chosen, else 0
 //   sigmoid                  dx_i = c s_i (1 - s_i) g_i for the chosen, else 0
+// Lane j has choice j; but for the second of these only the chosen scores are needed.
 template <typename T, int EPL>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(const T *logits, int64_t stride, int64_t tokens, Options o, const int *ids, const float *grad,
                                                                   T *out) {
     const int lane = threadIdx.x % 64;
     const int64_t t = (int64_t)blockIdx.x * kTokensAtOnce + threadIdx.x / 64;
     if (t >= tokens) return;
-    double x[EPL], score[EPL], g[EPL];
-    bool spoilt, chosen[EPL];
-    scores_of<T, EPL>(logits + t * stride, o, lane, x, score, spoilt);
+    int id = -1;
+    double g = 0.0;
+    float its = -INFINITY;
+    if (lane < o.choices) {
+        id = ids[t * o.choices + lane];
+        if (id < 0 || id >= o.experts) id = -1;
+        if (id >= 0) {
+            g = grad[t * o.choices + lane];
+            its = to_float(logits[t * stride + id]);
+        }
+    }
+    float x[EPL];
+    bool spoilt;
+    logits_of<T, EPL>(logits + t * stride, o, lane, x, spoilt);
+    double all[EPL], d = 0.0, sum = 0.0;
+    const bool every = !o.sigmoid && !o.renormalise;
+    if (every) {
+        scores_of<EPL>(x, o, all);
+        for (int j = 0; j < o.choices; j++) {
+            const int e = (int)of_lane((uint32_t)id, j);
+            const double gj = of_lane(g, j);
 #pragma unroll
-    for (int i = 0; i < EPL; i++) chosen[i] = false, g[i] = 0.0;
+            for (int i = 0; i < EPL; i++)
+                if (e == lane * EPL + i) sum += gj * all[i];
+        }
+        sum = wave_sum(sum);
+    } else {
+        double s;
+        if (o.sigmoid) {
+            s = id >= 0 ? sigmoid(its) : 0.0;
+        } else {
+            const uint32_t most = wave_most(id >= 0 ? key_of(its) : 0u);
+            s = id >= 0 && most ? exp((double)its - (double)of_key(most)) : 0.0;
+        }
+        double q = s;
+        if (o.renormalise) {
+            const double total = wave_sum(s);
+            q = total > 0.0 ? s / total : 0.0;
+            sum = wave_sum(g * q);
+        }
+        d = o.scale * q * (g - sum) * (o.sigmoid ? 1.0 - s : 1.0);
+    }
+    float y[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; i++) y[i] = every ? (float)(o.scale * all[i] * -sum) : 0.f;
     for (int j = 0; j < o.choices; j++) {
-        const int e = ids[t * o.choices + j];
-        const double its = grad[t * o.choices + j];
+        const int e = (int)of_lane((uint32_t)id, j);
+        const double one = of_lane(every ? g : d, j);
 #pragma unroll
         for (int i = 0; i < EPL; i++)
-            if (e == lane + 64 * i) chosen[i] = true, g[i] = its;
-    }
-    double sum = 0.0, total = 1.0;
-    if (o.renormalise) {
-        total = 0.0;
-#pragma unroll
-        for (int i = 0; i < EPL; i++) total += chosen[i] ? score[i] : 0.0;
-        total = wave_sum(total);
-    }
-    if (o.renormalise || !o.sigmoid) {
-#pragma unroll
-        for (int i = 0; i < EPL; i++) sum += chosen[i] ? g[i] * score[i] : 0.0;
-        sum = wave_sum(sum);
-        if (total > 0.0) sum /= total;
+            if (e == lane * EPL + i) y[i] = every ? (float)(o.scale * all[i] * (one - sum)) : (float)one;
     }
 #pragma unroll
-    for (int i = 0; i < EPL; i++) {
-        const int e = lane + 64 * i;
-        double d = 0.0;
-        if (total > 0.0 && (chosen[i] || (!o.renormalise && !o.sigmoid))) d = o.scale * (score[i] / total) * (g[i] - sum) * (o.sigmoid ? 1.0 - score[i] : 1.0);
-        if (e < o.experts) out[t * o.experts + e] = from_float<T>(spoilt ? NAN : (float)d);
+    for (int i = 0; i < EPL; i++) y[i] = spoilt ? NAN : y[i];
+    const int e0 = lane * EPL;
+    T *to = out + t * o.experts + e0;
+    if (e0 + EPL <= o.experts) {
+        struct __attribute__((packed, aligned(sizeof(T)))) Logits {
+            T v[EPL];
+        } l;
+#pragma unroll
+        for (int i = 0; i < EPL; i++) l.v[i] = from_float<T>(y[i]);
+        *reinterpret_cast<Logits *>(to) = l;
+    } else {
+#pragma unroll
+        for (int i = 0; i < EPL; i++)
+            if (e0 + i < o.experts) to[i] = from_float<T>(y[i]);
     }
 }
 
 template <typename T, int EPL>
-void route(const void *logits, int64_t stride, int64_t tokens, const Options &o, int *ids, float *weights, hipStream_t s) {
-    const size_t room = o.groups > 1 ? sizeof(double) * kTokensAtOnce * o.experts : 0;
-    route_kernel<T, EPL><<<(unsigned)((tokens + kTokensAtOnce - 1) / kTokensAtOnce), kThreads, room, s>>>((const T *)logits, stride, tokens, o, ids, weights);
+void route(const void *logits, int64_t stride, int64_t tokens, Options o, int *ids, float *weights, hipStream_t s) {
+    const unsigned grid = (unsigned)((tokens + kTokensAtOnce - 1) / kTokensAtOnce);
+    o.lanes_log2 = -1;
+    const int per = o.experts / o.groups;
+    if (per % EPL == 0 && (per / EPL & (per / EPL - 1)) == 0) o.lanes_log2 = ilog2(per / EPL);
+    const bool across = o.groups > 1 && o.lanes_log2 < 0;
+    const size_t room = across ? sizeof(double) * kTokensAtOnce * o.experts : 0;
+    const bool wide = o.bias || across || (!o.sigmoid && !o.renormalise) || (o.groups > 1 && o.two);
+    if (wide) route_kernel<T, EPL, true><<<grid, kThreads, room, s>>>((const T *)logits, stride, tokens, o, ids, weights);
+    else route_kernel<T, EPL, false><<<grid, kThreads, 0, s>>>((const T *)logits, stride, tokens, o, ids, weights);
 }
 template <typename T, int EPL>
 void route_backward(const void *logits, int64_t stride, int64_t tokens, const Options &o, const int *ids, const float *grad, void *out, hipStream_t s) {
@@ -222,7 +400,7 @@ bool options_ok(const bifeat_route_options *o, int32_t dtype, int64_t tokens, in
     return tokens >= 0 && tokens <= INT32_MAX / 64 && stride >= 0;
 }
 Options options_of(const bifeat_route_options *o) {
-    return {o->experts, o->choices, o->groups, o->top_groups, o->sigmoid != 0, o->group_two != 0, o->renormalise != 0, o->scale, o->bias};
+    return {o->experts, o->choices, o->groups, o->top_groups, o->sigmoid != 0, o->group_two != 0, o->renormalise != 0, o->scale, o->bias, -1};
 }
 
 }  // namespace

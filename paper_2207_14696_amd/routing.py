@@ -13,8 +13,9 @@ _SCORES, _GROUP_SCORES = {"softmax": 0, "sigmoid": 1}, {"best": 0, "two": 1}
 
 
 @functools.lru_cache(maxsize=None)
-def _entry() -> int:
-    return _b._address(load_library().bifeat_route)
+def _entries():
+    lib = load_library()
+    return _b._address(lib.bifeat_route), _b._address(lib.bifeat_route_backward)
 
 
 def _rows(logits):
@@ -72,7 +73,7 @@ def route(logits, choices: int, score: str = "softmax", bias=None, groups: int =
     weights.  An expert whose logit is -infinity is not chosen.  Weights have a gradient in the logits (once); the choice and
     the bias have none."""
     if score in _SCORES and group_score in _GROUP_SCORES and (calls := _b._calls or _b._load_calls()):
-        r = calls.route(_entry(), logits, choices, _SCORES[score], bias, groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale)
+        r = calls.route(*_entries(), logits, choices, _SCORES[score], bias, groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale)
         if r is not None:
             if r.__class__ is int:
                 _check(r)
