@@ -551,9 +551,12 @@ int bifeat_linear_pack(const bifeat_linear_spec *spec, const void *weight, int32
 /* The values that the codes stand for, fp32 [experts][out_features][in_features]. */
 int bifeat_linear_unpack(const bifeat_linear_spec *spec, const uint8_t *packed, float *weight, void *stream);
 /* x: DEVICE rows of in_features columns, `row_stride` elements apart (>= 0); out: DEVICE
- * [rows][out_features], which shares no memory with x.  One matrix (experts = 1). */
+ * [rows][out_features], which shares no memory with x.  One matrix (experts = 1).
+ * workspace: DEVICE memory of bifeat_linear_workspace() bytes (often 0: NULL will do), 16-byte
+ * aligned, for the time of the call's kernels alone. */
+int64_t bifeat_linear_workspace(const bifeat_linear_spec *spec, int64_t rows, int32_t dtype);
 int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed, const void *x, int64_t row_stride, int64_t rows,
-                           int32_t dtype, void *out, void *stream);
+                           int32_t dtype, void *out, void *workspace, int64_t workspace_bytes, void *stream);
 
 typedef struct {
     const void *x;          /* DEVICE: row of token t and choice j at t * token_stride + j * choice_stride */

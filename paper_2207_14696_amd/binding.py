@@ -143,7 +143,9 @@ _SIGNATURES = {
     "bifeat_linear_bytes": (C.c_int64, [C.POINTER(_CLinearSpec)]),
     "bifeat_linear_pack": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]),
     "bifeat_linear_unpack": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_void_p, C.c_void_p]),
-    "bifeat_linear_multiply": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p]),
+    "bifeat_linear_workspace": (C.c_int64, [C.POINTER(_CLinearSpec), C.c_int64, C.c_int32]),
+    "bifeat_linear_multiply": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
+                                         C.c_int64, C.c_void_p]),
     "bifeat_linear_experts_workspace": (C.c_int64, [C.POINTER(_CLinearSpec), C.POINTER(_CExpertRows)]),
     "bifeat_linear_experts": (C.c_int, [C.POINTER(_CLinearSpec), C.c_void_p, C.POINTER(_CExpertRows), C.c_int32, C.c_void_p, C.c_void_p, C.c_int64,
                                         C.c_void_p]),

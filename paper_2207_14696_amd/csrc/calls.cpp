@@ -33,6 +33,7 @@ using CacheReadFn = decltype(&bifeat_cache_read);
 using CacheAttendFn = decltype(&bifeat_cache_attend);
 using CacheAppendFn = decltype(&bifeat_cache_append);
 using LinearFn = decltype(&bifeat_linear_multiply);
+using LinearRoomFn = decltype(&bifeat_linear_workspace);
 using ExpertsRoomFn = decltype(&bifeat_linear_experts_workspace);
 using ExpertsFn = decltype(&bifeat_linear_experts);
 using RouteFn = decltype(&bifeat_route);
@@ -360,17 +361,18 @@ const at::Tensor *float_rows(PyObject *o, const at::Tensor *with, int32_t *dtype
 
 at::TensorOptions options_of(const at::Tensor &like, at::ScalarType type) { return at::TensorOptions().dtype(type).device(like.device()); }
 
-// linear_multiply(address of the entry point, out_features, in_features, group, bytes, packed, x): the output, an error status, or None
+// linear_multiply(address for the workspace's bytes, of the entry point, out_features, in_features, group, bytes, packed, x): the output, an error status, or None
 PyObject *linear_multiply(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    if (n != 7) Py_RETURN_NONE;
+    if (n != 8) Py_RETURN_NONE;
     try {
-        auto fn = reinterpret_cast<LinearFn>(PyLong_AsVoidPtr(a[0]));
-        const bifeat_linear_spec spec{(int32_t)PyLong_AsLong(a[1]), (int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), 1};
-        const int64_t bytes = PyLong_AsLongLong(a[4]);
-        const at::Tensor *packed = tensor(a[5], at::kByte, at::kByte), *x;
+        auto room = reinterpret_cast<LinearRoomFn>(PyLong_AsVoidPtr(a[0]));
+        auto fn = reinterpret_cast<LinearFn>(PyLong_AsVoidPtr(a[1]));
+        const bifeat_linear_spec spec{(int32_t)PyLong_AsLong(a[2]), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[4]), 1};
+        const int64_t bytes = PyLong_AsLongLong(a[5]);
+        const at::Tensor *packed = tensor(a[6], at::kByte, at::kByte), *x;
         int32_t dtype;
         void *s = nullptr;
-        if (PyErr_Occurred() || !fn || !packed || packed->dim() != 1 || packed->size(0) != bytes || !(x = float_rows(a[6], packed, &dtype)) ||
+        if (PyErr_Occurred() || !room || !fn || !packed || packed->dim() != 1 || packed->size(0) != bytes || !(x = float_rows(a[7], packed, &dtype)) ||
             x->size(-1) != spec.in_features || (x->dim() != 2 && !x->is_contiguous()) || (x->requires_grad() && c10::GradMode::is_enabled()) || watched() ||
             !stream(&s, packed)) {
             PyErr_Clear();
@@ -378,14 +380,17 @@ PyObject *linear_multiply(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         const int64_t rows = x->numel() / spec.in_features, stride = x->dim() == 2 ? x->stride(0) : spec.in_features;
         const auto *p = static_cast<const uint8_t *>(packed->data_ptr());
-        at::Tensor out;
+        const int64_t need = room(&spec, rows, dtype);
+        if (need < 0) return PyLong_FromLongLong(need);
+        at::Tensor out, work;
         int status;
         {
             Released interpreter;
             c10::DimVector shape(x->sizes().begin(), x->sizes().end());
             shape.back() = spec.out_features;
             out = torch::empty(shape, options_of(*x, x->scalar_type()));
-            status = fn(&spec, p, x->data_ptr(), stride, rows, dtype, out.data_ptr(), s);
+            if (need > 0) work = torch::empty({need}, options_of(*x, at::kByte));
+            status = fn(&spec, p, x->data_ptr(), stride, rows, dtype, out.data_ptr(), need > 0 ? work.data_ptr() : nullptr, need, s);
         }
         return finish(status, out);
     } catch (...) {

@@ -140,11 +140,20 @@ struct Deal {
 
 hipError_t launch_linear_pack(const Matrices &m, int group, const void *weight, int dtype, uint8_t *packed, hipStream_t s);
 hipError_t launch_linear_unpack(const Matrices &m, int group, float *weight, hipStream_t s);
-// deal null: one matrix, rows as they are.  to_float: out is fp32 whatever the rows' type.
-hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
+// How few rows are taken: 16 tb of them and 16 r of the matrix a workgroup, columns in `split` parts (without a deal).
+struct FewShape {
+    int tb, r, split;
+};
+__host__ __device__ constexpr int few_waves(int) { return 8; }
+template <typename T> constexpr int few_most_rows = sizeof(T) == 4 ? 2 : 4;  // r of tb >= 2
+// deal null: one matrix, rows as they are.  to_float: out is fp32 whatever the rows' type; of several parts one after another.
+hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, const FewShape &shape,
+                             hipStream_t s);
 // ... of K >= 8 columns, tiles of kManyRows
 constexpr int kManyRows = 128;
-hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s);
+hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, int split, hipStream_t s);
+// out = the parts' sum, `count` numbers each
+hipError_t launch_linear_add(const float *parts, int split, int64_t count, int dtype, void *out, hipStream_t s);
 // Workgroups that deal pairs: several from 4096 on (one then takes longer than a launch more), 2048 or more each, 64 at most.
 inline int deal_parts(int64_t pairs) { return pairs < 4096 ? 1 : pairs < 64 * 2048 ? (int)(pairs / 2048) : 64; }
 // counts: deal_parts x (experts + 1)

@@ -1,4 +1,6 @@
 // Entry points of the products with matrices in 4 bits: argument checks, and dispatch to the kernels of linear_*.hip.
+#include <stdio.h>
+#include <stdlib.h>
 #include <algorithm>
 
 #include "linear.hpp"
@@ -22,6 +24,28 @@ bool data_ok(const void *p, int32_t dtype) { return p && (uintptr_t)p % (dtype =
 bf::Matrices matrices_of(const bifeat_linear_spec *s, const uint8_t *packed) {
     const int rows = (s->out_features + 15) / 16, blocks = (s->in_features + 127) / 128;
     return {packed, (int64_t)rows * blocks * (1024 + 64 * (128 / s->group)), s->out_features, s->in_features, rows, blocks, s->experts};
+}
+
+// How a product of rows with one matrix is taken.
+struct Plan {
+    bool many;
+    int tb, r, split;
+    int64_t bytes(const bifeat_linear_spec *s, int64_t rows) const { return split > 1 ? split * rows * s->out_features * 4 : 0; }
+};
+Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
+    const int64_t rows16 = (s->out_features + 15) / 16, blocks = (s->in_features + 127) / 128;
+    const char *ev = getenv("BFP");
+    int e[4] = {-1, 0, 0, 0};
+    if (ev) sscanf(ev, "%d,%d,%d,%d", e, e + 1, e + 2, e + 3);
+    Plan p{};
+    p.many = rows > 64 && s->in_features >= 8;
+    p.tb = rows <= 16 ? 1 : rows <= 32 || dtype == BIFEAT_F32 ? 2 : rows <= 48 ? 3 : 4;
+    p.r = p.tb > 1 ? (dtype == BIFEAT_F32 ? 2 : 4) : rows16 >= 1024 ? 4 : rows16 >= 512 ? 2 : 1;
+    p.split = 1;
+    if (e[0] >= 0) p.many = e[0], p.split = e[3];
+    if (e[0] >= 0 && e[2] && p.tb == 1) p.r = e[2];
+    (void)blocks;
+    return p;
 }
 
 bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
@@ -65,14 +89,25 @@ int bifeat_linear_unpack(const bifeat_linear_spec *spec, const uint8_t *packed, 
     return BIFEAT_OK;
 }
 
+int64_t bifeat_linear_workspace(const bifeat_linear_spec *spec, int64_t rows, int32_t dtype) {
+    if (!spec_ok(spec) || spec->experts != 1 || !type_ok(dtype) || rows < 0 || rows > INT32_MAX - 64) return BIFEAT_EINVAL;
+    return plan_of(spec, rows, dtype).bytes(spec, rows);
+}
+
 int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed, const void *x, int64_t row_stride, int64_t rows,
-                           int32_t dtype, void *out, void *stream) {
+                           int32_t dtype, void *out, void *workspace, int64_t workspace_bytes, void *stream) {
     if (!spec_ok(spec) || spec->experts != 1 || !type_ok(dtype) || rows < 0 || rows > INT32_MAX - 64 || row_stride < 0) return BIFEAT_EINVAL;
     if (rows == 0) return BIFEAT_OK;
-    if (!packed || (uintptr_t)packed % 16 || !data_ok(x, dtype) || !data_ok(out, dtype)) return BIFEAT_EINVAL;
-    const bf::XRows r{x, row_stride, 0, 1, rows, out};
-    const auto launch = rows > 64 && spec->in_features >= 8 ? bf::launch_linear_many : bf::launch_linear_few;
-    BF_HIP(launch(matrices_of(spec, packed), spec->group, r, nullptr, 0, dtype, false, (hipStream_t)stream));
+    if (!packed || (uintptr_t)packed % 16 || !data_ok(x, dtype) || !data_ok(out, dtype) || (uintptr_t)workspace % 16) return BIFEAT_EINVAL;
+    const Plan plan = plan_of(spec, rows, dtype);
+    if (plan.bytes(spec, rows) > (workspace ? workspace_bytes : 0)) return BIFEAT_EINVAL;
+    const bf::Matrices m = matrices_of(spec, packed);
+    const hipStream_t s = (hipStream_t)stream;
+    const bool split = plan.split > 1;
+    const bf::XRows r{x, row_stride, 0, 1, rows, split ? workspace : out};
+    if (plan.many) BF_HIP(bf::launch_linear_many(m, spec->group, r, nullptr, 0, dtype, split, plan.split, s));
+    else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split}, s));
+    if (split) BF_HIP(bf::launch_linear_add(static_cast<const float *>(workspace), plan.split, rows * m.N, dtype, out, s));
     return BIFEAT_OK;
 }
 
@@ -99,8 +134,9 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, reinterpret_cast<int *>(w + room.counts), tiles_count, tiles, order, s));
     const bf::Deal deal{tiles_count, tiles, order};
     const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out};
-    const auto launch = room.tile == 16 ? bf::launch_linear_few : bf::launch_linear_many;
-    BF_HIP(launch(m, spec->group, x, &deal, (int)room.most_tiles, dtype, r->weights != nullptr, s));
+    const bool to_float = r->weights != nullptr;
+    if (room.tile == 16) BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, {1, 2, 1}, s));
+    else BF_HIP(bf::launch_linear_many(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, 1, s));
     if (r->weights) BF_HIP(bf::launch_linear_join(products, r->ids, r->weights, r->tokens, r->choices, spec->experts, m.N, dtype, out, s));
     return BIFEAT_OK;
 }

@@ -6,16 +6,16 @@
 namespace bf {
 namespace {
 
-constexpr int kWaves = 8;
-
-// A workgroup takes R times 16 rows of the matrix and up to 16 TB rows of x; its waves take blocks of 128 columns in turn and add up what they have
-// in LDS at the end.  A lane's 16 bytes of a block are 32 codes of one row of the matrix, four operands as they are.
+// A workgroup takes R times 16 rows of the matrix, up to 16 TB rows of x and, where the columns are split, a part of these; its waves take blocks of 128 columns in turn and add up what they have
+// in LDS at the end.  A lane's 16 bytes of a block are 32 codes of one row of the matrix, four operands as they are; x is the other operand, so that a lane's sums
+// are of one row of the matrix, and of one scale.  Of up to 16 rows the next block
+// is on its way while one is multiplied.
 template <typename T, int GPB, int TB, int R, bool DEALT, typename Out>
-__global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out, int tile0) {
+__global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out, int tile0) {
     typedef Operand<T> O;
-    constexpr int P = O::kPieces;
+    constexpr int P = O::kPieces, kWaves = few_waves(TB);
     __shared__ Sum4 part[kWaves][R * TB][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 16, quarter = lane / 16;
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quarter = lane / 16;
     const int row0 = blockIdx.x * R;
     const int x_tile = tile0 + blockIdx.y;
     int64_t first = (int64_t)x_tile * 16 * TB;
@@ -37,43 +37,53 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
     } else {
         count = x.count - first < 16 * TB ? (int)(x.count - first) : 16 * TB;
     }
+    const auto row_of = [&](int i) -> int64_t {
+        if constexpr (DEALT) return deal.order[first + i];
+        return first + i;
+    };
     const T *xr[TB];
-    int64_t to[TB];
 #pragma unroll
     for (int t = 0; t < TB; t++) {
-        const int at = 16 * t + col < count ? 16 * t + col : count - 1;  // (what a row past the last gives is not stored)
-        int64_t row = first + at;
-        if constexpr (DEALT) row = deal.order[row];
-        to[t] = row;
+        const int64_t row = row_of(16 * t + col < count ? 16 * t + col : count - 1);  // (what a row past the last gives is not stored)
         const int64_t token = DEALT ? (int64_t)((uint32_t)row / (uint32_t)x.choices) : row;
         xr[t] = static_cast<const T *>(x.x) + token * x.token_stride + (DEALT ? (row - token * x.choices) * x.choice_stride : 0);
     }
-    const uint32_t *levels = reinterpret_cast<const uint32_t *>(packed + m.code_bytes());
+    // the part of the columns, in blocks
+    const int begin = (int)((int64_t)m.blocks * blockIdx.z / gridDim.z), end = (int)((int64_t)m.blocks * (blockIdx.z + 1) / gridDim.z);
+    if constexpr (!DEALT) out += blockIdx.z * x.count * m.N;
+    const uint4 *codes[R];
+    const uint32_t *levels[R];
+#pragma unroll
+    for (int r = 0; r < R; r++) {
+        const int64_t at = (int64_t)(row0 + r < m.rows ? row0 + r : m.rows - 1) * m.blocks;
+        codes[r] = reinterpret_cast<const uint4 *>(packed) + at * 64 + lane;
+        levels[r] = reinterpret_cast<const uint32_t *>(packed + m.code_bytes()) + at * GPB * 16 + col;
+    }
     Sum4 total[R][TB];
 #pragma unroll
     for (int r = 0; r < R; r++)
 #pragma unroll
         for (int t = 0; t < TB; t++) total[r][t] = 0.f;
-    for (int k = wave; k < m.blocks; k += kWaves) {
-        uint4 codes[R], level[R][GPB];
+    struct Block {
+        uint4 codes[R];
+        uint32_t level[R][GPB];
+        Columns<T> columns[4][TB];
+    };
+    const auto bring_matrix = [&](Block &b, int k) {
 #pragma unroll
         for (int r = 0; r < R; r++) {
-            const int row = row0 + r < m.rows ? row0 + r : m.rows - 1;
-            codes[r] = reinterpret_cast<const uint4 *>(packed)[((int64_t)row * m.blocks + k) * 64 + lane];
+            b.codes[r] = codes[r][(int64_t)k * 64];
 #pragma unroll
-            for (int g = 0; g < GPB; g++)
-                level[r][g] = *reinterpret_cast<const uint4 *>(levels + (((int64_t)row * m.blocks + k) * GPB + g) * 16 + 4 * quarter);
+            for (int g = 0; g < GPB; g++) b.level[r][g] = levels[r][(k * GPB + g) * 16];
         }
-        Columns<T> columns[4][TB];
-        const auto load = [&](auto of) {
+    };
+    const auto bring_rows = [&](Block &b, int k, auto of) {
 #pragma unroll
-            for (int w = 0; w < 4; w++)
+        for (int w = 0; w < 4; w++)
 #pragma unroll
-                for (int t = 0; t < TB; t++) columns[w][t] = of(xr[t], 128 * k + 32 * w + 8 * quarter);
-        };
-        if (128 * (k + 1) <= m.K) load([&](const T *row, int at) { return load_columns(row + at); });
-        else if (m.K >= 8) load([&](const T *row, int at) { return load_last_columns(row, at, m.K); });
-        else load([&](const T *row, int at) { return at == 0 ? load_short_columns(row, m.K) : no_columns<T>(); });
+            for (int t = 0; t < TB; t++) b.columns[w][t] = of(xr[t], 128 * k + 32 * w + 8 * quarter);
+    };
+    const auto multiply = [&](const Block &b) {
 #pragma unroll
         for (int g = 0; g < GPB; g++) {
             Sum4 sum[R][TB], of_x[TB];
@@ -85,32 +95,60 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
             }
 #pragma unroll
             for (int w = 4 / GPB * g; w < 4 / GPB * (g + 1); w++) {
-                typename O::Eight a[R];
+                typename O::Eight c[R], o[TB][P];
 #pragma unroll
-                for (int r = 0; r < R; r++) a[r] = code_operands<T>(w == 0 ? codes[r].x : w == 1 ? codes[r].y : w == 2 ? codes[r].z : codes[r].w);
+                for (int t = 0; t < TB; t++) to_operands<T>(b.columns[w][t], o[t]);
 #pragma unroll
-                for (int t = 0; t < TB; t++) {
-                    typename O::Eight b[P];
-                    to_operands<T>(columns[w][t], b);
+                for (int r = 0; r < R; r++) c[r] = code_operands<T>(w == 0 ? b.codes[r].x : w == 1 ? b.codes[r].y : w == 2 ? b.codes[r].z : b.codes[r].w);
+#pragma unroll
+                for (int t = 0; t < TB; t++)
 #pragma unroll
                     for (int p = 0; p < P; p++) {
-                        of_x[t] = O::product(ones<T>(), b[p], of_x[t]);
+                        of_x[t] = O::product(o[t][p], ones<T>(), of_x[t]);
 #pragma unroll
-                        for (int r = 0; r < R; r++) sum[r][t] = O::product(a[r], b[p], sum[r][t]);
+                        for (int r = 0; r < R; r++) sum[r][t] = O::product(o[t][p], c[r], sum[r][t]);
                     }
-                }
             }
 #pragma unroll
-            for (int r = 0; r < R; r++)
+            for (int r = 0; r < R; r++) {
+                const float scale = __builtin_bit_cast(float, b.level[r][g] << 16), low = __builtin_bit_cast(float, b.level[r][g] & 0xffff0000u);
+                const float rest = fmaf(-O::kMore, scale, low);
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    const uint32_t word = i == 0 ? level[r][g].x : i == 1 ? level[r][g].y : i == 2 ? level[r][g].z : level[r][g].w;
-                    const float scale = __builtin_bit_cast(float, word << 16), low = __builtin_bit_cast(float, word & 0xffff0000u);
-                    const float rest = fmaf(-O::kMore, scale, low);
+                for (int t = 0; t < TB; t++)
 #pragma unroll
-                    for (int t = 0; t < TB; t++) total[r][t][i] = fmaf(scale, sum[r][t][i], fmaf(rest, of_x[t][i], total[r][t][i]));
-                }
+                    for (int i = 0; i < 4; i++) total[r][t][i] = fmaf(scale, sum[r][t][i], fmaf(rest, of_x[t][i], total[r][t][i]));
+            }
         }
+    };
+    const auto whole = [](const T *row, int at) { return load_columns(row + at); };
+    const int full = m.K / 128 < end ? m.K / 128 : end;
+    int k = begin + wave;
+    Block now;
+    if (TB == 1 && k < full) {
+        bring_matrix(now, k);
+        bring_rows(now, k, whole);
+    }
+    for (; k < full; k += kWaves) {
+        if constexpr (TB == 1) {
+            Block next;
+            if (k + kWaves < full) {
+                bring_matrix(next, k + kWaves);
+                bring_rows(next, k + kWaves, whole);
+            }
+            multiply(now);
+            now = next;
+        } else {
+            bring_matrix(now, k);
+            bring_rows(now, k, whole);
+            multiply(now);
+        }
+    }
+    if (full < end && wave == (full - begin) % kWaves) {
+        Block last;
+        bring_matrix(last, full);
+        if (m.K >= 8) bring_rows(last, full, [&](const T *row, int at) { return load_last_columns(row, at, m.K); });
+        else bring_rows(last, full, [&](const T *row, int at) { return at == 0 ? load_short_columns(row, m.K) : no_columns<T>(); });
+        multiply(last);
     }
 #pragma unroll
     for (int r = 0; r < R; r++)
@@ -121,52 +159,61 @@ __global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRo
         Sum4 y = part[0][i][lane];
 #pragma unroll
         for (int w = 1; w < kWaves; w++) y += part[w][i][lane];
-        const int r = i / TB, t = i - r * TB, n = 16 * (row0 + r) + 4 * quarter;
-        int64_t row = to[0];
+        const int r = i / TB, t = i - r * TB, n = 16 * (row0 + r) + col;
 #pragma unroll
-        for (int j = 1; j < TB; j++) row = t == j ? to[j] : row;
-        if (16 * t + col >= count) continue;
-#pragma unroll
-        for (int j = 0; j < 4; j++)
-            if (n + j < m.N) out[row * m.N + n + j] = from_float<Out>(y[j]);
+        for (int j = 0; j < 4; j++) {
+            const int at = 16 * t + 4 * quarter + j;
+            if (at < count && n < m.N) out[row_of(at) * m.N + n] = from_float<Out>(y[j]);
+        }
     }
 }
 
 template <typename T, typename Out, bool DEALT>
-void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int64_t tiles, hipStream_t s) {
-    const auto launch = [&](auto kernel, int r, int64_t y) {
+void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int64_t tiles, const FewShape &shape, hipStream_t s) {
+    const auto launch = [&](auto kernel, int tb, int r) {
+        const int64_t y = DEALT ? tiles : (x.count + 16 * tb - 1) / (16 * tb);
         const int row_tiles = (m.rows + r - 1) / r;
         // (a launch has fewer than 2^32 threads, and a grid's second dimension than 2^16)
-        const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, (1 << 22) / row_tiles));
+        const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, (1 << 22) / (row_tiles * shape.split)));
         for (int64_t at = 0; at < y; at += most)
-            kernel<<<dim3(row_tiles, (unsigned)std::min(most, y - at)), 64 * kWaves, 0, s>>>(m, x, deal, (Out *)x.out, (int)at);
+            kernel<<<dim3(row_tiles, (unsigned)std::min(most, y - at), shape.split), 64 * few_waves(tb), 0, s>>>(m, x, deal, (Out *)x.out, (int)at);
     };
-    const bool wide = !DEALT && x.count > 16;
-    const int64_t y = DEALT ? tiles : wide ? (x.count + 63) / 64 : (x.count + 15) / 16;
-#define BF_GO(GPB)                                                                       \
-    if constexpr (!DEALT) {                                                              \
-        if (wide) return launch(linear_few_kernel<T, GPB, 4, 1, DEALT, Out>, 1, y);      \
-    }                                                                                    \
-    launch(linear_few_kernel<T, GPB, 1, 1, DEALT, Out>, 1, y)
-    if (group == 128) { BF_GO(1); }
-    else if (group == 64) { BF_GO(2); }
-    else { BF_GO(4); }
+#define BF_GO(GPB)                                                                                                                     \
+    if (DEALT || shape.tb == 1) {                                                                                                      \
+        if (shape.r == 4) launch(linear_few_kernel<T, GPB, 1, 4, DEALT, Out>, 1, 4);                                                   \
+        else if (shape.r == 2) launch(linear_few_kernel<T, GPB, 1, 2, DEALT, Out>, 1, 2);                                              \
+        else launch(linear_few_kernel<T, GPB, 1, 1, DEALT, Out>, 1, 1);                                                                \
+    } else if constexpr (!DEALT) {                                                                                                     \
+        if (shape.tb == 2) launch(linear_few_kernel<T, GPB, 2, few_most_rows<T>, DEALT, Out>, 2, few_most_rows<T>);                    \
+        else if constexpr (sizeof(T) == 2) {                                                                                           \
+            if (shape.tb == 3) launch(linear_few_kernel<T, GPB, 3, 4, DEALT, Out>, 3, 4);                                              \
+            else launch(linear_few_kernel<T, GPB, 4, 4, DEALT, Out>, 4, 4);                                                            \
+        }                                                                                                                              \
+    }
+    if (group == 128) { BF_GO(1) }
+    else if (group == 64) { BF_GO(2) }
+    else { BF_GO(4) }
 #undef BF_GO
 }
 
 template <typename T>
-void by_rows(const Matrices &m, int group, const XRows &x, const Deal *deal, int tiles, bool to_float, hipStream_t s) {
-    if (!deal) go<T, T, false>(m, group, x, Deal{}, 0, s);
-    else if (to_float) go<T, float, true>(m, group, x, *deal, tiles, s);
-    else go<T, T, true>(m, group, x, *deal, tiles, s);
+void by_rows(const Matrices &m, int group, const XRows &x, const Deal *deal, int tiles, bool to_float, const FewShape &shape, hipStream_t s) {
+    if (deal) {
+        if (to_float) go<T, float, true>(m, group, x, *deal, tiles, shape, s);
+        else go<T, T, true>(m, group, x, *deal, tiles, shape, s);
+    } else {
+        if (to_float) go<T, float, false>(m, group, x, Deal{}, 0, shape, s);
+        else go<T, T, false>(m, group, x, Deal{}, 0, shape, s);
+    }
 }
 
 }  // namespace
 
-hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, hipStream_t s) {
-    if (dtype == BIFEAT_F32) by_rows<float>(m, group, x, deal, most_tiles, to_float, s);
-    else if (dtype == BIFEAT_F16) by_rows<Half16>(m, group, x, deal, most_tiles, to_float, s);
-    else by_rows<Brain16>(m, group, x, deal, most_tiles, to_float, s);
+hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, const FewShape &shape,
+                             hipStream_t s) {
+    if (dtype == BIFEAT_F32) by_rows<float>(m, group, x, deal, most_tiles, to_float, shape, s);
+    else if (dtype == BIFEAT_F16) by_rows<Half16>(m, group, x, deal, most_tiles, to_float, shape, s);
+    else by_rows<Brain16>(m, group, x, deal, most_tiles, to_float, shape, s);
     return hipGetLastError();
 }
 

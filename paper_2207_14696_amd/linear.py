@@ -27,7 +27,7 @@ class PackedLinear:
         self.experts = None if experts is None else int(experts)
         # what the native module's calls begin with: entry points, sizes
         sizes = (self.out_features, self.in_features, self.group)
-        self._multiply = (_b._address(self._lib.bifeat_linear_multiply), *sizes, self.bytes)
+        self._multiply = (_b._address(self._lib.bifeat_linear_workspace), _b._address(self._lib.bifeat_linear_multiply), *sizes, self.bytes)
         self._by_experts = (_b._address(self._lib.bifeat_linear_experts_workspace), _b._address(self._lib.bifeat_linear_experts), *sizes,
                             self.experts, self.bytes)
 
@@ -89,8 +89,12 @@ class PackedLinear:
         elif out.shape != shape or out.dtype != x.dtype:
             raise ValueError(f"out must be {list(shape)} of x's type")
         ptr = self._packed(packed, rows, out)
+        need = self._lib.bifeat_linear_workspace(C.byref(self._spec), rows.shape[0], code)
+        if need < 0:
+            _check(int(need))
+        room = torch.empty(need, dtype=torch.uint8, device=x.device)
         _check(self._lib.bifeat_linear_multiply(C.byref(self._spec), ptr, rows.data_ptr(), rows.stride(0), rows.shape[0], code, _dev_ptr(out),
-                                                _stream()))
+                                                room.data_ptr(), need, _stream()))
         return out
 
     def multiply_experts(self, packed, x, ids, weights=None, out=None):

@@ -48,13 +48,19 @@ def test_linear_argument_errors_come_before_any_gpu_call(bf):
     assert pack(s=spec(n=0)) == pack(w=None) == pack(w=2) == pack(t=3) == pack(p=None) == pack(p=8) == -1
     assert lib.bifeat_linear_unpack(spec(), None, 16, None) == -1 and lib.bifeat_linear_unpack(spec(), 16, 2, None) == -1
 
-    def multiply(s=None, p=16, x=16, stride=64, rows=3, t=0, out=16):
-        return lib.bifeat_linear_multiply(s or spec(), p, x, stride, rows, t, out, None)
+    def multiply(s=None, p=16, x=16, stride=64, rows=3, t=0, out=16, room=16, size=1 << 40):
+        return lib.bifeat_linear_multiply(s or spec(), p, x, stride, rows, t, out, room, size, None)
+
+    def room(s=None, rows=3, t=0):
+        return lib.bifeat_linear_workspace(s or spec(), rows, t)
+
+    assert room(s=spec(experts=2)) == room(s=spec(group=1)) == room(rows=-1) == room(t=3) == -1 and room(rows=0) >= 0
 
     assert multiply(s=spec(experts=2)) == multiply(s=spec(k=-1)) == multiply(p=None) == multiply(p=8) == multiply(x=None) == multiply(x=2) == -1
     assert multiply(stride=-1) == multiply(rows=-1) == multiply(rows=1 << 31) == multiply(t=-1) == multiply(t=3) == -1
     assert multiply(out=None) == multiply(out=1, t=1) == multiply(x=1, t=2) == -1
-    assert multiply(rows=0, x=None, out=None, p=None) == 0
+    assert multiply(room=8) == -1
+    assert multiply(rows=0, x=None, out=None, p=None, room=None, size=0) == 0
 
     def rows(x=16, ts=64, cs=0, ids=16, w=None, tokens=3, choices=2):
         return C.byref(_CExpertRows(x, ts, cs, ids, w, tokens, choices))
