@@ -53,6 +53,10 @@ template <typename T>
 __device__ inline typename Operand<T>::Eight code_operands(uint32_t w) {
     typedef Operand<T> O;
     uint32_t __attribute__((ext_vector_type(4))) r;
+    // (in registers, so that one instruction does both; as constants they would be two)
+    uint32_t mask = O::kMask, sixteen = O::kSixteen;
+    asm("" : "+v"(mask));
+    asm("" : "+s"(sixteen));
     if constexpr (O::kMore == 0.f) {
         // (a code is a 32-bit float of which bfloat16 is the upper half)
         const uint32_t even = w & 0x0f0f0f0fu, odd = w >> 4 & 0x0f0f0f0fu;
@@ -65,7 +69,7 @@ __device__ inline typename Operand<T>::Eight code_operands(uint32_t w) {
         return __builtin_bit_cast(typename O::Eight, r);
     }
 #pragma unroll
-    for (int j = 0; j < 4; j++) r[j] = ((O::kShift[j] > 0 ? w << (O::kShift[j] & 31) : w >> (-O::kShift[j] & 31)) & O::kMask) | O::kSixteen;
+    for (int j = 0; j < 4; j++) r[j] = ((O::kShift[j] > 0 ? w << (O::kShift[j] & 31) : w >> (-O::kShift[j] & 31)) & mask) | sixteen;
     return __builtin_bit_cast(typename O::Eight, r);
 }
 template <typename T>
@@ -125,6 +129,10 @@ struct XRows {
     int choices;  // rows of a token (1 without experts)
     int64_t count;
     void *out;
+    // of many rows, the sums of each group's columns: [3][sum_rows][sum_groups] bfloat16, a row of x as often as it lies in memory
+    const uint16_t *sums;
+    int64_t sum_rows;
+    int sum_groups;  // a multiple of 16
 };
 
 // Where rows are dealt to experts, the pairs of a token and one of its choices lie in `order` expert by expert, and a tile is up to
@@ -151,6 +159,7 @@ hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const
                              hipStream_t s);
 // ... of K >= 8 columns, tiles of kManyRows
 constexpr int kManyRows = 128;
+hipError_t launch_linear_sums(const Matrices &m, int group, const XRows &x, int dtype, hipStream_t s);
 hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, int split, hipStream_t s);
 // out = the parts' sum, `count` numbers each
 hipError_t launch_linear_add(const float *parts, int split, int64_t count, int dtype, void *out, hipStream_t s);

@@ -26,11 +26,16 @@ bf::Matrices matrices_of(const bifeat_linear_spec *s, const uint8_t *packed) {
     return {packed, (int64_t)rows * blocks * (1024 + 64 * (128 / s->group)), s->out_features, s->in_features, rows, blocks, s->experts};
 }
 
+int sum_groups(const bifeat_linear_spec *s) { return ((s->in_features + 127) / 128 * (128 / s->group) + 15) / 16 * 16; }
+int64_t sum_bytes(const bifeat_linear_spec *s, int64_t rows) { return 3 * rows * sum_groups(s) * 2; }
+
 // How a product of rows with one matrix is taken.
 struct Plan {
     bool many;
     int tb, r, split;
-    int64_t bytes(const bifeat_linear_spec *s, int64_t rows) const { return split > 1 ? split * rows * s->out_features * 4 : 0; }
+    // the workspace: parts of the sums, then the sums of x
+    int64_t parts_bytes(const bifeat_linear_spec *s, int64_t rows) const { return split > 1 ? (split * rows * s->out_features + 3) / 4 * 16 : 0; }
+    int64_t bytes(const bifeat_linear_spec *s, int64_t rows) const { return parts_bytes(s, rows) + (many ? sum_bytes(s, rows) : 0); }
 };
 Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
     const int64_t rows16 = (s->out_features + 15) / 16, blocks = (s->in_features + 127) / 128;
@@ -53,10 +58,11 @@ bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
            r->tokens <= (INT32_MAX - 64) / r->choices;
 }
 
-// The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, the parts' counts, 32-bit products.
+// The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, the parts' counts, the sums of x, 32-bit products.
 struct Room {
     int tile;
-    int64_t most_tiles, order, counts, products, bytes;
+    int64_t most_tiles, order, counts, sums, products, bytes;
+    int64_t sum_rows;  // of many rows: rows of x
 };
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
@@ -66,7 +72,9 @@ Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
     o.counts = o.order + (pairs + 3) / 4 * 16;
     const int parts = bf::deal_parts(pairs);
-    o.products = o.counts + (parts > 1 ? ((int64_t)parts * (s->experts + 1) + 3) / 4 * 16 : 0);
+    o.sums = o.counts + (parts > 1 ? ((int64_t)parts * (s->experts + 1) + 3) / 4 * 16 : 0);
+    o.sum_rows = o.tile == 16 ? 0 : r->choice_stride ? pairs : r->tokens;
+    o.products = o.sums + sum_bytes(s, o.sum_rows);
     o.bytes = o.products + (r->weights ? pairs * s->out_features * 4 : 0);
     return o;
 }
@@ -104,9 +112,12 @@ int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed
     const bf::Matrices m = matrices_of(spec, packed);
     const hipStream_t s = (hipStream_t)stream;
     const bool split = plan.split > 1;
-    const bf::XRows r{x, row_stride, 0, 1, rows, split ? workspace : out};
-    if (plan.many) BF_HIP(bf::launch_linear_many(m, spec->group, r, nullptr, 0, dtype, split, plan.split, s));
-    else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split}, s));
+    bf::XRows r{x, row_stride, 0, 1, rows, split ? workspace : out, nullptr, rows, sum_groups(spec)};
+    if (plan.many) {
+        r.sums = reinterpret_cast<const uint16_t *>(static_cast<uint8_t *>(workspace) + plan.parts_bytes(spec, rows));
+        BF_HIP(bf::launch_linear_sums(m, spec->group, r, dtype, s));
+        BF_HIP(bf::launch_linear_many(m, spec->group, r, nullptr, 0, dtype, split, plan.split, s));
+    } else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split}, s));
     if (split) BF_HIP(bf::launch_linear_add(static_cast<const float *>(workspace), plan.split, rows * m.N, dtype, out, s));
     return BIFEAT_OK;
 }
@@ -133,10 +144,14 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     float *products = reinterpret_cast<float *>(w + room.products);
     BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, reinterpret_cast<int *>(w + room.counts), tiles_count, tiles, order, s));
     const bf::Deal deal{tiles_count, tiles, order};
-    const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out};
+    const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out,
+                      reinterpret_cast<const uint16_t *>(w + room.sums), room.sum_rows, sum_groups(spec)};
     const bool to_float = r->weights != nullptr;
     if (room.tile == 16) BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, {1, 2, 1}, s));
-    else BF_HIP(bf::launch_linear_many(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, 1, s));
+    else {
+        BF_HIP(bf::launch_linear_sums(m, spec->group, x, dtype, s));
+        BF_HIP(bf::launch_linear_many(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, 1, s));
+    }
     if (r->weights) BF_HIP(bf::launch_linear_join(products, r->ids, r->weights, r->tokens, r->choices, spec->experts, m.N, dtype, out, s));
     return BIFEAT_OK;
 }

@@ -38,9 +38,50 @@ __device__ inline float of_neighbour(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, x), CTRL, 0xf, 0xf, true));
 }
 
-// Rows have 8 columns at least.  A workgroup of four waves takes 128 rows of the matrix and 128 of x, a wave 64 of each.  Codes come from memory as the operands that they are; x goes through
-// LDS, by steps of kStep columns, the next two steps' on their way while this one's products run; each four lanes that bring 32 columns of a row add them up on the
-// way.
+typedef Operand<Brain16>::Eight Brains;
+
+// The sums of each group's columns of the rows of x, each as three bfloat16 that are it together: sums[piece][row][group], groups past the last as zeros.
+// A wave takes a row, a lane eight columns.  The products take them times what is to be added for each column of a group, see below.
+template <typename T, int GPB>
+__global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t rows, int K, int groups, uint16_t *sums) {
+    constexpr int kLanes = 16 / GPB;  // of a group
+    const int lane = threadIdx.x % 64;
+    const int64_t r = (int64_t)blockIdx.x * (kThreads / 64) + threadIdx.x / 64;
+    if (r >= rows) return;
+    const int64_t token = x.choice_stride ? r / x.choices : r;
+    const T *row = static_cast<const T *>(x.x) + token * x.token_stride + (x.choice_stride ? (r - token * x.choices) * x.choice_stride : 0);
+    const auto put = [&](int at, const Columns<T> &c) {
+        float y = sum_of(c);
+        y += of_neighbour<0xb1>(y);                               // lane ^ 1
+        y += of_neighbour<0x4e>(y);                               // lane ^ 2
+        if constexpr (kLanes >= 8) y += of_neighbour<0x141>(y);   // the other four of eight
+        if constexpr (kLanes >= 16) y += of_neighbour<0x140>(y);  // the other eight of sixteen
+        const int g = at / (8 * kLanes);
+        if (lane % kLanes == 0 && g < groups)
+#pragma unroll
+            for (int p = 0; p < 3; p++) {
+                const uint32_t piece = __builtin_bit_cast(uint32_t, y) & 0xffff0000u;
+                sums[((int64_t)p * rows + r) * groups + g] = (uint16_t)(piece >> 16);
+                y -= __builtin_bit_cast(float, piece);
+            }
+    };
+    constexpr int kAhead = 4;
+    int at = 8 * lane;
+    for (; at - 8 * lane + 512 * kAhead <= K; at += 512 * kAhead) {
+        Columns<T> c[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) c[i] = load_columns(row + at + 512 * i);
+#pragma unroll
+        for (int i = 0; i < kAhead; i++) put(at + 512 * i, c[i]);
+    }
+    for (; at - 8 * lane < groups * 8 * kLanes; at += 512) put(at, load_last_columns(row, at, K));
+}
+
+// Rows have 8 columns at least.  A workgroup of four waves takes 128 rows of the matrix and 128 of x, a wave 32 of the matrix's and all of x's (64 of each would
+// unpack each code twice).  Codes come from memory as the operands that they are; x goes through LDS, by steps of kStep columns, those two and three steps on
+// on their way while this one's products run.
+// What (m_g - 16 s_g) sum x adds is a product too, of groups in place of columns: minimum and scale are bfloat16, the sums three of them (the kernel above),
+// so six exact products take 16 groups at a time, where adding it after each group would take two instructions a sum more.
 constexpr int kRows = kManyRows;
 template <typename T> constexpr int kStep = sizeof(T) == 4 ? 32 : 64;
 
@@ -51,8 +92,6 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
     constexpr int P = O::kPieces, S = kStep<T>, kChunks = S / 8, kLoads = kRows * kChunks / 256;
     constexpr int kStride = kRows + 1;  // (of a chunk in 16 bytes: the lanes that write a row's chunks meet no two in a bank)
     __shared__ uint4 tile[2][P][kChunks * kStride];
-    __shared__ float sums[2][GPB][kRows];       // [of this block, the next][group]: of x
-    __shared__ float levels[2][2][GPB][kRows];  // [of this block, the next][scale, rest]
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 32, half = lane / 32;
     const int n_tile = blockIdx.x % row_tiles, x_tile = tile0 + blockIdx.x / row_tiles;
     int64_t first = (int64_t)x_tile * kRows;
@@ -87,26 +126,21 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
     }
     const int begin = (int)((int64_t)m.blocks * blockIdx.y / gridDim.y), end = (int)((int64_t)m.blocks * (blockIdx.y + 1) / gridDim.y);  // of the columns
     if constexpr (!DEALT) out += blockIdx.y * x.count * m.N;
-    const int n0 = kRows * n_tile + 64 * (wave % 2), t0 = 64 * (wave / 2);  // the wave's part
+    const int n0 = kRows * n_tile + 32 * wave;  // the wave's rows of the matrix
     const uint4 *codes = reinterpret_cast<const uint4 *>(packed);
     const uint32_t *all_levels = reinterpret_cast<const uint32_t *>(packed + m.code_bytes());
     const int groups = m.blocks * GPB;
     const auto row16 = [&](int r) { return r < m.rows ? r : m.rows - 1; };
-    Sum16 total[2][2], sum[2][2];
+    Sum16 total[4], sum[4];
 #pragma unroll
-    for (int i = 0; i < 2; i++)
-#pragma unroll
-        for (int j = 0; j < 2; j++) total[i][j] = 0.f;
+    for (int j = 0; j < 4; j++) total[j] = 0.f;
 
-    Columns<T> coming[2][kLoads];  // of the next step, and of the one after it
+    Columns<T> coming[2][kLoads];  // of the next steps, by turns
     const auto bring = [&](int step, Columns<T> (&c)[kLoads]) {
 #pragma unroll
         for (int i = 0; i < kLoads; i++) c[i] = load_columns(from[i] + S * step + 8 * chunk);
     };
-    constexpr int kGroup = 128 / GPB, kPerGroup = kGroup > S ? kGroup / S : 1;  // steps
-    constexpr int kLanes = (kGroup < S ? kGroup : S) / 8;                        // that bring a row's columns of a group
-    float so_far[kLoads];
-    const auto put = [&](int k, int part, const Columns<T> (&c)[kLoads]) {  // what has come, of part `part` of block k
+    const auto put = [&](int part, const Columns<T> (&c)[kLoads]) {  // what has come, of a block's part
 #pragma unroll
         for (int i = 0; i < kLoads; i++) {
             const int at = threadIdx.x / kChunks + i * (256 / kChunks);
@@ -114,106 +148,116 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
             to_operands<T>(c[i], b);
 #pragma unroll
             for (int p = 0; p < P; p++) tile[part & 1][p][chunk * kStride + at] = __builtin_bit_cast(uint4, b[p]);
-            float y = sum_of(c[i]);
-            if (part % kPerGroup != 0) y += so_far[i];
-            so_far[i] = y;
-            if (part % kPerGroup == kPerGroup - 1) {
-                y += of_neighbour<0xb1>(y);                        // lane ^ 1
-                y += of_neighbour<0x4e>(y);                        // lane ^ 2
-                if constexpr (kLanes == 8) y += of_neighbour<0x141>(y);  // the other four of eight
-                if (chunk % kLanes == 0) sums[k & 1][(S * part + 8 * chunk) / kGroup][at] = y;
-            }
         }
     };
-    uint32_t level[GPB];
-    const auto bring_levels = [&](int k) {  // of block k: a thread has a row, as another one has
-        const int n = threadIdx.x % kRows, r = row16(kRows / 16 * n_tile + n / 16);
+    const uint32_t *my_levels = all_levels + (int64_t)row16(n0 / 16 + col / 16) * groups * 16 + col % 16;
+    uint32_t level[GPB], level_now[GPB];
+    const auto bring_levels = [&](int k) {
 #pragma unroll
-        for (int g = 0; g < GPB; g++) level[g] = all_levels[((int64_t)r * groups + k * GPB + g) * 16 + n % 16];
+        for (int g = 0; g < GPB; g++) level[g] = my_levels[(k * GPB + g) * 16];
     };
-    const auto put_levels = [&](int buffer) {
-        if (threadIdx.x < kRows)
-#pragma unroll
-            for (int g = 0; g < GPB; g++) {
-                const float scale = __builtin_bit_cast(float, level[g] << 16), low = __builtin_bit_cast(float, level[g] & 0xffff0000u);
-                levels[buffer][0][g][threadIdx.x] = scale;
-                levels[buffer][1][g][threadIdx.x] = fmaf(-O::kMore, scale, low);
-            }
-    };
-    const uint4 *my_codes[2];
-#pragma unroll
-    for (int i = 0; i < 2; i++) my_codes[i] = codes + (int64_t)row16(n0 / 16 + 2 * i + col / 16) * m.blocks * 64 + col % 16 + 16 * half;
-    uint4 a[2][2], now[2][2];
+    const uint4 *my_codes = codes + (int64_t)row16(n0 / 16 + col / 16) * m.blocks * 64 + col % 16 + 16 * half;
+    uint4 a[2], now[2];
     const auto bring_codes = [&](int k) {
 #pragma unroll
-        for (int i = 0; i < 2; i++)
-#pragma unroll
-            for (int e = 0; e < 2; e++) a[i][e] = my_codes[i][(int64_t)k * 64 + 32 * e];
+        for (int e = 0; e < 2; e++) a[e] = my_codes[(int64_t)k * 64 + 32 * e];
     };
-    const auto take_codes = [&] {
+    const auto take = [&] {
 #pragma unroll
-        for (int i = 0; i < 2; i++)
+        for (int e = 0; e < 2; e++) now[e] = a[e];
 #pragma unroll
-            for (int e = 0; e < 2; e++) now[i][e] = a[i][e];
+        for (int g = 0; g < GPB; g++) level_now[g] = level[g];
     };
-    const auto multiply = [&](int k, int part) {
+    const auto multiply = [&](int part) {
+        constexpr int kDeep = P == 1 ? 2 : 1;  // (of three pieces two would not fit the registers)
+        Operands b[kDeep][4][P];
+        const auto read = [&](int s16) {
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int p = 0; p < P; p++)
+                    b[s16 % kDeep][j][p] = __builtin_bit_cast(Operands, tile[part & 1][p][(2 * s16 + half) * kStride + 32 * j + col]);
+        };
+        if (kDeep == 2) read(0);
 #pragma unroll
         for (int s16 = 0; s16 < S / 16; s16++) {
             const int s = part * (S / 16) + s16;  // of the block's eight
             constexpr int kPer = 8 / GPB;         // 16 columns at a time, of a group
-            const bool begins = s % kPer == 0;
-            Operands b[2][P];
+            if (kDeep == 1) read(s16);
+            else if (s16 + 1 < S / 16) read(s16 + 1);
+            __builtin_amdgcn_sched_barrier(0x11);  // (reads stay ahead of the products)
+            const uint4 w = now[s % 2];
+            const Operands c = code_operands<T>(s / 2 == 0 ? w.x : s / 2 == 1 ? w.y : s / 2 == 2 ? w.z : w.w);
 #pragma unroll
-            for (int j = 0; j < 2; j++)
+            for (int j = 0; j < 4; j++)
 #pragma unroll
-                for (int p = 0; p < P; p++)
-                    b[j][p] = __builtin_bit_cast(Operands, tile[part & 1][p][(2 * s16 + half) * kStride + t0 + 32 * j + col]);
+                for (int p = 0; p < P; p++) {
+                    if (s % kPer == 0 && p == 0) {
+                        Sum16 zero;
 #pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const uint4 w = now[i][s % 2];
-                const Operands c = code_operands<T>(s / 2 == 0 ? w.x : s / 2 == 1 ? w.y : s / 2 == 2 ? w.z : w.w);
-#pragma unroll
-                for (int j = 0; j < 2; j++) {
-#pragma unroll
-                    for (int p = 0; p < P; p++) {
-                        if (begins && p == 0) {
-                            Sum16 zero;
-#pragma unroll
-                            for (int e = 0; e < 16; e++) zero[e] = 0.f;
-                            sum[i][j] = product32<T>(b[j][p], c, zero);
-                        } else {
-                            sum[i][j] = product32<T>(b[j][p], c, sum[i][j]);
-                        }
+                        for (int e = 0; e < 16; e++) zero[e] = 0.f;
+                        sum[j] = product32<T>(b[s16 % kDeep][j][p], c, zero);
+                    } else {
+                        sum[j] = product32<T>(b[s16 % kDeep][j][p], c, sum[j]);
                     }
                 }
-            }
             if (s % kPer == kPer - 1) {
                 const int g = s / kPer;
                 __builtin_amdgcn_sched_barrier(0);
-                float scale[2], rest[2];
+                const float scale = __builtin_bit_cast(float, level_now[g] << 16);
 #pragma unroll
-                for (int i = 0; i < 2; i++) {
-                    scale[i] = levels[k & 1][0][g][64 * (wave % 2) + 32 * i + col];
-                    rest[i] = levels[k & 1][1][g][64 * (wave % 2) + 32 * i + col];
-                }
+                for (int j = 0; j < 4; j++)
 #pragma unroll
-                for (int j = 0; j < 2; j++)
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        const Sum4 of_x = *reinterpret_cast<const Sum4 *>(&sums[k & 1][g][t0 + 32 * j + 8 * e + 4 * half]);
-#pragma unroll
-                        for (int i = 0; i < 2; i++)
-#pragma unroll
-                            for (int c = 0; c < 4; c++)
-                                total[i][j][4 * e + c] = fmaf(scale[i], sum[i][j][4 * e + c], fmaf(rest[i], of_x[c], total[i][j][4 * e + c]));
-                    }
+                    for (int e = 0; e < 16; e++) total[j][e] = fmaf(scale, sum[j][e], total[j][e]);
                 // (here and not where they are used next: the compiler would keep what they are made of until then)
 #pragma unroll
-                for (int i = 0; i < 2; i++)
-#pragma unroll
-                    for (int j = 0; j < 2; j++) asm volatile("" : "+v"(total[i][j]));
+                for (int j = 0; j < 4; j++) asm volatile("" : "+v"(total[j]));
                 __builtin_amdgcn_sched_barrier(0);
             }
+        }
+    };
+    const auto add_sums = [&] {
+        int64_t at[4];
+#pragma unroll
+        for (int j = 0; j < 4; j++) {
+            int64_t row = first + (32 * j + col < count ? 32 * j + col : count - 1);
+            if constexpr (DEALT) row = x.choice_stride ? deal.order[row] : (int64_t)((uint32_t)deal.order[row] / (uint32_t)x.choices);
+            at[j] = row * x.sum_groups;
+        }
+        for (int g0 = begin * GPB / 16 * 16; g0 < end * GPB; g0 += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int i = 0; i < 8; i++) {
+                const int g = g0 + 8 * half + i;
+                w[i] = my_levels[(g < groups ? g : groups - 1) * 16];
+                w[i] = g >= begin * GPB && g < end * GPB ? w[i] : 0u;  // (of the part of the columns)
+            }
+            uint4 of[4][3];
+#pragma unroll
+            for (int j = 0; j < 4; j++)
+#pragma unroll
+                for (int p = 0; p < 3; p++) {
+                    struct __attribute__((packed, aligned(4))) Four {
+                        uint32_t w[4];
+                    };
+                    const Four f = *reinterpret_cast<const Four *>(x.sums + p * x.sum_rows * x.sum_groups + at[j] + g0 + 8 * half);
+                    of[j][p] = make_uint4(f.w[0], f.w[1], f.w[2], f.w[3]);
+                }
+            uint32_t __attribute__((ext_vector_type(4))) low, scale;
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                low[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+                // (-kMore times it: the sign, and 4 more in the exponent; a scale of 0 stays it, the largest ones pass what the header allows)
+                const float s0 = __builtin_bit_cast(float, w[2 * i] << 16) * -O::kMore, s1 = __builtin_bit_cast(float, w[2 * i + 1] << 16) * -O::kMore;
+                scale[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, s1), __builtin_bit_cast(uint32_t, s0), 0x07060302u);
+            }
+#pragma unroll
+            for (int p = 2; p >= 0; p--)
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    total[j] = product32<Brain16>(__builtin_bit_cast(Brains, of[j][p]), __builtin_bit_cast(Brains, low), total[j]);
+                    if constexpr (O::kMore != 0.f) total[j] = product32<Brain16>(__builtin_bit_cast(Brains, of[j][p]), __builtin_bit_cast(Brains, scale), total[j]);
+                }
         }
     };
     // Whole blocks: no branch leads to a load, so that none is waited for before its use; what is asked for past the last step is the last again.
@@ -225,53 +269,50 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
         bring(begin * kParts + 1, coming[1]);
         bring_levels(begin);
         bring_codes(begin);
-        put(begin, 0, coming[0]);
-        put_levels(begin & 1);
+        add_sums();
+        put(0, coming[0]);
+        bring(begin * kParts + 2 < last ? begin * kParts + 2 : last, coming[0]);
         __syncthreads();
         for (int k = begin; k < whole; k++) {
             const int next = k + 1 < whole ? k + 1 : k;
-            take_codes();
+            take();
             bring_codes(next);
             bring_levels(next);
 #pragma unroll
             for (int part = 0; part < kParts; part++) {
-                const int ahead = k * kParts + part + 2;
-                bring(ahead < last ? ahead : last, coming[part & 1]);
-                put(part == kParts - 1 ? k + 1 : k, (part + 1) % kParts, coming[(part + 1) & 1]);
-                multiply(k, part);
-                if (part == kParts - 1) put_levels((k + 1) & 1);
+                const int ahead = k * kParts + part + 3;
+                put((part + 1) % kParts, coming[(part + 1) & 1]);
+                bring(ahead < last ? ahead : last, coming[(part + 1) & 1]);
+                multiply(part);
                 __syncthreads();
             }
         }
     }
     if (whole < end) {  // the rows' last columns
+        if (begin >= whole) add_sums();
         bring_levels(whole);
         bring_codes(whole);
-        put_levels(whole & 1);
-        take_codes();
+        take();
 #pragma unroll
         for (int part = 0; part < kParts; part++) {
 #pragma unroll
             for (int i = 0; i < kLoads; i++) coming[0][i] = load_last_columns(from[i], 128 * whole + S * part + 8 * chunk, m.K);
-            put(whole, part, coming[0]);
+            put(part, coming[0]);
             __syncthreads();
-            multiply(whole, part);
+            multiply(part);
             __syncthreads();
         }
     }
+    const int n = n0 + col;
 #pragma unroll
-    for (int j = 0; j < 2; j++)
+    for (int j = 0; j < 4; j++)
 #pragma unroll
         for (int e = 0; e < 16; e++) {
-            const int at = t0 + 32 * j + 8 * (e / 4) + 4 * half + e % 4;
-            if (at >= count) continue;
+            const int at = 32 * j + 8 * (e / 4) + 4 * half + e % 4;
+            if (at >= count || n >= m.N) continue;
             int64_t row = first + at;
             if constexpr (DEALT) row = deal.order[row];
-#pragma unroll
-            for (int i = 0; i < 2; i++) {
-                const int n = n0 + 32 * i + col;
-                if (n < m.N) out[row * m.N + n] = from_float<Out>(total[i][j][e]);
-            }
+            out[row * m.N + n] = from_float<Out>(total[j][e]);
         }
 }
 
@@ -329,6 +370,22 @@ __global__ __launch_bounds__(kThreads) void linear_add_kernel(const float *parts
 }
 
 }  // namespace
+
+hipError_t launch_linear_sums(const Matrices &m, int group, const XRows &x, int dtype, hipStream_t s) {
+    const int64_t rows = x.sum_rows;
+    // (a launch has fewer than 2^32 threads: rows are below 2^31)
+    const unsigned grid = (unsigned)((rows + kThreads / 64 - 1) / (kThreads / 64));
+    uint16_t *sums = const_cast<uint16_t *>(x.sums);
+#define BF_GO(T)                                                                                                              \
+    if (group == 128) linear_sums_kernel<T, 1><<<grid, kThreads, 0, s>>>(x, rows, m.K, x.sum_groups, sums);                  \
+    else if (group == 64) linear_sums_kernel<T, 2><<<grid, kThreads, 0, s>>>(x, rows, m.K, x.sum_groups, sums);              \
+    else linear_sums_kernel<T, 4><<<grid, kThreads, 0, s>>>(x, rows, m.K, x.sum_groups, sums)
+    if (dtype == BIFEAT_F32) { BF_GO(float); }
+    else if (dtype == BIFEAT_F16) { BF_GO(Half16); }
+    else { BF_GO(Brain16); }
+#undef BF_GO
+    return hipGetLastError();
+}
 
 hipError_t launch_linear_many(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, int split, hipStream_t s) {
     if (dtype == BIFEAT_F32) by_rows<float>(m, group, x, deal, most_tiles, to_float, split, s);
