@@ -1,6 +1,4 @@
 // Entry points of the products with matrices in 4 bits: argument checks, and dispatch to the kernels of linear_*.hip.
-#include <stdio.h>
-#include <stdlib.h>
 #include <algorithm>
 
 #include "linear.hpp"
@@ -37,20 +35,31 @@ struct Plan {
     int64_t parts_bytes(const bifeat_linear_spec *s, int64_t rows) const { return split > 1 ? (split * rows * s->out_features + 3) / 4 * 16 : 0; }
     int64_t bytes(const bifeat_linear_spec *s, int64_t rows) const { return parts_bytes(s, rows) + (many ? sum_bytes(s, rows) : 0); }
 };
+// Of the ways to take the rows the one that is the fastest by what they measured (bf16, in parentheses fp32; us; 256 workgroups run at a time, for 128 rows 512):
+//   16 tb rows by 16 r of the matrix a workgroup: 2.5 a call, and a round of workgroups 0.12, 0.2, 0.37, 0.55 a block of columns for tb = 1..4 (0.3, 0.6
+//     for 1, 2): 16 rows by 4096 x 4096 6.8, 64 rows 20; by 16 384 x 4096 24, 128 rows 43;
+//   128 rows by 128: 8 (what is summed first, and the beginning), 1.25 a block (3.6), 2.3 where two workgroups share a CU: 64 rows by 4096 x 4096 46,
+//     1024 51, 2048 83; fp32 64 rows 122, 2048 205;
+//   columns in parts: the parts' sums written and added, 2.5 and 8 bytes a sum and part at 4 TB/s: 40 rows by 8192 columns in one part 26, in four 15.
 Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
+    const bool wide = dtype == BIFEAT_F32;
     const int64_t rows16 = (s->out_features + 15) / 16, blocks = (s->in_features + 127) / 128;
-    const char *ev = getenv("BFP");
-    int e[4] = {-1, 0, 0, 0};
-    if (ev) sscanf(ev, "%d,%d,%d,%d", e, e + 1, e + 2, e + 3);
-    Plan p{};
-    p.many = rows > 64 && s->in_features >= 8;
-    p.tb = rows <= 16 ? 1 : rows <= 32 || dtype == BIFEAT_F32 ? 2 : rows <= 48 ? 3 : 4;
-    p.r = p.tb > 1 ? (dtype == BIFEAT_F32 ? 2 : 4) : rows16 >= 1024 ? 4 : rows16 >= 512 ? 2 : 1;
-    p.split = 1;
-    if (e[0] >= 0) p.many = e[0], p.split = e[3];
-    if (e[0] >= 0 && e[2] && p.tb == 1) p.r = e[2];
-    (void)blocks;
-    return p;
+    Plan best{};
+    double least = 0.0;
+    const auto consider = [&](Plan p, int64_t workgroups, double begin, double block, int64_t at_once, int64_t least_blocks) {
+        for (p.split = 1; p.split <= 16 && (p.split == 1 || blocks / p.split >= least_blocks); p.split *= 2) {
+            const double rounds = std::max(1.0, at_once == 256 ? (double)((workgroups * p.split + 255) / 256) : 0.92 * (double)(workgroups * p.split) / 256);
+            const double us = begin + rounds * block * (double)((blocks + p.split - 1) / p.split) +
+                              (p.split > 1 ? 2.5 + 8e-6 / 4 * (double)p.split * (double)rows * s->out_features : 0.0);
+            if (best.split == 0 || us < least) best = p, least = us;
+        }
+    };
+    const int tb = rows <= 16 ? 1 : rows <= 32 || wide ? 2 : rows <= 48 ? 3 : 4;
+    const int r = tb > 1 ? (wide ? 2 : 4) : rows16 >= 512 ? 2 : 1;
+    const double few[2][5] = {{0, 0.12, 0.2, 0.37, 0.55}, {0, 0.3, 0.6, 0, 0}};
+    consider({false, tb, r, 1}, (rows16 + r - 1) / r * ((rows + 16 * tb - 1) / (16 * tb)), 2.5, few[wide][tb], 256, 8);
+    if (rows > 64 && s->in_features >= 8) consider({true, 0, 0, 1}, (rows16 + 7) / 8 * ((rows + 127) / 128), 8.0, wide ? 3.6 : 1.25, 512, 4);
+    return best;
 }
 
 bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
@@ -67,7 +76,9 @@ struct Room {
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
     const int64_t pairs = r->tokens * r->choices;
-    o.tile = pairs >= 32 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
+    // tiles of 128 rows from 22 pairs an expert on: 64 matrices of 1536 x 2048 with 16 each 57 us in tiles of 16, 68 in tiles of 128; with 24 75 and 72, with
+    // 64 161 and 86
+    o.tile = pairs >= 22 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
     o.counts = o.order + (pairs + 3) / 4 * 16;

@@ -118,6 +118,13 @@ __global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices
 #pragma unroll
                     for (int i = 0; i < 4; i++) total[r][t][i] = fmaf(scale, sum[r][t][i], fmaf(rest, of_x[t][i], total[r][t][i]));
             }
+            if constexpr (TB * R >= 12) {  // (here and not where they are used next: the compiler would keep what they are made of until then)
+#pragma unroll
+                for (int r = 0; r < R; r++)
+#pragma unroll
+                    for (int t = 0; t < TB; t++) asm volatile("" : "+v"(total[r][t]));
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
     };
     const auto whole = [](const T *row, int at) { return load_columns(row + at); };
@@ -180,8 +187,7 @@ void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int64_t 
     };
 #define BF_GO(GPB)                                                                                                                     \
     if (DEALT || shape.tb == 1) {                                                                                                      \
-        if (shape.r == 4) launch(linear_few_kernel<T, GPB, 1, 4, DEALT, Out>, 1, 4);                                                   \
-        else if (shape.r == 2) launch(linear_few_kernel<T, GPB, 1, 2, DEALT, Out>, 1, 2);                                              \
+        if (shape.r == 2) launch(linear_few_kernel<T, GPB, 1, 2, DEALT, Out>, 1, 2);                                              \
         else launch(linear_few_kernel<T, GPB, 1, 1, DEALT, Out>, 1, 1);                                                                \
     } else if constexpr (!DEALT) {                                                                                                     \
         if (shape.tb == 2) launch(linear_few_kernel<T, GPB, 2, few_most_rows<T>, DEALT, Out>, 2, few_most_rows<T>);                    \
