@@ -135,10 +135,10 @@ struct XRows {
     int sum_groups;  // a multiple of 16
 };
 
-// Where rows are dealt to experts, the pairs of a token and one of its choices lie in `order` expert by expert, and a tile is up to
-// kTile of one expert's.
+// Where rows are dealt to experts, a tile is up to 16 or kManyRows pairs of a token and one of its choices that name one expert; it has as many places in `order`,
+// of which the first `count` are filled.
 struct Tile {
-    int expert, first, count, unused;  // expert -1: pairs that name none
+    int expert, count;  // expert -1: pairs that name none
 };
 struct Deal {
     const int *tiles_count;

@@ -80,8 +80,9 @@ Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     // 64 161 and 86
     o.tile = pairs >= 22 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
-    o.order = 16 + o.most_tiles * (int64_t)sizeof(bf::Tile);
-    o.counts = o.order + (pairs + 3) / 4 * 16;
+    o.order = 16 + (o.most_tiles + 1) / 2 * 16;  // (a tile is 8 bytes)
+    static_assert(sizeof(bf::Tile) == 8, "");
+    o.counts = o.order + o.most_tiles * o.tile * 4;
     const int parts = bf::deal_parts(pairs);
     o.sums = o.counts + (parts > 1 ? ((int64_t)parts * (s->experts + 1) + 3) / 4 * 16 : 0);
     o.sum_rows = o.tile == 16 ? 0 : r->choice_stride ? pairs : r->tokens;

@@ -35,13 +35,14 @@ __global__ __launch_bounds__(kDealThreads) void linear_count_kernel(const int *i
     for (int e = threadIdx.x; e <= experts; e += kDealThreads) counts[blockIdx.x * (experts + 1) + e] = count[e];
 }
 
-// Pairs of a token and a choice, expert by expert, and tiles of up to `tile` of one expert's.  The order of an expert's pairs is not fixed; their products do
+// Pairs of a token and a choice, expert by expert, in tiles of up to `tile` of one expert's, a power of two; a tile has that many places in `order`, so that its
+// pairs are found without knowing it.  The order of an expert's pairs is not fixed; their products do
 // not depend on it.  Those that name no expert come last, as an expert of their own.  A workgroup places a part of the pairs; one part is counted
 // here, of several `counts` has the numbers.  32 768 pairs of 128 experts in one part 30 us, in 16 3 + 4.
 __global__ __launch_bounds__(kDealThreads) void linear_deal_kernel(const int *ids, int pairs, int per_part, int experts, int tile, const int *counts,
                                                                    int *tiles_count, Tile *tiles, int *order) {
-    __shared__ int count[kMostExperts + 1], first[kMostExperts + 1], tile_at[kMostExperts + 1];
-    __shared__ int sums[2][kDealThreads / 64];
+    __shared__ int count[kMostExperts + 1], first[kMostExperts + 1], tile_at[kMostExperts + 1];  // first: of this part's, among the expert's
+    __shared__ int sums[kDealThreads / 64];
     const int begin = blockIdx.x * per_part, end = pairs - begin < per_part ? pairs : begin + per_part;
     if (counts) {
         for (int e = threadIdx.x; e <= experts; e += kDealThreads) {
@@ -60,37 +61,29 @@ __global__ __launch_bounds__(kDealThreads) void linear_deal_kernel(const int *id
         each_pair(ids, begin, end, experts, [&](int, int e) { atomicAdd(&count[e], 1); });
     }
     __syncthreads();
-    // sums of the pairs and tiles before each expert: a thread an expert, the last with those of none besides
-    int c = (int)threadIdx.x < experts ? count[threadIdx.x] : 0, before = c, t = (c + tile - 1) / tile, tiles_before = t;
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    // the tiles before each expert's: a thread an expert, the last those of none besides
+    const int c = (int)threadIdx.x < experts ? count[threadIdx.x] : 0, t = (c + tile - 1) / tile, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    int before = t;
 #pragma unroll
     for (int by = 1; by < 64; by *= 2) {
-        const int a = __shfl_up(before, by), b = __shfl_up(tiles_before, by);
-        if (lane >= by) before += a, tiles_before += b;
+        const int a = __shfl_up(before, by);
+        if (lane >= by) before += a;
     }
-    if (lane == 63) sums[0][wave] = before, sums[1][wave] = tiles_before;
+    if (lane == 63) sums[wave] = before;
     __syncthreads();
-    for (int w = 0; w < wave; w++) before += sums[0][w], tiles_before += sums[1][w];
-    int of_all = 0;  // where the thread's expert begins
-    if ((int)threadIdx.x < experts) {
-        of_all = before - c;
-        first[threadIdx.x] += of_all;
-        tile_at[threadIdx.x] = tiles_before - t;
-    }
-    if (threadIdx.x == kDealThreads - 1) {  // (experts beyond the last have none, so this thread's sums are all of them)
-        first[experts] += before;
-        tile_at[experts] = tiles_before;
-        if (blockIdx.x == 0) *tiles_count = tiles_before + (count[experts] + tile - 1) / tile;
+    for (int w = 0; w < wave; w++) before += sums[w];
+    if ((int)threadIdx.x < experts) tile_at[threadIdx.x] = before - t;
+    if (threadIdx.x == kDealThreads - 1) {  // (experts beyond the last have none, so this thread's sum is all of them)
+        tile_at[experts] = before;
+        if (blockIdx.x == 0) *tiles_count = before + (count[experts] + tile - 1) / tile;
     }
     if (blockIdx.x == 0) {
-        for (int at = 0, i = tiles_before - t; (int)threadIdx.x < experts && at < c; at += tile, i++)
-            tiles[i] = {(int)threadIdx.x, of_all + at, c - at < tile ? c - at : tile, 0};
+        for (int at = 0, i = before - t; (int)threadIdx.x < experts && at < c; at += tile, i++) tiles[i] = {(int)threadIdx.x, c - at < tile ? c - at : tile};
         if (threadIdx.x == kDealThreads - 1)
-            for (int at = 0, i = tiles_before; at < count[experts]; at += tile, i++)
-                tiles[i] = {-1, before + at, count[experts] - at < tile ? count[experts] - at : tile, 0};
+            for (int at = 0, i = before; at < count[experts]; at += tile, i++) tiles[i] = {-1, count[experts] - at < tile ? count[experts] - at : tile};
     }
     __syncthreads();
-    each_pair(ids, begin, end, experts, [&](int i, int e) { order[atomicAdd(&first[e], 1)] = i; });
+    each_pair(ids, begin, end, experts, [&](int i, int e) { order[tile_at[e] * tile + atomicAdd(&first[e], 1)] = i; });
 }
 
 // out[t] = sum over j, ascending, of weights[t][j] products[t][j].  Four columns a lane, the rows of eight choices on their way at a time.

@@ -18,13 +18,21 @@ __global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quarter = lane / 16;
     const int row0 = blockIdx.x * R;
     const int x_tile = tile0 + blockIdx.y;
-    int64_t first = (int64_t)x_tile * 16 * TB;
+    const int64_t first = (int64_t)x_tile * 16 * TB;
     int count;
     const uint8_t *packed = m.packed;
+    // the tile's rows: what a lane brings, and the four that it stores
+    const int mine[4] = {4 * quarter, 4 * quarter + 1, 4 * quarter + 2, 4 * quarter + 3};
+    int64_t from[TB], to[4];
     if constexpr (DEALT) {
-        if (x_tile >= *deal.tiles_count) return;
+        // (all of it asked for at a time; places that are not filled are the first one's)
+        const int tiles = *deal.tiles_count;
         const Tile t = deal.tiles[x_tile];
-        first = t.first;
+        const int head = deal.order[first];
+        int mine_to[4], mine_from = deal.order[first + col];
+#pragma unroll
+        for (int j = 0; j < 4; j++) mine_to[j] = deal.order[first + mine[j]];
+        if (x_tile >= tiles) return;
         count = t.count;
         if (t.expert < 0) {
             for (int i = threadIdx.x; i < count * 16 * R; i += 64 * kWaves) {
@@ -34,18 +42,18 @@ __global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices
             return;
         }
         packed += t.expert * m.bytes;
+        from[0] = col < count ? mine_from : head;
+#pragma unroll
+        for (int j = 0; j < 4; j++) to[j] = mine_to[j];
     } else {
         count = x.count - first < 16 * TB ? (int)(x.count - first) : 16 * TB;
+#pragma unroll
+        for (int t = 0; t < TB; t++) from[t] = first + (16 * t + col < count ? 16 * t + col : count - 1);  // (what a row past the last gives is not stored)
     }
-    const auto row_of = [&](int i) -> int64_t {
-        if constexpr (DEALT) return deal.order[first + i];
-        return first + i;
-    };
     const T *xr[TB];
 #pragma unroll
     for (int t = 0; t < TB; t++) {
-        const int64_t row = row_of(16 * t + col < count ? 16 * t + col : count - 1);  // (what a row past the last gives is not stored)
-        const int64_t token = DEALT ? (int64_t)((uint32_t)row / (uint32_t)x.choices) : row;
+        const int64_t row = from[t], token = DEALT ? (int64_t)((uint32_t)row / (uint32_t)x.choices) : row;
         xr[t] = static_cast<const T *>(x.x) + token * x.token_stride + (DEALT ? (row - token * x.choices) * x.choice_stride : 0);
     }
     // the part of the columns, in blocks
@@ -169,8 +177,8 @@ __global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices
         const int r = i / TB, t = i - r * TB, n = 16 * (row0 + r) + col;
 #pragma unroll
         for (int j = 0; j < 4; j++) {
-            const int at = 16 * t + 4 * quarter + j;
-            if (at < count && n < m.N) out[row_of(at) * m.N + n] = from_float<Out>(y[j]);
+            const int at = 16 * t + mine[j];
+            if (at < count && n < m.N) out[(DEALT ? to[j] : first + at) * m.N + n] = from_float<Out>(y[j]);
         }
     }
 }
