@@ -10,18 +10,25 @@ constexpr int kDealThreads = 1024, kMostExperts = 1024;
 
 __device__ inline int expert_of(int e, int experts) { return e >= 0 && e < experts ? e : experts; }
 
-// Each pair of a part of them, with its expert (those that name none: `experts`); loads ahead of their use.
+// A thread's pairs of a part of them, and their experts (those that name none: `experts`; past the end: -1), loads ahead of their use.
+constexpr int kPairsAhead = 4;
+struct Pairs {
+    int first, e[kPairsAhead];
+};
+__device__ inline Pairs pairs_of(const int *ids, int first, int last, int experts) {
+    Pairs p;
+    p.first = first;
+#pragma unroll
+    for (int j = 0; j < kPairsAhead; j++) p.e[j] = first + j * kDealThreads < last ? ids[first + j * kDealThreads] : 0;
+#pragma unroll
+    for (int j = 0; j < kPairsAhead; j++) p.e[j] = first + j * kDealThreads < last ? expert_of(p.e[j], experts) : -1;
+    return p;
+}
 template <typename F>
-__device__ inline void each_pair(const int *ids, int first, int last, int experts, F f) {
-    constexpr int kAhead = 8;
-    for (int i0 = first + threadIdx.x; i0 < last; i0 += kAhead * kDealThreads) {
-        int e[kAhead];
+__device__ inline void each_of(const Pairs &p, F f) {
 #pragma unroll
-        for (int j = 0; j < kAhead; j++) e[j] = i0 + j * kDealThreads < last ? ids[i0 + j * kDealThreads] : 0;
-#pragma unroll
-        for (int j = 0; j < kAhead; j++)
-            if (i0 + j * kDealThreads < last) f(i0 + j * kDealThreads, expert_of(e[j], experts));
-    }
+    for (int j = 0; j < kPairsAhead; j++)
+        if (p.e[j] >= 0) f(p.first + j * kDealThreads, p.e[j]);
 }
 
 // How many pairs of each part name each expert: counts[part][expert].
@@ -29,8 +36,9 @@ __global__ __launch_bounds__(kDealThreads) void linear_count_kernel(const int *i
     __shared__ int count[kMostExperts + 1];
     for (int e = threadIdx.x; e <= experts; e += kDealThreads) count[e] = 0;
     __syncthreads();
-    const int first = blockIdx.x * per_part;
-    each_pair(ids, first, pairs - first < per_part ? pairs : first + per_part, experts, [&](int, int e) { atomicAdd(&count[e], 1); });
+    const int first = blockIdx.x * per_part, last = pairs - first < per_part ? pairs : first + per_part;
+    for (int i = first + threadIdx.x; i < last; i += kPairsAhead * kDealThreads)
+        each_of(pairs_of(ids, i, last, experts), [&](int, int e) { atomicAdd(&count[e], 1); });
     __syncthreads();
     for (int e = threadIdx.x; e <= experts; e += kDealThreads) counts[blockIdx.x * (experts + 1) + e] = count[e];
 }
@@ -44,21 +52,22 @@ __global__ __launch_bounds__(kDealThreads) void linear_deal_kernel(const int *id
     __shared__ int count[kMostExperts + 1], first[kMostExperts + 1], tile_at[kMostExperts + 1];  // first: of this part's, among the expert's
     __shared__ int sums[kDealThreads / 64];
     const int begin = blockIdx.x * per_part, end = pairs - begin < per_part ? pairs : begin + per_part;
+    const Pairs mine = pairs_of(ids, begin + threadIdx.x, end, experts);  // (of a part of up to 4096 all)
     if (counts) {
         for (int e = threadIdx.x; e <= experts; e += kDealThreads) {
-            int all = 0, mine = 0;  // ... and what the parts before this one have
+            int all = 0, earlier = 0;  // ... and what the parts before this one have
             for (int p = 0; p < (int)gridDim.x; p++) {
                 const int c = counts[p * (experts + 1) + e];
                 all += c;
-                mine += p < (int)blockIdx.x ? c : 0;
+                earlier += p < (int)blockIdx.x ? c : 0;
             }
             count[e] = all;
-            first[e] = mine;
+            first[e] = earlier;
         }
     } else {
         for (int e = threadIdx.x; e <= experts; e += kDealThreads) count[e] = first[e] = 0;
         __syncthreads();
-        each_pair(ids, begin, end, experts, [&](int, int e) { atomicAdd(&count[e], 1); });
+        each_of(mine, [&](int, int e) { atomicAdd(&count[e], 1); });  // (one part is not longer)
     }
     __syncthreads();
     // the tiles before each expert's: a thread an expert, the last those of none besides
@@ -83,7 +92,9 @@ __global__ __launch_bounds__(kDealThreads) void linear_deal_kernel(const int *id
             for (int at = 0, i = before; at < count[experts]; at += tile, i++) tiles[i] = {-1, count[experts] - at < tile ? count[experts] - at : tile};
     }
     __syncthreads();
-    each_pair(ids, begin, end, experts, [&](int i, int e) { order[tile_at[e] * tile + atomicAdd(&first[e], 1)] = i; });
+    const auto place = [&](int i, int e) { order[tile_at[e] * tile + atomicAdd(&first[e], 1)] = i; };
+    each_of(mine, place);
+    for (int i = begin + threadIdx.x + kPairsAhead * kDealThreads; i < end; i += kPairsAhead * kDealThreads) each_of(pairs_of(ids, i, end, experts), place);
 }
 
 // out[t] = sum over j, ascending, of weights[t][j] products[t][j].  Four columns a lane, the rows of eight choices on their way at a time.

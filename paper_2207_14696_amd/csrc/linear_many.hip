@@ -112,14 +112,18 @@ constexpr int kRows = kManyRows;
 template <typename T> constexpr int kStep = sizeof(T) == 4 ? 32 : 64;
 
 template <typename T, int GPB, bool DEALT, typename Out>
-__global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x, Deal deal, Out *out, int row_tiles, int tile0) {
+__global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x, Deal deal, Out *out, int row_tiles, int tile0, int tiles_end) {
     typedef Operand<T> O;
     typedef typename O::Eight Operands;
     constexpr int P = O::kPieces, S = kStep<T>, kChunks = S / 8, kLoads = kRows * kChunks / 256;
     constexpr int kStride = kRows + 1;  // (of a chunk in 16 bytes: the lanes that write a row's chunks meet no two in a bank)
     __shared__ uint4 tile[2][P][kChunks * kStride];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 32, half = lane / 32;
-    const int n_tile = blockIdx.x % row_tiles, x_tile = tile0 + blockIdx.x / row_tiles;
+    // Workgroups go to the eight XCDs in turn.  tiles_end > 0: each XCD takes whole tiles of x, whose products with all rows of the matrix find them in its L2
+    const int die = blockIdx.x % 8, of_die = blockIdx.x / 8;
+    const int n_tile = tiles_end ? of_die % row_tiles : blockIdx.x % row_tiles;
+    const int x_tile = tile0 + (tiles_end ? of_die / row_tiles * 8 + die : blockIdx.x / row_tiles);
+    if (tiles_end && x_tile >= tiles_end) return;
     const int64_t first = (int64_t)x_tile * kRows;
     int count;
     const uint8_t *packed = m.packed;
@@ -350,12 +354,15 @@ void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int tile
     const int row_tiles = (m.N + kRows - 1) / kRows;
     const int64_t all = DEALT ? (int64_t)tiles : (x.count + kRows - 1) / kRows;
     // (a launch has fewer than 2^32 threads)
-    const int64_t most = std::max<int64_t>(1, (1 << 22) / (row_tiles * split));
+    const int64_t most = std::max<int64_t>(8, (1 << 22) / (row_tiles * split) / 8 * 8);
     for (int64_t at = 0; at < all; at += most) {
-        const dim3 grid((unsigned)(row_tiles * std::min(most, all - at)), split);
-        if (group == 128) linear_many_kernel<T, 1, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at);
-        else if (group == 64) linear_many_kernel<T, 2, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at);
-        else linear_many_kernel<T, 4, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at);
+        const int64_t here = std::min(most, all - at);
+        const bool whole = here % 8 == 0 || here >= 64;
+        const dim3 grid((unsigned)(row_tiles * (whole ? (here + 7) / 8 * 8 : here)), split);
+        const int end = whole ? (int)(at + here) : 0;
+        if (group == 128) linear_many_kernel<T, 1, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at, end);
+        else if (group == 64) linear_many_kernel<T, 2, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at, end);
+        else linear_many_kernel<T, 4, DEALT, Out><<<grid, 256, 0, s>>>(m, x, deal, (Out *)x.out, row_tiles, (int)at, end);
     }
 }
 
