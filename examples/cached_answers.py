@@ -52,22 +52,26 @@ class Sequences:
         self.lengths, self.held = [0] * count, [0] * count
         self.tables = torch.zeros(count, -(-most // PAGE), dtype=torch.int32, device=device)
 
-    def step(self, model, tokens):
-        """tokens: one list a sequence (empty ones among them).  The logits of all of them, one after another."""
+    def grow(self, tokens):
+        """Room for one list of new tokens a sequence; lengths, offsets and the tokens on the device."""
         for b, new in enumerate(tokens):
             self.lengths[b] += len(new)
             while self.held[b] * PAGE < self.lengths[b]:
                 self.tables[b, self.held[b]] = self.free.pop()
                 self.held[b] += 1
         device = self.tables.device
-        lengths = torch.tensor(self.lengths, device=device)
-        indptr = torch.tensor([0] + [len(t) for t in tokens], device=device).cumsum(0)
+        return (torch.tensor(self.lengths, device=device), torch.tensor([0] + [len(t) for t in tokens], device=device).cumsum(0),
+                torch.tensor([t for new in tokens for t in new], device=device))
+
+    def step(self, model, tokens):
+        """tokens: one list a sequence (empty ones among them).  The logits of all of them, one after another."""
+        lengths, indptr, ids = self.grow(tokens)
 
         def attend(layer, q, k, v):
             self.cache.write(self.pages[layer], k, v, self.tables, lengths, indptr)
             return self.cache.attend(self.pages[layer], q, self.tables, lengths, indptr, window=window_of(layer))
 
-        return model.forward(torch.tensor([t for new in tokens for t in new], device=device), attend)
+        return model.forward(ids, attend)
 
 
 def whole(model, ids):

@@ -530,7 +530,7 @@ int bifeat_cache_attend(bifeat_cache *c, const uint8_t *pages, int64_t num_pages
  *   minimum = NaN: its row of the matrix gives NaN, and no other.
  * multiply: out[t][n] = sum_k x[t][k] weight[n][k], for rows x of any number.  16-bit x enter
  *   the matrix cores as they are, codes with them as 16 + code; 32-bit x in three pieces that are
- *   them together, codes as they are: all exact.  Sums are fp32, then rounded to x's type.  A row of
+ *   them together (but for what of them lies below 2^-133), codes as they are: all exact.  Sums are fp32, then rounded to x's type.  A row of
  *   x with an infinity or a NaN gives infinities and NaN, as may one with a group whose sum of
  *   |x|, or that times 16 scales or the minimum, passes 2^122; other rows are as they were without it.
  * experts: `experts` matrices of one size, and tokens with `choices` of them each.  out[t][j] =
@@ -563,7 +563,7 @@ typedef struct {
     int64_t token_stride, choice_stride; /* elements, >= 0; choice_stride 0: a token's choices share its row */
     const int32_t *ids;     /* DEVICE [tokens][choices] */
     const float *weights;   /* DEVICE [tokens][choices], or NULL: no sum */
-    int64_t tokens;
+    int64_t tokens;         /* tokens * choices at most 2^30 */
     int32_t choices;        /* 1..64 */
 } bifeat_expert_rows;
 

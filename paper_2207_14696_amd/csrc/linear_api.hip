@@ -64,7 +64,7 @@ Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
 
 bool rows_ok(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     return r && r->tokens >= 0 && r->choices >= 1 && r->choices <= 64 && r->token_stride >= 0 && r->choice_stride >= 0 &&
-           r->tokens <= (INT32_MAX - 64) / r->choices;
+           r->tokens <= (1 << 30) / r->choices;
 }
 
 // The memory of bifeat_linear_experts: the number of tiles, the tiles, the pairs in order, the parts' counts, the sums of x, 32-bit products.

@@ -198,6 +198,55 @@ def test_sizes_of_x_do_not_matter(bf, torch, dtype):
             _assert_close(_host(layer.multiply(packed, x)), want, _bound(500, h, size, want, dtype), str(scale))
 
 
+@pytest.mark.parametrize("dtype,size", [("f16", 3e-6), ("f16", 3e-7), ("bf16", 1e-38), ("f32", 1e-37)])
+@pytest.mark.parametrize("T", [3, 40, 2000])
+def test_subnormal_rows(bf, torch, dtype, size, T):
+    """Numbers below the type's smallest normal one are products' operands like others."""
+    rng = np.random.default_rng(8)
+    N = 2000 if T == 2000 else 64
+    layer, packed, value, size_of = _layer(bf, torch, rng, N, 500, 128)
+    x = torch.from_numpy((size * rng.standard_normal((T, 500))).astype(np.float32)).cuda().to(_dtype(torch, dtype))
+    h = _host(x).astype(np.float64)
+    want = h @ value.T
+    # fp32 sums have their own smallest steps too, 2^-150 to nearest, an addition; of a 32-bit number three bfloat16 are it but for what lies below
+    # 2^-133, their smallest step, and so of a group's sum: twice that for each column, times the largest that a code stands for
+    lost = 2.0 ** -132 * size_of.sum(1) if dtype == "f32" else 0.0
+    _assert_close(_host(layer.multiply(packed, x)), want, _bound(500, h, size_of, want, dtype) + 700 * 2.0 ** -149 + lost)
+
+
+# sizes at which tiles of many rows are taken, with the columns in one part and in four; few whole blocks of columns, and none
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("group,T,K,N,stride", [(128, 1100, 1001, 3001, 1001), (64, 1300, 1152, 2500, 1160), (32, 1200, 1030, 3100, 1033), (128, 600, 8192, 2048, 8192),
+                                                (32, 650, 8200, 2001, 8200), (64, 20000, 40, 3000, 47), (128, 20000, 9, 3003, 9), (128, 4096, 2304, 1000, 2304)])
+def test_many_rows(bf, torch, dtype, group, T, K, N, stride):
+    g = torch.Generator(device="cuda").manual_seed(T + K)
+    layer = bf.PackedLinear(N, K, group=group)
+    packed = layer.pack(torch.randn(N, K, device="cuda", generator=g) + 0.3 * torch.randn(N, 1, device="cuda", generator=g))
+    wide = torch.full((T * stride + 3,), float("nan"), dtype=_dtype(torch, dtype), device="cuda")
+    x = torch.as_strided(wide, (T, K), (stride, 1), 3)
+    x.copy_(torch.randn(T, K, device="cuda", generator=g) + 0.5)
+    room = torch.full((T + 2, N), 7.0, dtype=x.dtype, device="cuda")
+    y = layer.multiply(packed, x, out=room[1:T + 1])
+    value = layer.unpack(packed).double()
+    want = x.double() @ value.T
+    # as _bound; the largest that a code stands for in a group's sums: 31 scales and the minimum, 6 times the largest weight at most (a range of 15
+    # scales has a weight of 7.5 of them at least: 31 scales are 4.2 of it, and the minimum is at most one)
+    chain = 32 + 12 + 3 * (-(-K // 128)) + 8 + 16
+    top = value.abs().view(N, K).nan_to_num()
+    per = torch.stack([top[:, i:i + group].amax(1) for i in range(0, K, group)], 1).repeat_interleave(group, 1)[:, :K]
+    off = chain * 2.0 ** -23 * (x.double().abs() @ (6 * per).T)
+    assert ((y.double() - want).abs() <= off + (want.abs() + off) * HALF_ULP[dtype] + LEAST[dtype]).all()
+    assert (room[0] == 7).all() and (room[T + 1] == 7).all() and torch.equal(layer.multiply(packed, x), y)
+    # rows do not reach each other
+    clean = y.clone()
+    bad = [0, 130, T - 1]
+    x[bad, [0, K // 2, K - 1]] = torch.tensor([float("nan"), float("inf"), -float("inf")], device="cuda").to(x.dtype)
+    got = layer.multiply(packed, x)
+    good = torch.ones(T, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    assert torch.equal(got[good], clean[good]) and not torch.isfinite(got[bad]).any()
+
+
 def test_32_bit_rows_keep_32_bits(bf, torch):
     """A weight of one code and x of full mantissas: the three pieces are all of x."""
     K, N = 64, 16
@@ -390,3 +439,16 @@ def test_captured_calls(bf, torch, T):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)), i
+
+
+def test_the_example():
+    """It runs, whole prompts and tokens one by one; of its numbers only that they are some."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "packed_answers.py")
+    spec = importlib.util.spec_from_file_location("packed_answers", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for bits in (4, 8):
+        off = example.answer(bits, prompts=(70, 33, 5), tokens=6, chunk=32)
+        assert len(off) == 3 and np.isfinite(off).all()

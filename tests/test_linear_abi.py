@@ -201,3 +201,13 @@ def test_reference_turn_keeps_lengths_and_differences():
         # products depend on the distance alone
         a, b = ref.turn(x[:2], [3, 9], f, interleaved), ref.turn(x[:2], [103, 109], f, interleaved)
         assert np.allclose((a[0] * a[1]).sum(-1), (b[0] * b[1]).sum(-1))
+
+
+def test_the_product_kernels_spill_no_vector_registers(bf):
+    import os
+    from test_cache_abi import READELF, _kernels_of
+    if not os.path.exists(READELF):
+        pytest.skip("no llvm-readelf")
+    kernels = [(n, s) for n, s in _kernels_of(bf.library_path()) if "linear_" in n or "route_" in n or "cache_append" in n]
+    assert len(kernels) >= 100, len(kernels)
+    assert not [k for k in kernels if k[1]]
