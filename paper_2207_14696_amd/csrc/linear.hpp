@@ -150,9 +150,8 @@ hipError_t launch_linear_pack(const Matrices &m, int group, const void *weight, 
 hipError_t launch_linear_unpack(const Matrices &m, int group, float *weight, hipStream_t s);
 // How few rows are taken: 16 tb of them and 16 r of the matrix a workgroup, columns in `split` parts (without a deal).
 struct FewShape {
-    int tb, r, split;
+    int tb, r, split, waves;
 };
-__host__ __device__ constexpr int few_waves(int) { return 8; }
 template <typename T> constexpr int few_most_rows = sizeof(T) == 4 ? 2 : 4;  // r of tb >= 2
 // deal null: one matrix, rows as they are.  to_float: out is fp32 whatever the rows' type; of several parts one after another.
 hipError_t launch_linear_few(const Matrices &m, int group, const XRows &x, const Deal *deal, int most_tiles, int dtype, bool to_float, const FewShape &shape,

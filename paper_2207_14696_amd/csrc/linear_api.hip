@@ -55,7 +55,8 @@ Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
         }
     };
     const int tb = rows <= 16 ? 1 : rows <= 32 || wide ? 2 : rows <= 48 ? 3 : 4;
-    const int r = tb > 1 ? (wide ? 2 : 4) : rows16 >= 512 ? 2 : 1;
+    // (one row by 8192 x 28 672: 31.5 us with r = 2, 29.2 with 4; by 4096 x 4096 4.9 with 1, 5.7 with 2, 7.7 with 4)
+    const int r = tb > 1 ? (wide ? 2 : 4) : rows16 >= 1536 ? 4 : rows16 >= 512 ? 2 : 1;
     const double few[2][5] = {{0, 0.12, 0.2, 0.37, 0.55}, {0, 0.3, 0.6, 0, 0}};
     consider({false, tb, r, 1}, (rows16 + r - 1) / r * ((rows + 16 * tb - 1) / (16 * tb)), 2.5, few[wide][tb], 256, 8);
     if (rows > 64 && s->in_features >= 8) consider({true, 0, 0, 1}, (rows16 + 7) / 8 * ((rows + 127) / 128), 8.0, wide ? 3.6 : 1.25, 512, 4);
@@ -129,7 +130,7 @@ int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed
         r.sums = reinterpret_cast<const uint16_t *>(static_cast<uint8_t *>(workspace) + plan.parts_bytes(spec, rows));
         BF_HIP(bf::launch_linear_sums(m, spec->group, r, dtype, s));
         BF_HIP(bf::launch_linear_many(m, spec->group, r, nullptr, 0, dtype, split, plan.split, s));
-    } else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split}, s));
+    } else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split, 8}, s));
     if (split) BF_HIP(bf::launch_linear_add(static_cast<const float *>(workspace), plan.split, rows * m.N, dtype, out, s));
     return BIFEAT_OK;
 }
@@ -159,7 +160,10 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out,
                       reinterpret_cast<const uint16_t *>(w + room.sums), room.sum_rows, sum_groups(spec)};
     const bool to_float = r->weights != nullptr;
-    if (room.tile == 16) BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, {1, 2, 1}, s));
+    // many workgroups have four waves each: a wave then has more blocks to go through, and the beginnings and ends of the others beside it (32 tokens of 8
+    // of 128 experts of 1536 x 2048 54 us by eight waves and 32 rows, 45 by four, 43 by four and 64 rows; one token 8.7 and 9.4)
+    const int waves = room.most_tiles * m.rows >= 2048 ? 4 : 8;
+    if (room.tile == 16) BF_HIP(bf::launch_linear_few(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, {1, waves == 4 ? 4 : 2, 1, waves}, s));
     else {
         BF_HIP(bf::launch_linear_sums(m, spec->group, x, dtype, s));
         BF_HIP(bf::launch_linear_many(m, spec->group, x, &deal, (int)room.most_tiles, dtype, to_float, 1, s));

@@ -10,10 +10,10 @@ namespace {
 // in LDS at the end.  A lane's 16 bytes of a block are 32 codes of one row of the matrix, four operands as they are; x is the other operand, so that a lane's sums
 // are of one row of the matrix, and of one scale.  Of up to 16 rows the next block
 // is on its way while one is multiplied.
-template <typename T, int GPB, int TB, int R, bool DEALT, typename Out>
-__global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out, int tile0) {
+template <typename T, int GPB, int TB, int R, int kWaves, bool DEALT, typename Out>
+__global__ __launch_bounds__(64 * kWaves) void linear_few_kernel(Matrices m, XRows x, Deal deal, Out *out, int tile0) {
     typedef Operand<T> O;
-    constexpr int P = O::kPieces, kWaves = few_waves(TB);
+    constexpr int P = O::kPieces;
     __shared__ Sum4 part[kWaves][R * TB][64];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 16, quarter = lane / 16;
     const int row0 = blockIdx.x * R;
@@ -185,29 +185,34 @@ __global__ __launch_bounds__(64 * few_waves(TB)) void linear_few_kernel(Matrices
 
 template <typename T, typename Out, bool DEALT>
 void go(const Matrices &m, int group, const XRows &x, const Deal &deal, int64_t tiles, const FewShape &shape, hipStream_t s) {
-    const auto launch = [&](auto kernel, int tb, int r) {
+    const auto launch = [&](auto kernel, int tb, int r, int waves) {
         const int64_t y = DEALT ? tiles : (x.count + 16 * tb - 1) / (16 * tb);
         const int row_tiles = (m.rows + r - 1) / r;
         // (a launch has fewer than 2^32 threads, and a grid's second dimension than 2^16)
         const int64_t most = std::max<int64_t>(1, std::min<int64_t>(65535, (1 << 22) / (row_tiles * shape.split)));
         for (int64_t at = 0; at < y; at += most)
-            kernel<<<dim3(row_tiles, (unsigned)std::min(most, y - at), shape.split), 64 * few_waves(tb), 0, s>>>(m, x, deal, (Out *)x.out, (int)at);
+            kernel<<<dim3(row_tiles, (unsigned)std::min(most, y - at), shape.split), 64 * waves, 0, s>>>(m, x, deal, (Out *)x.out, (int)at);
     };
-#define BF_GO(GPB)                                                                                                                     \
-    if (DEALT || shape.tb == 1) {                                                                                                      \
-        if (shape.r == 2) launch(linear_few_kernel<T, GPB, 1, 2, DEALT, Out>, 1, 2);                                              \
-        else launch(linear_few_kernel<T, GPB, 1, 1, DEALT, Out>, 1, 1);                                                                \
-    } else if constexpr (!DEALT) {                                                                                                     \
-        if (shape.tb == 2) launch(linear_few_kernel<T, GPB, 2, few_most_rows<T>, DEALT, Out>, 2, few_most_rows<T>);                    \
-        else if constexpr (sizeof(T) == 2) {                                                                                           \
-            if (shape.tb == 3) launch(linear_few_kernel<T, GPB, 3, 4, DEALT, Out>, 3, 4);                                              \
-            else launch(linear_few_kernel<T, GPB, 4, 4, DEALT, Out>, 4, 4);                                                            \
-        }                                                                                                                              \
+#define BF_GO(GPB, TB, R, W) launch(linear_few_kernel<T, GPB, TB, R, W, DEALT, Out>, TB, R, W)
+#define BF_BY_SHAPE(GPB)                                                        \
+    if constexpr (DEALT) {                                                      \
+        if (shape.waves == 4) BF_GO(GPB, 1, 4, 4);                              \
+        else BF_GO(GPB, 1, 2, 8);                                               \
+    } else if (shape.tb == 1) {                                                 \
+        if (shape.r == 4) BF_GO(GPB, 1, 4, 8);                                  \
+        else if (shape.r == 2) BF_GO(GPB, 1, 2, 8);                             \
+        else BF_GO(GPB, 1, 1, 8);                                               \
+    } else if (shape.tb == 2) {                                                 \
+        BF_GO(GPB, 2, few_most_rows<T>, 8);                                     \
+    } else if constexpr (sizeof(T) == 2) {                                      \
+        if (shape.tb == 3) BF_GO(GPB, 3, 4, 8);                                 \
+        else BF_GO(GPB, 4, 4, 8);                                               \
     }
-    if (group == 128) { BF_GO(1) }
-    else if (group == 64) { BF_GO(2) }
-    else { BF_GO(4) }
+    if (group == 128) { BF_BY_SHAPE(1) }
+    else if (group == 64) { BF_BY_SHAPE(2) }
+    else { BF_BY_SHAPE(4) }
 #undef BF_GO
+#undef BF_BY_SHAPE
 }
 
 template <typename T>
