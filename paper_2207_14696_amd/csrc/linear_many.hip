@@ -215,6 +215,9 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
                     b[s16 % kDeep][j][p] = __builtin_bit_cast(Operands, tile[part & 1][p][(2 * s16 + half) * kStride + 32 * j + col]);
         };
         if (kDeep == 2) read(0);
+        // (a wave's products before the other wave's other work: two waves that keep in step would both wait for the matrix cores, then both for the vector ones;
+        // 8192 rows 291 us, 281 so)
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int s16 = 0; s16 < S / 16; s16++) {
             const int s = part * (S / 16) + s16;  // of the block's eight
@@ -240,6 +243,7 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
             if (s % kPer == kPer - 1) {
                 const int g = s / kPer;
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(0);
                 const float scale = __builtin_bit_cast(float, level_now[g] << 16);
 #pragma unroll
                 for (int j = 0; j < 4; j++)
@@ -249,8 +253,10 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
 #pragma unroll
                 for (int j = 0; j < 4; j++) asm volatile("" : "+v"(total[j]));
                 __builtin_amdgcn_sched_barrier(0);
+                __builtin_amdgcn_s_setprio(1);
             }
         }
+        __builtin_amdgcn_s_setprio(0);
     };
     const auto add_sums = [&] {
         int64_t at[4];
