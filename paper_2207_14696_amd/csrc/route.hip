@@ -287,7 +287,7 @@ __global__ __launch_bounds__(kThreads) void route_kernel(const T *logits, int64_
 //   softmax                  dx_i = c s_i ([i chosen] g_i - sum_j g_j s_j)
 //   sigmoid, renormalised    dx_i = c q_i (1 - s_i) (g_i - sum_j g_j q_j) for the chosen, else 0
 //   sigmoid                  dx_i = c s_i (1 - s_i) g_i for the chosen, else 0
-// Lane j has choice j; but for the second of these only the chosen scores are needed.
+// Lane j has choice j; but for the second of these only the chosen scores are needed, and of the first the largest logit.
 template <typename T, int EPL>
 __global__ __launch_bounds__(kThreads) void route_backward_kernel(const T *logits, int64_t stride, int64_t tokens, Options o, const int *ids, const float *grad,
                                                                   T *out) {
@@ -325,7 +325,11 @@ __global__ __launch_bounds__(kThreads) void route_backward_kernel(const T *logit
         if (o.sigmoid) {
             s = id >= 0 ? sigmoid(its) : 0.0;
         } else {
-            const uint32_t most = wave_most(id >= 0 ? key_of(its) : 0u);
+            // (beside the largest logit of all, not of the chosen: scores that are 0 have weights of 0, and no gradient)
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < EPL; i++) most = key_of(x[i]) > most ? key_of(x[i]) : most;
+            most = wave_most(most);
             s = id >= 0 && most ? exp((double)its - (double)of_key(most)) : 0.0;
         }
         double q = s;

@@ -147,6 +147,18 @@ def test_spoilt_tokens(bf, torch, dtype):
             assert int(ids[4, 0]) == 69 and (ids[6] == -1).all()
 
 
+def test_chosen_scores_of_zero_have_no_gradient(bf, torch):
+    """A bias, or groups by their two best, can choose experts whose softmax is 0 in 64 bits: weights of 0, which no logit moves."""
+    x = torch.tensor([[0.0, -2000.0, -2001.0, -2000.0], [-2000.0, 0.0, -2000.0, -2000.5], [0.0, 1.0, 2.0, 1.5]], device="cuda")
+    bias = np.array([0.0, 10.0, 10.0, 10.0], np.float32)
+    _, w = _check(bf, torch, x, 2, "f32", bias)
+    assert (w[0] == 0).all() and w[1, 0] == 1
+    x = torch.tensor([[0.0, -np.inf, -np.inf, -np.inf, -800.0, -800.5, -801.0, -900.0]], device="cuda")
+    bias = np.array([0, 0, 0, 0, 2, 2, 2, 2], np.float32)
+    _, w = _check(bf, torch, x, 3, "f32", bias, groups=2, top_groups=1, group_score="two")
+    assert (w == 0).all()
+
+
 def test_scores_that_differ_in_their_last_digits(bf, torch):
     """Ranks of scores and biases that 32 bits would not tell apart."""
     E, T = 64, 50
