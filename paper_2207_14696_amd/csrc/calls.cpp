@@ -507,6 +507,13 @@ struct RouteWithGradient : torch::autograd::Function<RouteWithGradient> {
     }
 };
 
+// (what 32 bits do not hold leaves an error set)
+int32_t int32_of(PyObject *o) {
+    const long x = PyLong_AsLong(o);
+    if (x < INT32_MIN || x > INT32_MAX) PyErr_SetNone(PyExc_OverflowError);
+    return (int32_t)x;
+}
+
 // route(address of the entry point, and of its backward pass, logits, choices, sigmoid, bias or None, groups, top_groups, group_two, renormalise,
 // scale): (ids, weights), an error status, or None
 PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
@@ -522,8 +529,8 @@ PyObject *route(PyObject *, PyObject *const *a, Py_ssize_t n) {
         }
         const bool biased = a[5] != Py_None;
         auto &o = r.options;
-        o = {(int32_t)x->size(-1), (int32_t)PyLong_AsLong(a[3]), (int32_t)PyLong_AsLong(a[4]), (int32_t)PyLong_AsLong(a[6]),
-             (int32_t)PyLong_AsLong(a[7]), (int32_t)PyLong_AsLong(a[8]), (int32_t)PyLong_AsLong(a[9]), PyFloat_AsDouble(a[10]), nullptr};
+        o = {(int32_t)x->size(-1), int32_of(a[3]), (int32_t)PyLong_AsLong(a[4]), int32_of(a[6]), int32_of(a[7]),
+             (int32_t)PyLong_AsLong(a[8]), (int32_t)PyLong_AsLong(a[9]), PyFloat_AsDouble(a[10]), nullptr};
         if (PyErr_Occurred() || o.experts < 1 || o.choices < 1 ||
             (biased && (!(bias = tensor(a[5], at::kFloat, at::kFloat, x)) || bias->dim() != 1 || bias->size(0) != o.experts)) || watched() ||
             !stream(&r.stream, x)) {

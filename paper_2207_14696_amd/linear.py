@@ -21,7 +21,8 @@ class PackedLinear:
         self._lib = load_library()
         self._spec = _b._CLinearSpec(out_features, in_features, group, 1 if experts is None else experts)
         self.bytes = int(self._lib.bifeat_linear_bytes(C.byref(self._spec)))
-        if self.bytes < 0:
+        if self.bytes < 0 or (self._spec.out_features, self._spec.in_features, self._spec.group) != (out_features, in_features, group) or \
+                self._spec.experts != (1 if experts is None else experts):  # (sizes that 32 bits do not hold)
             _check(EINVAL)
         self.out_features, self.in_features, self.group = int(out_features), int(in_features), int(group)
         self.experts = None if experts is None else int(experts)

@@ -6,7 +6,7 @@ import ctypes as C
 import functools
 
 from . import binding as _b
-from .binding import _check, _dev_ptr, _dtype_code, _on_current_device, _stream, load_library
+from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _on_current_device, _stream, load_library
 
 
 _SCORES, _GROUP_SCORES = {"softmax": 0, "sigmoid": 1}, {"best": 0, "two": 1}
@@ -88,6 +88,8 @@ def route(logits, choices: int, score: str = "softmax", bias=None, groups: int =
         _on_current_device(logits, bias)
     options = _b._CRouteOptions(experts, choices, _SCORES[score], groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale,
                                 _dev_ptr(bias, (torch.float32,)))
+    if (options.choices, options.groups, options.top_groups) != (choices, groups, top_groups):   # (numbers that 32 bits do not hold)
+        _check(EINVAL)
     options.kept = bias     # (as long as a backward pass may need the options)
     if logits.requires_grad and torch.is_grad_enabled():
         return _function().apply(logits, options)
