@@ -5,6 +5,7 @@ it is built; what it leaves goes through ctypes, behind the checks here."""
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import math
 
 from . import binding as _b
@@ -117,8 +118,8 @@ class PagedCache:
         """``write`` of keys that are turned to their positions on the way; returns the queries, q [tokens, query heads, head_dim], turned
         with them (None for q None).  ``frequencies`` float32 [pairs], pairs <= head_dim / 2: radians a position of the column pairs
         (i, i + pairs), or (2 i, 2 i + 1) where ``interleaved``; columns from 2 * pairs on stay as they are.  ``scale``: of the turned
-        columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q requires one,
-        going back through the output raises."""
+        columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q or frequencies
+        require one, going back through the output raises."""
         if calls := _b._calls or _b._load_calls():
             r = calls.cache_append(*self._append, pages, q, k, v, frequencies, bool(interleaved), scale, tables, lengths, indptr)
             if r is not None:
@@ -126,9 +127,9 @@ class PagedCache:
                     _check(r)
                 return None if r is True else r
         import torch
-        if q is not None and q.requires_grad and torch.is_grad_enabled():
-            return _without_backward().apply("PagedCache.append has no backward pass",
-                                             lambda: self.append(pages, q.detach(), k, v, frequencies, tables, lengths, indptr, interleaved, scale), q)
+        if q is not None and (q.requires_grad or frequencies.requires_grad) and torch.is_grad_enabled():
+            call = functools.partial(self.append, pages, q.detach(), k, v, frequencies.detach(), tables, lengths, indptr, interleaved, scale)
+            return _without_backward().apply("PagedCache.append has no backward pass", call, q, frequencies)
         rows = [_head_rows(t, self.heads, self.head_dim, name) for t, name in ((k, "k"), (v, "v"))]
         if k.shape != v.shape or k.dtype != v.dtype:
             raise ValueError("k and v must be alike")

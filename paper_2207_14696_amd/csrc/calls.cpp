@@ -244,9 +244,9 @@ PyObject *cache_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const double scale = PyFloat_AsDouble(a[11]);
         if (PyErr_Occurred() || !cache_of(a, &c) || !(tk = head_rows(a[7], c, &k, &dtype)) || !(tv = head_rows(a[8], c, &v, &other)) || dtype != other ||
             tk->size(1) != c.heads || tv->size(1) != c.heads || tk->size(0) != tv->size(0) ||
-            (queries && (!(tq = head_rows(a[6], c, &q, &third)) || third != dtype || tq->size(0) != tk->size(0) || tq->size(1) > INT32_MAX ||
-                         (tq->requires_grad() && c10::GradMode::is_enabled()))) ||
-            !(f = tensor(a[9], at::kFloat, at::kFloat, c.pages)) || f->dim() != 1 || f->size(0) > INT32_MAX || !batch_of(a + 12, c, tk->size(0), &b) ||
+            (queries && (!(tq = head_rows(a[6], c, &q, &third)) || third != dtype || tq->size(0) != tk->size(0) || tq->size(1) > INT32_MAX)) ||
+            !(f = tensor(a[9], at::kFloat, at::kFloat, c.pages)) || f->dim() != 1 ||
+            (queries && (tq->requires_grad() || f->requires_grad()) && c10::GradMode::is_enabled()) || f->size(0) > INT32_MAX || !batch_of(a + 12, c, tk->size(0), &b) ||
             !stream(&s, c.pages)) {
             PyErr_Clear();
             Py_RETURN_NONE;

@@ -137,6 +137,20 @@ def test_going_back_raises_and_refusals(bf, torch):  # noqa: F811
     assert c.append(pages, q, k, v, f, *rest) is not None
 
 
+def test_going_back_to_frequencies_raises(bf, torch):  # noqa: F811
+    batch = Batch(torch, [6], [6], 16)
+    c = bf.PagedCache(8, 2, 16, 16)
+    pages = c.new_pages(batch.count)
+    q, k, v = (torch.randn(6, 2, 16, device="cuda") for _ in range(3))
+    f = _frequencies(torch, 8)
+    rest = (batch.d_tables, batch.d_lengths)
+    y = c.append(pages, q, k, v, f.clone().requires_grad_(True), *rest)
+    assert y.requires_grad and torch.equal(y, c.append(pages, q, k, v, f, *rest))
+    with pytest.raises(NotImplementedError):
+        y.sum().backward()
+    assert c.append(pages, None, k, v, f.clone().requires_grad_(True), *rest) is None
+
+
 def test_a_step_of_a_model_captured(bf, torch):  # noqa: F811
     """Product, turned keys, attention, product, routing, the experts' two products: together, and replayed."""
     heads, cached, d, width, E, top = 8, 2, 64, 256, 8, 2
