@@ -551,7 +551,7 @@ int bifeat_linear_pack(const bifeat_linear_spec *spec, const void *weight, int32
 /* The values that the codes stand for, fp32 [experts][out_features][in_features]. */
 int bifeat_linear_unpack(const bifeat_linear_spec *spec, const uint8_t *packed, float *weight, void *stream);
 /* x: DEVICE rows of in_features columns, `row_stride` elements apart (>= 0); out: DEVICE
- * [rows][out_features], which shares no memory with x.  One matrix (experts = 1).
+ * [rows][out_features], which shares no memory with x (BIFEAT_EINVAL).  One matrix (experts = 1).
  * workspace: DEVICE memory of bifeat_linear_workspace() bytes (often 0: NULL will do), 16-byte
  * aligned, for the time of the call's kernels alone. */
 int64_t bifeat_linear_workspace(const bifeat_linear_spec *spec, int64_t rows, int32_t dtype);
@@ -570,7 +570,8 @@ typedef struct {
 /* Bytes of DEVICE memory that bifeat_linear_experts needs besides, 16-byte aligned and for
  * the time of the call's kernels alone; or BIFEAT_EINVAL. */
 int64_t bifeat_linear_experts_workspace(const bifeat_linear_spec *spec, const bifeat_expert_rows *rows);
-/* out: DEVICE [tokens][choices][out_features], with weights [tokens][out_features]. */
+/* out: DEVICE [tokens][choices][out_features], with weights [tokens][out_features]; it shares no
+ * memory with x (BIFEAT_EINVAL) or the other arrays. */
 int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed, const bifeat_expert_rows *rows, int32_t dtype,
                           void *out, void *workspace, int64_t workspace_bytes, void *stream);
 

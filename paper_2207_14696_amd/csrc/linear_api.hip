@@ -92,6 +92,15 @@ Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     return o;
 }
 
+// Whether one of `rows` rows, `stride` elements apart, and `bytes` of out share memory.
+bool meets(const void *x, int64_t rows, int64_t stride, int64_t columns, int32_t dtype, const void *out, int64_t bytes) {
+    const __int128 element = dtype == BIFEAT_F32 ? 4 : 2, apart = stride * element, row = columns * element;
+    const __int128 begin = (__int128)(uintptr_t)out - (__int128)(uintptr_t)x, end = begin + bytes;
+    // (the first row that ends behind out's beginning)
+    const __int128 first = row > begin ? 0 : apart == 0 ? rows : (begin - row) / apart + 1;
+    return first < rows && first * apart < end;
+}
+
 }  // namespace
 
 extern "C" {
@@ -120,6 +129,8 @@ int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed
     if (!spec_ok(spec) || spec->experts != 1 || !type_ok(dtype) || rows < 0 || rows > INT32_MAX - 64 || row_stride < 0) return BIFEAT_EINVAL;
     if (rows == 0) return BIFEAT_OK;
     if (!packed || (uintptr_t)packed % 16 || !data_ok(x, dtype) || !data_ok(out, dtype) || (uintptr_t)workspace % 16) return BIFEAT_EINVAL;
+    // (others read x while out is written)
+    if (meets(x, rows, row_stride, spec->in_features, dtype, out, rows * spec->out_features * (dtype == BIFEAT_F32 ? 4 : 2))) return BIFEAT_EINVAL;
     const Plan plan = plan_of(spec, rows, dtype);
     if (plan.bytes(spec, rows) > (workspace ? workspace_bytes : 0)) return BIFEAT_EINVAL;
     const bf::Matrices m = matrices_of(spec, packed);
@@ -146,6 +157,12 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     if (!packed || (uintptr_t)packed % 16 || !data_ok(r->x, dtype) || !data_ok(out, dtype) || !r->ids || (uintptr_t)r->ids % 4 ||
         (uintptr_t)r->weights % 4 || !workspace || (uintptr_t)workspace % 16)
         return BIFEAT_EINVAL;
+    const int64_t outputs = r->tokens * (r->weights ? 1 : r->choices) * spec->out_features;
+    for (int j = 0; j < (r->choice_stride ? r->choices : 1); j++) {
+        const uint8_t *x = static_cast<const uint8_t *>(r->x);
+        const int64_t element = dtype == BIFEAT_F32 ? 4 : 2;
+        if (meets(x + j * r->choice_stride * element, r->tokens, r->token_stride, spec->in_features, dtype, out, outputs * element)) return BIFEAT_EINVAL;
+    }
     const Room room = room_of(spec, r);
     if (workspace_bytes < room.bytes) return BIFEAT_EINVAL;
     const bf::Matrices m = matrices_of(spec, packed);

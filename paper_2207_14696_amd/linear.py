@@ -64,7 +64,7 @@ class PackedLinear:
     def multiply(self, packed, x, out=None):
         """x [..., in_features] times the matrix's rows: [..., out_features] of x's type (float32, float16 or bfloat16).  Rows may lie any
         distance apart, their columns next to each other.  There is no backward pass: where x requires a gradient, going back
-        through the output raises, and ``out`` is refused."""
+        through the output raises, and ``out`` is refused.  ``out`` shares no memory with x (refused too)."""
         if out is None and self.experts is None and (calls := _b._calls or _b._load_calls()):
             r = calls.linear_multiply(*self._multiply, packed, x)
             if r is not None:
@@ -103,7 +103,7 @@ class PackedLinear:
         own; ids int32 [tokens, choices], as ``route`` gives them (an id outside [0, experts) names none and gives zeros).  Returns
         [tokens, choices, out_features] of x's type, or with ``weights`` float32 [tokens, choices] their weighted sum,
         [tokens, out_features].  Takes memory for the time of the call: 4 bytes a pair of a token and a choice, with weights
-        4 * out_features more.  No backward pass, as ``multiply``."""
+        4 * out_features more.  No backward pass, and an ``out`` of its own memory, as ``multiply``."""
         if out is None and self.experts is not None and (calls := _b._calls or _b._load_calls()):
             r = calls.linear_experts(*self._by_experts, packed, x, ids, weights)
             if r is not None:

@@ -362,6 +362,34 @@ def test_experts_all_tokens_to_one_and_to_none(bf, torch):
 
 # ------------------------------------------------------------------ gradients, streams, graphs
 
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_outputs_beside_and_on_top_of_rows(bf, torch, T):
+    rng = np.random.default_rng(T)
+    N = K = 128
+    layer, packed, values, size = _layer(bf, torch, rng, N, K, 64)
+    rows = torch.randn(T, K, device="cuda").half()
+    exact = _host(rows).astype(np.float64) @ values.T
+    bound = _bound(K, np.abs(_host(rows).astype(np.float64)), size, exact, "f16")
+    room = torch.zeros((2 * T + 1) * K, dtype=torch.float16, device="cuda")
+    x = room[T * K:2 * T * K].view(T, K)
+    x.copy_(rows)
+    experts = bf.PackedLinear(N, K, group=64, experts=1)
+    ids = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    for first in (T * K, 1, T * K + 127):
+        out = room[first:first + T * K].view(T, N)
+        with pytest.raises(bf.BifeatError):
+            layer.multiply(packed, x, out=out)
+        with pytest.raises(bf.BifeatError):
+            experts.multiply_experts(packed[None], x, ids, out=out[:, None])
+    beside = room[:T * K].view(T, N)
+    _assert_close(_host(layer.multiply(packed, x, out=beside)), exact, bound)
+    assert torch.equal(x, rows)
+    _assert_close(_host(experts.multiply_experts(packed[None], x, ids, out=beside[:, None])[:, 0]), exact, bound)
+    apart = torch.zeros(T, (T + 2) * K, dtype=torch.float16, device="cuda")     # out between the first row and the second
+    apart[:, :K] = rows
+    _assert_close(_host(layer.multiply(packed, apart[:, :K], out=apart[0, K:(T + 1) * K].view(T, N))), exact, bound)
+
+
 def test_going_back_raises(bf, torch):
     rng = np.random.default_rng(0)
     layer, packed, *_ = _layer(bf, torch, rng, 16, 64, 64)

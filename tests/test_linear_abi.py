@@ -33,6 +33,13 @@ def test_sizes_and_specs(bf):
             bf.PackedLinear(16, 16, 64, experts)
 
 
+def test_sizes_that_32_bits_do_not_hold(bf):
+    for sizes in ((1 << 32 | 16, 128), (16, 1 << 32 | 128), (16, 128, 1 << 32 | 64), (16, 128, 64, 1 << 32 | 2), (16 - (1 << 32), 128)):
+        with pytest.raises(bf.BifeatError) as e:
+            bf.PackedLinear(*sizes)
+        assert e.value.status == bf.EINVAL
+
+
 def test_linear_argument_errors_come_before_any_gpu_call(bf):
     from paper_2207_14696_amd.binding import _CExpertRows, _CLinearSpec
     lib = bf.load_library()
@@ -78,6 +85,29 @@ def test_linear_argument_errors_come_before_any_gpu_call(bf):
     small, joined = (lib.bifeat_linear_experts_workspace(spec(experts=4), rows(w=w)) for w in (None, 16))
     assert joined == small + 6 * 32 * 4 and small % 16 == 0
     assert experts(r=rows(w=16), size=joined - 1) == -1
+
+
+def test_outputs_on_top_of_rows_are_refused(bf):
+    from paper_2207_14696_amd.binding import _CExpertRows, _CLinearSpec
+    lib = bf.load_library()
+    x, T, N, K = 1 << 30, 4000, 32, 64
+    for dtype, e in ((0, 4), (1, 2), (2, 2)):
+        row, outs = K * e, T * N * e
+
+        def multiply(out, stride=K):
+            return lib.bifeat_linear_multiply(C.byref(_CLinearSpec(N, K, 64, 1)), 16, x, stride, T, dtype, out, 16, 1 << 40, None)
+
+        far = 10 ** 6
+        assert multiply(x) == multiply(x - outs + e) == multiply(x + T * row - e) == multiply(x + row - e, far) == multiply(x + far * e - outs + e, far) == -1
+        assert multiply(x + (T - 1) * far * e, far) == multiply(x, 0) == multiply(x + row - e, 0) == multiply(x, 1 << 62) == -1
+
+        def experts(out, own=False, weights=None, token=2 * K, choice=K):
+            r = _CExpertRows(x, token, choice if own else 0, 16, weights, T, 2)
+            return lib.bifeat_linear_experts(C.byref(_CLinearSpec(N, K, 64, 4)), 16, C.byref(r), dtype, out, 16, 1 << 40, None)
+
+        for w in (None, 16):
+            assert experts(x, weights=w) == experts(x - e, weights=w) == experts(x + (2 * T - 1) * row - e, weights=w) == -1
+            assert experts(x + 2 * T * row - e, True, w) == experts(x + far * e + row - e, True, w, 2 * far, far) == -1
 
 
 def test_route_argument_errors_come_before_any_gpu_call(bf):
