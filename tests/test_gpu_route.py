@@ -264,3 +264,10 @@ def test_refusals_on_the_device(bf, torch):
     for bias in (torch.zeros(16), torch.zeros(16, device="cuda").half(), torch.zeros(32, device="cuda")[::2]):
         with pytest.raises(ValueError):
             bf.route(x, 2, bias=bias)
+
+
+def test_numbers_that_32_bits_do_not_hold(bf, torch):
+    x = torch.zeros(3, 16, device="cuda")
+    for kw in (dict(choices=1 << 32 | 2), dict(choices=2, groups=1 << 32 | 4), dict(choices=2, groups=4, top_groups=(1 << 32) + 1), dict(choices=2 - (1 << 32))):
+        with pytest.raises(bf.BifeatError):
+            bf.route(x, **kw)
