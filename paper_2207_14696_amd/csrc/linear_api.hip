@@ -77,9 +77,9 @@ struct Room {
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
     const int64_t pairs = r->tokens * r->choices;
-    // tiles of 128 rows from 22 pairs an expert on: 64 matrices of 1536 x 2048 with 16 each 57 us in tiles of 16, 68 in tiles of 128; with 24 75 and 72, with
-    // 64 161 and 86
-    o.tile = pairs >= 22 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
+    // tiles of 128 rows from 40 pairs an expert on: 64 matrices of 1536 x 2048 with 24 each 48 us in tiles of 16, 69 in tiles of 128; with 32 59 and 68, with 48
+    // 81 and 72, with 64 101 and 80 (16 of 4096 x 4096: with 32 66 and 81, with 48 90 and 82; 128 of 2048 x 768: 72 and 84, 95 and 90)
+    o.tile = pairs >= 40 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + (o.most_tiles + 1) / 2 * 16;  // (a tile is 8 bytes)
     static_assert(sizeof(bf::Tile) == 8, "");
