@@ -77,9 +77,11 @@ struct Room {
 Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
     const int64_t pairs = r->tokens * r->choices;
-    // tiles of 128 rows from 40 pairs an expert on: 64 matrices of 1536 x 2048 with 24 each 48 us in tiles of 16, 69 in tiles of 128; with 32 59 and 68, with 48
-    // 81 and 72, with 64 101 and 80 (16 of 4096 x 4096: with 32 66 and 81, with 48 90 and 82; 128 of 2048 x 768: 72 and 84, 95 and 90)
-    o.tile = pairs >= 40 * (int64_t)s->experts && s->in_features >= 8 ? bf::kManyRows : 16;
+    // Tiles of up to 128 pairs where an expert has 16 on the average, and where so large ones are enough for the whole card: there 14 000 pairs times 128-row
+    // tiles of the matrix.  In tiles of 16 and of 128: 64 matrices of 1536 x 2048 with 16 pairs each 37 us and 37, with 32 57 and 44, with 48 79 and 59; 128 of
+    // 2048 x 768 with 16 44 and 43, with 32 69 and 52; 16 of 4096 x 4096 with 24 51 and 46; 200 of 512 x 1024 with 16 26 and 31, with 32 40 and 38; 8 of 1024 x 1024
+    // with 64 11 and 21, with 256 25 and 24; 32 of them with 48 21 and 23, with 96 33 and 30; 8 of 4096 x 4096 with 24 31 and 34, with 48 47 and 42.
+    o.tile = pairs >= 16 * (int64_t)s->experts && pairs * ((s->out_features + 127) / 128) >= 14000 && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + (o.most_tiles + 1) / 2 * 16;  // (a tile is 8 bytes)
     static_assert(sizeof(bf::Tile) == 8, "");

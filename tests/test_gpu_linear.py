@@ -328,6 +328,39 @@ def test_experts(bf, torch, dtype, T, E, k, K, N, group, own_rows, joined):
     assert torch.equal(layer.multiply_experts(*args), got)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,E,k,K,N,group", [(450, 40, 4, 160, 1000, 64), (900, 16, 2, 300, 1030, 128), (600, 100, 3, 77, 900, 32), (7100, 3, 1, 96, 130, 32),
+                                             (2000, 130, 8, 8, 65, 64), (700, 6, 3, 260, 1160, 32)])
+@pytest.mark.parametrize("own_rows,joined", [(False, False), (True, True)])
+def test_experts_of_many_pairs(bf, torch, dtype, T, E, k, K, N, group, own_rows, joined):
+    test_experts(bf, torch, dtype, T, E, k, K, N, group, own_rows, joined)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("joined", [False, True])
+def test_experts_tiles_of_every_fill(bf, torch, dtype, joined):
+    """Experts with 1, 2, ... 140 pairs each."""
+    rng = np.random.default_rng(5)
+    E, K, N, group = 140, 136, 257, 64
+    layer, packed, values, sizes = _experts(bf, torch, rng, E, N, K, group)
+    ids = rng.permutation(np.repeat(np.arange(E), np.arange(1, E + 1)))[:, None]
+    T = len(ids)
+    assert T * 3 >= 14000 and T >= 16 * E
+    x = torch.from_numpy(rng.standard_normal((T, K)).astype(np.float32)).cuda().to(_dtype(torch, dtype))
+    w = rng.random((T, 1)).astype(np.float32)
+    h = _host(x).astype(np.float64)
+    exact, size = np.zeros((T, N)), np.zeros((T, N))
+    for e in range(E):
+        at = ids[:, 0] == e
+        exact[at] = h[at] @ values[e].T
+        size[at] = _bound(K, np.abs(h[at]), sizes[e], exact[at], dtype)
+    device_ids = torch.from_numpy(ids.astype(np.int32)).cuda()
+    got = layer.multiply_experts(packed, x, device_ids, torch.from_numpy(w).cuda() if joined else None)
+    if joined:      # (the product of the sum and the weight is rounded to 32 bits once more)
+        exact, size = exact * w, size * w + np.abs(exact) * w * 2.0 ** -24 + LEAST[dtype]
+    _assert_close(_host(got).reshape(T, N), exact, size)
+
+
 @pytest.mark.parametrize("own_rows", [False, True])
 def test_experts_rows_with_strides(bf, torch, own_rows):
     rng = np.random.default_rng(3)
