@@ -38,8 +38,8 @@ struct Plan {
 // Of the ways to take the rows the one that is the fastest by what they measured (bf16, in parentheses fp32; us; 256 workgroups run at a time, for 128 rows 512):
 //   16 tb rows by 16 r of the matrix a workgroup: 2.5 a call, and a round of workgroups 0.12, 0.2, 0.37, 0.55 a block of columns for tb = 1..4 (0.3, 0.6
 //     for 1, 2): 16 rows by 4096 x 4096 6.8, 64 rows 20; by 16 384 x 4096 24, 128 rows 43;
-//   128 rows by 128: 8 (what is summed first, and the beginning), 1.25 a block (3.6), 2.3 where two workgroups share a CU: 64 rows by 4096 x 4096 46,
-//     1024 51, 2048 83; fp32 64 rows 122, 2048 205;
+//   128 rows by 128: 8 (what is summed first, and the beginning), 1.25 a block (3.6), 2.3 where two workgroups share a CU: 128 rows by 4096 x 4096 44,
+//     1024 51, 2048 79; fp32 128 rows 135, 2048 205 (a tile of 65 to 96 rows 0.8 of it);
 //   columns in parts: the parts' sums written and added, 2.5 and 8 bytes a sum and part at 4 TB/s: 40 rows by 8192 columns in one part 26, in four 15.
 Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
     const bool wide = dtype == BIFEAT_F32;
