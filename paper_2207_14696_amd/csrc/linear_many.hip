@@ -105,8 +105,8 @@ __global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t 
 }
 
 // Rows have 8 columns at least.  A workgroup of four waves takes 128 rows of the matrix and 128 of x, a wave 32 of the matrix's and all of x's (64 of each would
-// unpack each code twice).  Codes come from memory as the operands that they are; x goes through LDS, by steps of kStep columns, those two and three steps on
-// on their way while this one's products run.
+// unpack each code twice).  Codes come from memory as the operands that they are; x goes through LDS, by steps of kStep columns, the next but one and the
+// one after it on their way while this one's products run.
 // What (m_g - 16 s_g) sum x adds is a product too, of groups in place of columns: minimum and scale are bfloat16, the sums three of them (the kernel above),
 // so six exact products take 16 groups at a time, where adding it after each group would take two instructions a sum more.
 constexpr int kRows = kManyRows;
