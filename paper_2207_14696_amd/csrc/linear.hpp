@@ -129,10 +129,9 @@ struct XRows {
     int choices;  // rows of a token (1 without experts)
     int64_t count;
     void *out;
-    // of many rows, the sums of each group's columns: [3][sum_rows][sum_groups] bfloat16, a row of x as often as it lies in memory
-    const uint16_t *sums;
+    // of many rows, the sums of each group's columns: [sum_rows][groups of all blocks][4] bfloat16, a row of x as often as it lies in memory
+    const uint2 *sums;
     int64_t sum_rows;
-    int sum_groups;  // a multiple of 16
 };
 
 // Where rows are dealt to experts, a tile is up to 16 or kManyRows pairs of a token and one of its choices that name one expert; it has as many places in `order`,

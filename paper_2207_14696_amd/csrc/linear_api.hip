@@ -24,8 +24,9 @@ bf::Matrices matrices_of(const bifeat_linear_spec *s, const uint8_t *packed) {
     return {packed, (int64_t)rows * blocks * (1024 + 64 * (128 / s->group)), s->out_features, s->in_features, rows, blocks, s->experts};
 }
 
-int sum_groups(const bifeat_linear_spec *s) { return ((s->in_features + 127) / 128 * (128 / s->group) + 15) / 16 * 16; }
-int64_t sum_bytes(const bifeat_linear_spec *s, int64_t rows) { return 3 * rows * sum_groups(s) * 2; }
+int64_t sum_bytes(const bifeat_linear_spec *s, int64_t rows) {  // (a multiple of 16)
+    return (rows * ((s->in_features + 127) / 128 * (128 / s->group)) + 1) / 2 * 16;
+}
 
 // How a product of rows with one matrix is taken.
 struct Plan {
@@ -138,9 +139,9 @@ int bifeat_linear_multiply(const bifeat_linear_spec *spec, const uint8_t *packed
     const bf::Matrices m = matrices_of(spec, packed);
     const hipStream_t s = (hipStream_t)stream;
     const bool split = plan.split > 1;
-    bf::XRows r{x, row_stride, 0, 1, rows, split ? workspace : out, nullptr, rows, sum_groups(spec)};
+    bf::XRows r{x, row_stride, 0, 1, rows, split ? workspace : out, nullptr, rows};
     if (plan.many) {
-        r.sums = reinterpret_cast<const uint16_t *>(static_cast<uint8_t *>(workspace) + plan.parts_bytes(spec, rows));
+        r.sums = reinterpret_cast<const uint2 *>(static_cast<uint8_t *>(workspace) + plan.parts_bytes(spec, rows));
         BF_HIP(bf::launch_linear_sums(m, spec->group, r, dtype, s));
         BF_HIP(bf::launch_linear_many(m, spec->group, r, nullptr, 0, dtype, split, plan.split, s));
     } else BF_HIP(bf::launch_linear_few(m, spec->group, r, nullptr, 0, dtype, split, {plan.tb, plan.r, plan.split, 8}, s));
@@ -177,7 +178,7 @@ int bifeat_linear_experts(const bifeat_linear_spec *spec, const uint8_t *packed,
     BF_HIP(bf::launch_linear_deal(r->ids, (int)pairs, spec->experts, room.tile, reinterpret_cast<int *>(w + room.counts), tiles_count, tiles, order, s));
     const bf::Deal deal{tiles_count, tiles, order};
     const bf::XRows x{r->x, r->token_stride, r->choice_stride, r->choices, pairs, r->weights ? (void *)products : out,
-                      reinterpret_cast<const uint16_t *>(w + room.sums), room.sum_rows, sum_groups(spec)};
+                      reinterpret_cast<const uint2 *>(w + room.sums), room.sum_rows};
     const bool to_float = r->weights != nullptr;
     // many workgroups have four waves each: a wave then has more blocks to go through, and the beginnings and ends of the others beside it (32 tokens of 8
     // of 128 experts of 1536 x 2048 54 us by eight waves and 32 rows, 45 by four, 43 by four and 64 rows; one token 8.7 and 9.4)

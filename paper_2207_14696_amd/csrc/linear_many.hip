@@ -41,11 +41,11 @@ __device__ inline float of_neighbour(float x) {
 
 typedef Operand<Brain16>::Eight Brains;
 
-// The sums of each group's columns of the rows of x, each as three bfloat16 that are it together: sums[piece][row][group], groups past the last as zeros.
+// The sums of each group's columns of the rows of x, each as three bfloat16 that are it together and a zero: sums[row][group][4], groups past the last as zeros.
 // A wave takes kRowsOf rows, a lane eight columns; four loads of 512 columns are on their way at a time, of one long row or of four short ones, and 64 groups at
 // a time are written side by side.  2048 rows of 4096 columns 5.0 us (a lane each writing what it has 10), 32 768 of 768 10 (20).
 template <typename T, int GPB, int kRowsOf>
-__global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t row0, int64_t rows, int K, int groups, uint16_t *sums) {
+__global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t row0, int64_t rows, int K, int groups, uint2 *sums) {
     constexpr int kLanes = 16 / GPB, kChunks = 4 / kRowsOf;  // lanes of a group, loads of a row
     constexpr int kPerChunk = 64 / kLanes;                    // groups
     __shared__ float all[kThreads / 64][kRowsOf][64];
@@ -92,13 +92,13 @@ __global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t 
 #pragma unroll
         for (int i = 0; i < kRowsOf; i++) {
             float y = all[wave][i][lane];
-            if (g0 + lane < groups && r0 + i < rows)
+            uint32_t piece[3];
 #pragma unroll
-                for (int p = 0; p < 3; p++) {
-                    const uint32_t piece = __builtin_bit_cast(uint32_t, y) & 0xffff0000u;
-                    sums[((int64_t)p * rows + r0 + i) * groups + g0 + lane] = (uint16_t)(piece >> 16);
-                    y -= __builtin_bit_cast(float, piece);
-                }
+            for (int p = 0; p < 3; p++) {
+                piece[p] = __builtin_bit_cast(uint32_t, y) & 0xffff0000u;
+                y -= __builtin_bit_cast(float, piece[p]);
+            }
+            if (g0 + lane < groups && r0 + i < rows) sums[(r0 + i) * groups + g0 + lane] = make_uint2(piece[0] >> 16 | piece[1], piece[2] >> 16);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -107,19 +107,31 @@ __global__ __launch_bounds__(kThreads) void linear_sums_kernel(XRows x, int64_t 
 // Rows have 8 columns at least.  A workgroup of four waves takes 128 rows of the matrix and 128 of x, a wave 32 of the matrix's and all of x's (64 of each would
 // unpack each code twice).  Codes come from memory as the operands that they are; x goes through LDS, by steps of kStep columns, the next but one and the
 // one after it on their way while this one's products run.
-// What (m_g - 16 s_g) sum x adds is a product too, of groups in place of columns: minimum and scale are bfloat16, the sums three of them (the kernel above),
-// so six exact products take 16 groups at a time, where adding it after each group would take two instructions a sum more.
+// What (m_g - 16 s_g) sum x adds is a product too: minimum and scale are bfloat16, the sums three of them (the kernel above), so that one product of 16
+// "columns" adds two groups', exactly: of a block of 64 or 128 columns, where a group is 128 of every other block and the one before it (a product a block 305 us at
+// 8192 rows, 288 so).  All groups' minima at first would take a product for 16 groups (2048 rows 78 us for 80, in groups of 32 105 for 97), but the result would then
+// stand at the size of all minima together, and the 16's, until the sums take them back: hundreds of times its own where the columns of x have a mean.  (x of
+// mean and deviation 1 in 32 bits by 8192 columns in groups of 32: an error of 3.3e-5 then, 2.7e-6 now, by few rows' kernel 8.8e-7; by 4096 in groups of 128 2.5e-6
+// and 3.4e-6.)
 constexpr int kRows = kManyRows;
 template <typename T> constexpr int kStep = sizeof(T) == 4 ? 32 : 64;
+
+template <typename X>
+__device__ inline X of_bytes(const X *p, uint32_t further) {
+    return *reinterpret_cast<const X *>(reinterpret_cast<const uint8_t *>(p) + further);
+}
 
 template <typename T, int GPB, bool DEALT, typename Out>
 __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x, Deal deal, Out *out, int row_tiles, int tile0, int tiles_end) {
     typedef Operand<T> O;
     typedef typename O::Eight Operands;
-    constexpr int P = O::kPieces, S = kStep<T>, kChunks = S / 8, kLoads = kRows * kChunks / 256;
+    constexpr int P = O::kPieces, S = kStep<T>, kChunks = S / 8;
     constexpr int kStride = kRows + 1;  // (of a chunk in 16 bytes: the lanes that write a row's chunks meet no two in a bank)
     __shared__ uint4 tile[2][P][kChunks * kStride];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, col = lane % 32, half = lane / 32;
+    constexpr int kPairs = GPB == 4 ? 2 : 1;        // of groups that a block has
+    constexpr bool kTwo = GPB == 1 && P == 1;        // where it is one group, two blocks are a pair (of 32-bit rows, for want of registers, each by itself)
+    __shared__ uint4 pair_sums[2][kPairs][kRows];  // the sums of x of two groups
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), col = lane % 32, half = lane / 32;
     // Workgroups go to the eight XCDs in turn.  tiles_end > 0: each XCD takes whole tiles of x, whose products with all rows of the matrix find them in its L2
     const int die = blockIdx.x % 8, of_die = blockIdx.x / 8;
     const int n_tile = tiles_end ? of_die % row_tiles : blockIdx.x % row_tiles;
@@ -154,13 +166,10 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
     };
     // what a thread brings of x: chunk `threadIdx.x % kChunks` of the rows threadIdx.x / kChunks, + 256 / kChunks, ...
     const int chunk = threadIdx.x % kChunks;
-    const T *from[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; i++) {
-        const int at = threadIdx.x / kChunks + i * (256 / kChunks);
-        const int64_t row = row_of(at), token = DEALT ? (int64_t)((uint32_t)row / (uint32_t)x.choices) : row;
-        from[i] = static_cast<const T *>(x.x) + token * x.token_stride + (DEALT ? (row - token * x.choices) * x.choice_stride : 0);
-    }
+    const auto from_of = [&](int thread, int i) {
+        const int64_t row = row_of(thread / kChunks + i * (256 / kChunks)), token = DEALT ? (int64_t)((uint32_t)row / (uint32_t)x.choices) : row;
+        return static_cast<const T *>(x.x) + token * x.token_stride + (DEALT ? (row - token * x.choices) * x.choice_stride : 0);
+    };
     const int begin = (int)((int64_t)m.blocks * blockIdx.y / gridDim.y), end = (int)((int64_t)m.blocks * (blockIdx.y + 1) / gridDim.y);  // of the columns
     if constexpr (!DEALT) out += blockIdx.y * x.count * m.N;
     const int n0 = kRows * n_tile + 32 * wave;  // the wave's rows of the matrix
@@ -168,6 +177,9 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
     const uint32_t *all_levels = reinterpret_cast<const uint32_t *>(packed + m.code_bytes());
     const int groups = m.blocks * GPB;
     const auto row16 = [&](int r) { return r < m.rows ? r : m.rows - 1; };
+    // (the wave's part of an address, and the lane's in 32 bits: fewer registers)
+    const int rows0 = row16(n0 / 16);
+    const uint32_t lane_rows = row16(n0 / 16 + col / 16) - rows0;
     // The products with 32 J rows of x.
     const auto run = [&](auto wide) {
         constexpr int J = decltype(wide)::value, L = (32 * J * kChunks + 255) / 256;  // (loads that reach them)
@@ -175,6 +187,13 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
 #pragma unroll
         for (int j = 0; j < J; j++) total[j] = 0.f;
 
+        const T *from[L];
+        {
+            int thread = threadIdx.x;  // (worked out here, and again for the last columns: they would be kept from the other widths' beginnings, or beside what the loop counts up)
+            asm("" : "+v"(thread));
+#pragma unroll
+            for (int i = 0; i < L; i++) from[i] = from_of(thread, i);
+        }
         Columns<T> coming[2][L];  // of the next steps, by turns
         const auto bring = [&](int step, Columns<T> (&c)[L]) {
 #pragma unroll
@@ -190,26 +209,58 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
                 for (int p = 0; p < P; p++) tile[part & 1][p][chunk * kStride + at] = __builtin_bit_cast(uint4, b[p]);
             }
         };
-        const uint32_t *my_levels = all_levels + (int64_t)row16(n0 / 16 + col / 16) * groups * 16 + col % 16;
-        uint32_t level[GPB], level_now[GPB];
+        const uint32_t *my_levels = all_levels + (int64_t)rows0 * groups * 16;
+        const uint32_t levels_at = (lane_rows * groups * 16 + col % 16) * 4;
+        uint32_t level[GPB], level_now[GPB] = {}, level_before = 0;
         const auto bring_levels = [&](int k) {
 #pragma unroll
-            for (int g = 0; g < GPB; g++) level[g] = my_levels[(k * GPB + g) * 16];
+            for (int g = 0; g < GPB; g++) level[g] = of_bytes(my_levels + (k * GPB + g) * 16, levels_at);
         };
-        const uint4 *my_codes = codes + (int64_t)row16(n0 / 16 + col / 16) * m.blocks * 64 + col % 16 + 16 * half;
+        const uint4 *my_codes = codes + (int64_t)rows0 * m.blocks * 64;
+        const uint32_t codes_at = (lane_rows * m.blocks * 64 + col % 16 + 16 * half) * 16;
         uint4 a[2], now[2];
         const auto bring_codes = [&](int k) {
 #pragma unroll
-            for (int e = 0; e < 2; e++) a[e] = my_codes[(int64_t)k * 64 + 32 * e];
+            for (int e = 0; e < 2; e++) a[e] = of_bytes(my_codes + (int64_t)k * 64 + 32 * e, codes_at);
         };
         const auto take = [&] {
+            level_before = level_now[0];
 #pragma unroll
             for (int e = 0; e < 2; e++) now[e] = a[e];
 #pragma unroll
             for (int g = 0; g < GPB; g++) level_now[g] = level[g];
         };
-        const auto multiply = [&](int part) {
-            constexpr int kDeep = P == 1 ? 2 : 1;  // (of three pieces two would not fit the registers)
+        constexpr int kParts = 128 / S;
+        // What a pair of groups' minima add, of the block r after the first (where two are a pair the block before it besides, of odd r).
+        uint4 of[J];
+        const auto read_sums = [&](int r, int pair) {
+#pragma unroll
+            for (int j = 0; j < J; j++) of[j] = pair_sums[(kTwo ? r / 2 : r) & 1][pair][32 * j + col];
+        };
+        constexpr int kDeep = P == 1 ? 2 : 1;  // (of three pieces two would not fit the registers)
+        const auto add_minima = [&](int r, int pair, bool both) {
+            const bool two = kTwo && both;
+            uint32_t __attribute__((ext_vector_type(4))) rest;
+#pragma unroll
+            for (int i = 0; i < 2; i++) {
+                const uint32_t w = GPB > 1 ? level_now[GPB > 1 ? 2 * pair + i : 0] : i == 0 && two ? level_before : i == 0 || two ? level_now[0] : 0u;
+                // the lower half of the lanes has minima, the upper one -kMore scales (the sign, and 4 more in the exponent; a scale of 0 stays it, the largest ones pass
+                // what the header allows)
+                uint32_t more = 0;
+                if constexpr (O::kMore != 0.f) more = __builtin_bit_cast(uint32_t, __builtin_bit_cast(float, w << 16) * -O::kMore);
+                const uint32_t v = half ? more : w;  // (in its upper 16 bits)
+                rest[2 * i] = __builtin_amdgcn_perm(v, v, 0x07060706u);
+                rest[2 * i + 1] = v >> 16;
+            }
+#pragma unroll
+            for (int j = 0; j < J; j++) {
+                uint4 a = kDeep == 1 ? pair_sums[r & 1][pair][32 * j + col] : of[j];
+                if (GPB == 1 && !two) a.z = a.w = 0;
+                total[j] = product32<Brain16>(__builtin_bit_cast(Brains, a), __builtin_bit_cast(Brains, rest), total[j]);
+                if (kDeep == 1) __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        const auto multiply = [&](int r, int part, bool minima, bool both) {
             Operands b[kDeep][J][P];
             const auto read = [&](int s16) {
 #pragma unroll
@@ -218,7 +269,14 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
                     for (int p = 0; p < P; p++)
                         b[s16 % kDeep][j][p] = __builtin_bit_cast(Operands, tile[part & 1][p][(2 * s16 + half) * kStride + 32 * j + col]);
             };
+            constexpr int kPerPair = kParts / kPairs;
+            constexpr bool kAhead = kDeep == 2 && GPB > 1;
+            if (kAhead && part % kPerPair == 0) read_sums(r, part / kPerPair);
             if (kDeep == 2) read(0);
+            else if (part % kPerPair == 0) {  // (before x takes the registers)
+                add_minima(r, part / kPerPair, both);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             // (a wave's products before the other wave's other work: two waves that keep in step would both wait for the matrix cores, then both for the vector ones;
             // 8192 rows 291 us, 281 so)
             __builtin_amdgcn_s_setprio(1);
@@ -244,6 +302,10 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
                             sum[j] = product32<T>(b[s16 % kDeep][j][p], c, sum[j]);
                         }
                     }
+                if (kDeep == 2 && part % kPerPair == 0 && s16 == 0 && minima) {
+                    if (!kAhead) read_sums(r, part / kPerPair);
+                    add_minima(r, part / kPerPair, both);
+                }
                 if (s % kPer == kPer - 1) {
                     const int g = s / kPer;
                     __builtin_amdgcn_sched_barrier(0);
@@ -262,52 +324,22 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
             }
             __builtin_amdgcn_s_setprio(0);
         };
-        const auto add_sums = [&] {
-            int64_t at[J];
-#pragma unroll
-            for (int j = 0; j < J; j++) {
-                int64_t row = row_of(32 * j + col);
-                if (DEALT && !x.choice_stride) row = (int64_t)((uint32_t)row / (uint32_t)x.choices);
-                at[j] = row * x.sum_groups;
-            }
-            for (int g0 = begin * GPB / 16 * 16; g0 < end * GPB; g0 += 16) {
-                uint32_t w[8];
-#pragma unroll
-                for (int i = 0; i < 8; i++) {
-                    const int g = g0 + 8 * half + i;
-                    w[i] = my_levels[(g < groups ? g : groups - 1) * 16];
-                    w[i] = g >= begin * GPB && g < end * GPB ? w[i] : 0u;  // (of the part of the columns)
-                }
-                uint4 of[J][3];
-#pragma unroll
-                for (int j = 0; j < J; j++)
-#pragma unroll
-                    for (int p = 0; p < 3; p++) {
-                        struct __attribute__((packed, aligned(4))) Four {
-                            uint32_t w[4];
-                        };
-                        const Four f = *reinterpret_cast<const Four *>(x.sums + p * x.sum_rows * x.sum_groups + at[j] + g0 + 8 * half);
-                        of[j][p] = make_uint4(f.w[0], f.w[1], f.w[2], f.w[3]);
-                    }
-                uint32_t __attribute__((ext_vector_type(4))) low, scale;
-#pragma unroll
-                for (int i = 0; i < 4; i++) {
-                    low[i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
-                    // (-kMore times it: the sign, and 4 more in the exponent; a scale of 0 stays it, the largest ones pass what the header allows)
-                    const float s0 = __builtin_bit_cast(float, w[2 * i] << 16) * -O::kMore, s1 = __builtin_bit_cast(float, w[2 * i + 1] << 16) * -O::kMore;
-                    scale[i] = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, s1), __builtin_bit_cast(uint32_t, s0), 0x07060302u);
-                }
-#pragma unroll
-                for (int p = 2; p >= 0; p--)
-#pragma unroll
-                    for (int j = 0; j < J; j++) {
-                        total[j] = product32<Brain16>(__builtin_bit_cast(Brains, of[j][p]), __builtin_bit_cast(Brains, low), total[j]);
-                        if constexpr (O::kMore != 0.f) total[j] = product32<Brain16>(__builtin_bit_cast(Brains, of[j][p]), __builtin_bit_cast(Brains, scale), total[j]);
-                    }
-            }
+        // A block's sums of x: a thread brings half of a row's.
+        const uint32_t *my_sums = reinterpret_cast<const uint32_t *>(x.sums) + GPB * (threadIdx.x % 2);
+        {
+            int64_t row = row_of(threadIdx.x / 2);
+            if (DEALT && !x.choice_stride) row = (int64_t)((uint32_t)row / (uint32_t)x.choices);
+            my_sums += row * groups * 2;
+        }
+        typedef uint32_t HalfSums __attribute__((ext_vector_type(GPB)));
+        HalfSums half_sums;
+        const auto bring_sums = [&](int k) { half_sums = *reinterpret_cast<const HalfSums *>(my_sums + (int64_t)k * GPB * 2); };
+        const auto put_sums = [&](int r) {
+            const int row = threadIdx.x / 2, of = threadIdx.x % 2;
+            uint4 *to = &pair_sums[(kTwo ? r / 2 : r) & 1][kPairs == 2 ? of : 0][row];
+            *reinterpret_cast<HalfSums *>(reinterpret_cast<uint32_t *>(to) + (kTwo ? 2 * (r & 1) + of : GPB * of % 4)) = half_sums;
         };
         // Whole blocks: no branch leads to a load, so that none is waited for before its use; what is asked for past the last step is the last again.
-        constexpr int kParts = 128 / S;
         const int whole = end < m.K / 128 ? end : m.K / 128;
         if (begin < whole) {
             const int last = whole * kParts - 1;
@@ -315,37 +347,48 @@ __global__ __launch_bounds__(256, 2) void linear_many_kernel(Matrices m, XRows x
             bring(begin * kParts + 1, coming[1]);
             bring_levels(begin);
             bring_codes(begin);
-            add_sums();
+            bring_sums(begin);
             put(0, coming[0]);
+            put_sums(0);
             bring(begin * kParts + 2 < last ? begin * kParts + 2 : last, coming[0]);
+            bring_sums(begin + 1 < whole ? begin + 1 : begin);
             __syncthreads();
             for (int k = begin; k < whole; k++) {
                 const int next = k + 1 < whole ? k + 1 : k;
                 take();
                 bring_codes(next);
                 bring_levels(next);
+                put_sums(k - begin + 1);
+                bring_sums(k + 2 < whole ? k + 2 : whole - 1);
 #pragma unroll
                 for (int part = 0; part < kParts; part++) {
                     const int ahead = k * kParts + part + 3;
                     put((part + 1) % kParts, coming[(part + 1) & 1]);
                     bring(ahead < last ? ahead : last, coming[(part + 1) & 1]);
-                    multiply(part);
+                    multiply(k - begin, part, !kTwo || (k - begin) & 1, true);
                     __syncthreads();
                 }
             }
         }
+        if (kTwo && whole == end && (whole - begin) & 1) {  // (a block without another)
+            read_sums(whole - begin - 1, 0);
+            add_minima(whole - begin - 1, 0, false);
+        }
         if (whole < end) {  // the rows' last columns
-            if (begin >= whole) add_sums();
             bring_levels(whole);
             bring_codes(whole);
+            bring_sums(whole);
+            put_sums(whole - begin);
             take();
+            int again = threadIdx.x;
+            asm("" : "+v"(again));
 #pragma unroll
             for (int part = 0; part < kParts; part++) {
 #pragma unroll
-                for (int i = 0; i < L; i++) coming[0][i] = load_last_columns(from[i], 128 * whole + S * part + 8 * chunk, m.K);
+                for (int i = 0; i < L; i++) coming[0][i] = load_last_columns(from_of(again, i), 128 * whole + S * part + 8 * chunk, m.K);
                 put(part, coming[0]);
                 __syncthreads();
-                multiply(part);
+                multiply(whole - begin, part, true, (whole - begin) & 1);
                 __syncthreads();
             }
         }
@@ -428,10 +471,10 @@ hipError_t launch_linear_sums(const Matrices &m, int group, const XRows &x, int 
     const int64_t rows = x.sum_rows;
     const int of = m.K > 1024 ? 1 : 4;
     const int64_t per = kThreads / 64 * of, most = per << 23;  // (a launch has fewer than 2^32 threads)
-    uint16_t *sums = const_cast<uint16_t *>(x.sums);
+    uint2 *sums = const_cast<uint2 *>(x.sums);
 #define BF_RUN(T, GPB)                                                                                                          \
-    if (of == 1) linear_sums_kernel<T, GPB, 1><<<grid, kThreads, 0, s>>>(x, row0, rows, m.K, x.sum_groups, sums);                    \
-    else linear_sums_kernel<T, GPB, 4><<<grid, kThreads, 0, s>>>(x, row0, rows, m.K, x.sum_groups, sums)
+    if (of == 1) linear_sums_kernel<T, GPB, 1><<<grid, kThreads, 0, s>>>(x, row0, rows, m.K, m.blocks * GPB, sums);                    \
+    else linear_sums_kernel<T, GPB, 4><<<grid, kThreads, 0, s>>>(x, row0, rows, m.K, m.blocks * GPB, sums)
 #define BF_GO(T)                                  \
     if (group == 128) { BF_RUN(T, 1); }           \
     else if (group == 64) { BF_RUN(T, 2); }       \
