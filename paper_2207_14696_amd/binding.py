@@ -258,6 +258,13 @@ def _without_backward():
     return WithoutBackward
 
 
+def _without_tangent(why, *tensors) -> None:
+    """Refuses what carries a tangent of forward-mode differentiation: the output would have none, which is a derivative of zero."""
+    from torch.autograd import forward_ad
+    if any(t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors):
+        raise NotImplementedError(why)
+
+
 def _np_ptr(a):
     return None if a is None else a.ctypes.data_as(C.c_void_p)
 

@@ -9,7 +9,7 @@ import functools
 import math
 
 from . import binding as _b
-from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _stream, _without_backward, load_library
+from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _stream, _without_backward, _without_tangent, load_library
 
 
 def _head_rows(t, heads: int, head_dim: int, name: str):
@@ -119,7 +119,7 @@ class PagedCache:
         with them (None for q None).  ``frequencies`` float32 [pairs], pairs <= head_dim / 2: radians a position of the column pairs
         (i, i + pairs), or (2 i, 2 i + 1) where ``interleaved``; columns from 2 * pairs on stay as they are.  ``scale``: of the turned
         columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q or frequencies
-        require one, going back through the output raises."""
+        require one, going back through the output raises, and tensors with a tangent of forward-mode differentiation are refused."""
         if calls := _b._calls or _b._load_calls():
             r = calls.cache_append(*self._append, pages, q, k, v, frequencies, bool(interleaved), scale, tables, lengths, indptr)
             if r is not None:
@@ -127,6 +127,7 @@ class PagedCache:
                     _check(r)
                 return None if r is True else r
         import torch
+        _without_tangent("PagedCache.append has no forward-mode derivative", q, k, v, frequencies)
         if q is not None and (q.requires_grad or frequencies.requires_grad) and torch.is_grad_enabled():
             call = functools.partial(self.append, pages, q.detach(), k, v, frequencies.detach(), tables, lengths, indptr, interleaved, scale)
             return _without_backward().apply("PagedCache.append has no backward pass", call, q, frequencies)
@@ -176,7 +177,7 @@ class PagedCache:
         ``softcap`` c > 0: c * tanh(score / c); ``window`` w > 0: the last w positions only; ``prefix`` int64
         [B]: positions that all queries see; ``slopes`` float32 [query heads]: bias by distance.  Returns
         [tokens, query heads, head_dim] of q's dtype.  There is no backward pass: where q requires a gradient, going back
-        through the output raises, and ``out`` is refused."""
+        through the output raises, and ``out`` is refused; a q with a tangent of forward-mode differentiation is refused."""
         scale = self._scale if scale is None else scale
         if out is None and (calls := _b._calls or _b._load_calls()):
             r = calls.cache_attend(*self._attend, pages, q, scale, softcap, window, prefix, slopes, tables, lengths, indptr)
@@ -185,6 +186,7 @@ class PagedCache:
                     _check(r)
                 return r
         import torch
+        _without_tangent("PagedCache.attend has no forward-mode derivative", q)
         if q.requires_grad and torch.is_grad_enabled():
             if out is not None:
                 raise ValueError("attend has no backward pass: no out where q requires a gradient")

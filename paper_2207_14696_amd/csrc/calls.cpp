@@ -10,6 +10,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/PythonTorchFunctionTLS.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <torch/csrc/autograd/custom_function.h>
@@ -43,6 +44,9 @@ using AggregateFn = int (*)(void *, const uint8_t *, int64_t, const int64_t *, c
 
 PyObject *g_device = nullptr, *g_stream = nullptr;  // torch._C._cuda_getDevice, ._cuda_getCurrentRawStream
 
+// Carries a tangent of forward-mode differentiation: none of these calls has a derivative of that kind, and binding.py says so.
+bool tangent(const at::Tensor &t) { return c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(/*level=*/0).defined(); }
+
 // `with`: of whose device it has to be
 const at::Tensor *tensor(PyObject *o, at::ScalarType a, at::ScalarType b, const at::Tensor *with = nullptr) {
     if (!THPVariable_CheckExact(o)) return nullptr;
@@ -50,6 +54,7 @@ const at::Tensor *tensor(PyObject *o, at::ScalarType a, at::ScalarType b, const 
     if (!t.defined() || !t.is_cuda() || t.dim() < 1 || t.layout() != at::kStrided) return nullptr;
     if (!t.unsafeGetTensorImpl()->has_storage() || !t.is_contiguous()) return nullptr;
     if (with && t.device() != with->device()) return nullptr;
+    if (t.is_floating_point() && tangent(t)) return nullptr;
     return t.scalar_type() == a || t.scalar_type() == b ? &t : nullptr;
 }
 
@@ -190,7 +195,7 @@ const at::Tensor *head_rows(PyObject *o, const Cache &c, bifeat_head_rows *r, in
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.dim() != 3 || t.layout() != at::kStrided || !t.unsafeGetTensorImpl()->has_storage() ||
-        t.size(2) != c.d || t.stride(2) != 1 || t.device() != c.pages->device())
+        t.size(2) != c.d || t.stride(2) != 1 || t.device() != c.pages->device() || tangent(t))
         return nullptr;
     const auto type = t.scalar_type();
     if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return nullptr;
@@ -351,7 +356,7 @@ const at::Tensor *float_rows(PyObject *o, const at::Tensor *with, int32_t *dtype
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor &t = THPVariable_Unpack(o);
     if (!t.defined() || !t.is_cuda() || t.dim() < 1 || t.layout() != at::kStrided || !t.unsafeGetTensorImpl()->has_storage() || t.stride(-1) != 1 ||
-        (with && t.device() != with->device()))
+        (with && t.device() != with->device()) || tangent(t))
         return nullptr;
     const auto type = t.scalar_type();
     if (type != at::kFloat && type != at::kHalf && type != at::kBFloat16) return nullptr;

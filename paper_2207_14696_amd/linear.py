@@ -6,9 +6,10 @@ from __future__ import annotations
 import ctypes as C
 
 from . import binding as _b
-from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _on_current_device, _stream, _without_backward, load_library
+from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _on_current_device, _stream, _without_backward, _without_tangent, load_library
 
 _WHY = "PackedLinear has no backward pass: its weights are codes"
+_FORWARD = "PackedLinear has no forward-mode derivative"
 
 
 class PackedLinear:
@@ -64,7 +65,7 @@ class PackedLinear:
     def multiply(self, packed, x, out=None):
         """x [..., in_features] times the matrix's rows: [..., out_features] of x's type (float32, float16 or bfloat16).  Rows may lie any
         distance apart, their columns next to each other.  There is no backward pass: where x requires a gradient, going back
-        through the output raises, and ``out`` is refused.  ``out`` shares no memory with x (refused too)."""
+        through the output raises, and ``out`` is refused; an x with a tangent of forward-mode differentiation is refused.  ``out`` shares no memory with x (refused too)."""
         if out is None and self.experts is None and (calls := _b._calls or _b._load_calls()):
             r = calls.linear_multiply(*self._multiply, packed, x)
             if r is not None:
@@ -76,6 +77,7 @@ class PackedLinear:
             raise ValueError("a layer of experts: multiply_experts")
         if x.dim() < 1 or x.shape[-1] != self.in_features:
             raise ValueError(f"x must be [..., {self.in_features}]")
+        _without_tangent(_FORWARD, x)
         if x.requires_grad and torch.is_grad_enabled():
             if out is not None:
                 raise ValueError(_WHY + ": no out where x requires a gradient")
@@ -118,6 +120,7 @@ class PackedLinear:
             raise ValueError(f"ids must be [tokens, choices], x [tokens, {self.in_features}] or [tokens, choices, {self.in_features}]")
         if weights is not None and weights.shape != ids.shape:
             raise ValueError("weights must be like ids")
+        _without_tangent(_FORWARD, x, weights)
         if torch.is_grad_enabled() and (x.requires_grad or (weights is not None and weights.requires_grad)):
             if out is not None:
                 raise ValueError(_WHY + ": no out where x or weights require a gradient")

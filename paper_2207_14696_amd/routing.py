@@ -6,7 +6,7 @@ import ctypes as C
 import functools
 
 from . import binding as _b
-from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _on_current_device, _stream, load_library
+from .binding import EINVAL, _check, _dev_ptr, _dtype_code, _on_current_device, _stream, _without_tangent, load_library
 
 
 _SCORES, _GROUP_SCORES = {"softmax": 0, "sigmoid": 1}, {"best": 0, "two": 1}
@@ -71,7 +71,7 @@ def route(logits, choices: int, score: str = "softmax", bias=None, groups: int =
     weights.  ``groups`` > 1: only the experts of the ``top_groups`` best groups of neighbours compete, a group being as good as
     its "best" expert or (``group_score`` "two") the sum of its two best.  ``renormalise``: weights are shares of their sum.  ``scale``: of the
     weights.  An expert whose logit is -infinity is not chosen.  Weights have a gradient in the logits (once); the choice and
-    the bias have none."""
+    the bias have none.  Logits with a tangent of forward-mode differentiation are refused."""
     if score in _SCORES and group_score in _GROUP_SCORES and (calls := _b._calls or _b._load_calls()):
         r = calls.route(*_entries(), logits, choices, _SCORES[score], bias, groups, top_groups, _GROUP_SCORES[group_score], bool(renormalise), scale)
         if r is not None:
@@ -81,6 +81,7 @@ def route(logits, choices: int, score: str = "softmax", bias=None, groups: int =
     import torch
     if logits.dim() < 1 or score not in _SCORES or group_score not in _GROUP_SCORES:
         raise ValueError('logits must be [..., experts], score "softmax" or "sigmoid", group_score "best" or "two"')
+    _without_tangent("route has no forward-mode derivative", logits)
     experts = logits.shape[-1]
     if bias is not None:
         if bias.shape != (experts,):
