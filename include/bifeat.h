@@ -395,7 +395,9 @@ int bifeat_scale_profile(const float *x, int64_t N, int64_t D, const int64_t *in
  *   queries turned with them.  Column pair i < pairs of a row of a token at position p is
  *   (i, i + pairs), or (2 i, 2 i + 1) where interleaved; with a = p * frequencies[i] it becomes
  *     (u, w) -> scale * (u cos a - w sin a),  scale * (u sin a + w cos a)
- *   and the columns from 2 * pairs on stay.  Angles, cosines and sines in 64 bits, as are the
+ *   and the columns from 2 * pairs on stay.  An angle a is exact below position 2^29 and the 64-bit
+ *   number next to it up to 2^30; a pair whose angle is 2^50 or more in size, or no number, becomes
+ *   NaN, and with it the token's keys.  Angles, cosines and sines in 64 bits, as are the
  *   turns of keys, which are then rounded to fp32 and written as above, and of 32-bit queries;
  *   16-bit queries are turned in fp32 and rounded to their type.  Values are written as
  *   they are.  Queries before their sequence's beginning come out as zeros.
@@ -473,7 +475,7 @@ typedef struct {
 
 /* How bifeat_cache_append turns rows by their position. */
 typedef struct {
-    const float *frequencies; /* DEVICE [pairs]: radians a position */
+    const float *frequencies; /* DEVICE [pairs]: radians a position; position * frequency below 2^50 in size */
     int32_t pairs;            /* 0..head_dim / 2 */
     int32_t interleaved;      /* 1: a pair's columns lie next to each other */
     double scale;             /* of the turned columns; usually 1 */

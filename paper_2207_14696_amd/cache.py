@@ -118,7 +118,8 @@ class PagedCache:
         """``write`` of keys that are turned to their positions on the way; returns the queries, q [tokens, query heads, head_dim], turned
         with them (None for q None).  ``frequencies`` float32 [pairs], pairs <= head_dim / 2: radians a position of the column pairs
         (i, i + pairs), or (2 i, 2 i + 1) where ``interleaved``; columns from 2 * pairs on stay as they are.  ``scale``: of the turned
-        columns.  The turn is computed in 64 bits, at any position.  No gradient passes through codes; where q or frequencies
+        columns.  Angles, and what becomes of keys and of 32-bit queries, are computed in 64 bits, queries of 16 bits in 32; a pair whose angle,
+        position times frequency, is 2^50 or more in size becomes NaN.  No gradient passes through codes; where q or frequencies
         require one, going back through the output raises, and tensors with a tangent of forward-mode differentiation are refused."""
         if calls := _b._calls or _b._load_calls():
             r = calls.cache_append(*self._append, pages, q, k, v, frequencies, bool(interleaved), scale, tables, lengths, indptr)

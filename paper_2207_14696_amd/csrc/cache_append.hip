@@ -7,8 +7,8 @@ namespace bf {
 namespace {
 
 // Column pair i of a row is turned by the angle a = p f_i, p the token's position: (u, w) becomes (u cos a - w sin a, u sin a + w cos a),
-// times a scale.  Angle, cosine, sine and the turned columns are 64-bit numbers: p f_i is exact below 2^29 positions, and a key's column comes
-// to its quantiser as the 32-bit number next to the exact one, so that codes are the definition's (an error of 2^-53 moves a rounding to 32
+// times a scale.  Angle, cosine, sine and the turned columns are 64-bit numbers: p f_i is exact below 2^29 positions (and the number next to it up to the last), and a
+// key's column comes to its quantiser as the 32-bit number next to the exact one, so that codes are the definition's (an error of 2^-53 moves a rounding to 32
 // bits once in 2^29 columns, where one of 2^-24 moves a level in 10 000).
 struct Turn {
     const float *frequencies;
@@ -17,11 +17,12 @@ struct Turn {
     double scale;
 };
 
-// Sine and cosine of an angle below 2^50 in size, off by less than 2^-51: what is left of it after the nearest multiple of a quarter turn (whose
+// Sine and cosine of an angle below 2^50 in size, off by less than 2^-51, of others NaN: what is left of it after the nearest multiple of a quarter turn (whose
 // product with a quarter turn of 106 bits the fused multiply-adds take off with one rounding each), by the series at zero as far as r^17 and r^16
 // (the next terms are below 2^-58 of 1).
 __device__ inline void sine_and_cosine(double angle, double &sine, double &cosine) {
-    const double n = rint(angle * 0x1.45f306dc9c883p-1);                                                   // 2 / pi
+    const bool far = !(fabs(angle) < 0x1p50);
+    const double n = far ? 0.0 : rint(angle * 0x1.45f306dc9c883p-1);                                       // 2 / pi
     const double r = fma(-n, 0x1.1a62633145c07p-54, fma(-n, 0x1.921fb54442d18p+0, angle)), z = r * r;     // pi / 2 in two pieces
     double s = 1.0 / 355687428096000.0, c = 1.0 / 20922789888000.0;
     s = fma(z, s, -1.0 / 1307674368000.0);
@@ -42,8 +43,8 @@ __device__ inline void sine_and_cosine(double angle, double &sine, double &cosin
     c = fma(z, c, 1.0);
     const long long quarter = (long long)n;
     const double a = quarter & 1 ? c : s, b = quarter & 1 ? s : c;
-    sine = quarter & 2 ? -a : a;
-    cosine = (quarter + 1) & 2 ? -b : b;
+    sine = far ? NAN : quarter & 2 ? -a : a;
+    cosine = far ? NAN : (quarter + 1) & 2 ? -b : b;
 }
 
 // What the widths of rows and turns allow: any; whole eights of columns, pairs next to each other (or none); whole eights that are paired with whole eights.

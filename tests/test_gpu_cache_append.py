@@ -194,3 +194,28 @@ def test_a_step_of_a_model_captured(bf, torch):  # noqa: F811
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(out, want)) and torch.equal(pages, held), i
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_angles_as_far_as_the_limit_and_past_it(bf, torch, dtype, interleaved):  # noqa: F811
+    """Angles below 2^50 are turned by as any others; a pair whose angle is not gives NaN, and no number that looks like a key."""
+    ps, far = 1024, 1 << 20
+    batch = Batch(torch, [4], [4], ps)
+    tables = torch.full((1, far // ps), -7, dtype=torch.int32, device="cuda")
+    tables[0, -1] = 0
+    batch.d_tables, batch.d_lengths, batch.lengths = tables, torch.tensor([far], device="cuda"), [far]
+    batch.places = lambda: ((i, 0, (far - 4 + i) % ps) for i in range(4))
+    f = torch.tensor([2.0 ** 30 - 64, 1.0, -2.0 ** 29, 2.0 ** 29 / 3, 12345678.0, 0.0, 2.0 ** -20, 3.5], device="cuda")   # (position times frequency: below 2^50)
+    _check(bf, torch, batch, 8, 2, 2, 16, ps, dtype, "joint", 8, interleaved, frequencies=f)
+    c = bf.PagedCache(8, 1, 16, ps)
+    for bad in (2.0 ** 31, -2.0 ** 31, 2.0 ** 120, float("inf"), float("nan")):
+        f[3] = bad
+        k = torch.randn(4, 1, 16, device="cuda").to(_dtype(torch, dtype))
+        pages = torch.zeros(1, c.page_bytes, dtype=torch.uint8, device="cuda")
+        q = c.append(pages, k, k, k, f, batch.d_tables, batch.d_lengths, interleaved=interleaved)
+        back, values = c.read(pages, batch.d_tables, batch.d_lengths, 4)
+        nan = [6, 7] if interleaved else [3, 11]
+        rest = [i for i in range(16) if i not in nan]
+        assert torch.isnan(q[..., nan]).all() and torch.isfinite(q[..., rest]).all(), bad
+        assert torch.isnan(back).all() and torch.isfinite(values).all(), bad
