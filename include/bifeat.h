@@ -603,8 +603,9 @@ typedef struct {
     const float *bias;   /* DEVICE [experts] or NULL */
 } bifeat_route_options;
 
-/* logits: DEVICE rows of `experts` columns of dtype, row_stride elements apart (>= 0).  ids: DEVICE
- * int32 [tokens][choices], weights: DEVICE fp32 of that shape. */
+/* logits: DEVICE rows of `experts` columns of dtype, row_stride elements apart (>= 0); tokens: at most
+ * INT32_MAX / 64 (33 554 431; both calls).  ids: DEVICE int32 [tokens][choices], weights: DEVICE fp32
+ * of that shape. */
 int bifeat_route(const void *logits, int64_t row_stride, int32_t dtype, int64_t tokens, const bifeat_route_options *options, int32_t *ids,
                  float *weights, void *stream);
 /* grad_logits: DEVICE [tokens][experts] of dtype. */

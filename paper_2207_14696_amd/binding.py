@@ -1,7 +1,7 @@
 """ctypes binding of the C ABI in ``include/bifeat.h``: same names, argument
 marshalling only.  Tensors are torch CUDA tensors; their ``data_ptr()`` and the
-current stream's handle are what crosses the boundary.  ``gather_dequant``, ``gather_mean``, ``gather_sum`` and the paged cache's
-calls (``cache.py``) without ``out`` go through a native module (``csrc/calls.cpp``) to the same entry points where it is built."""
+current stream's handle are what crosses the boundary.  ``gather_dequant``, ``gather_mean``, ``gather_sum``, the paged cache's
+calls (``cache.py``), products (``linear.py``) and ``route`` (``routing.py``) without ``out`` go through a native module (``csrc/calls.cpp``) to the same entry points where it is built."""
 from __future__ import annotations
 
 import ctypes as C

@@ -61,7 +61,7 @@ int check(const bifeat_cache *c, int64_t num_pages, const bf::CacheBatch &b, hip
     return bad ? BIFEAT_EINVAL : BIFEAT_OK;
 }
 
-// What the three calls ask of their common arguments.
+// What the four calls ask of their common arguments.
 int common(const bifeat_cache *c, const uint8_t *pages, int64_t num_pages, const bifeat_cache_batch *batch, int64_t heads,
            int32_t dtype) {
     if (!c || !type_ok(dtype) || num_pages < 0 || num_pages > INT32_MAX || !batch_ok(c, batch, heads)) return BIFEAT_EINVAL;

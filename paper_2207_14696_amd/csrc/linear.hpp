@@ -5,8 +5,10 @@
 //     = sum_g  s_g sum_{k in g} x_k (16 + q_k) + (m_g - 16 s_g) sum_{k in g} x_k.
 // 16 + q is a 16-bit float whose highest mantissa bits are q: two codes become two operands of a matrix product by a shift and one
 // bitwise instruction, exactly.  With rows of 32 bits the codes are taken as they are (twice the instructions, beside three products): the 16 would
-// bring sums three times as large, and cost them 1.5 bits.  The products of a group are summed in fp32 by the matrix cores, the sum of x beside them (a product with
-// ones), and two fused multiply-adds a group bring them to the result's.  Neither a weight nor a partial sum is ever rounded to 16 bits.
+// bring sums three times as large, and cost them 1.5 bits; a 16-bit result has 13 and more to spare.  The products of a group are summed in fp32 by the matrix cores and
+// scaled into the result; what sums of x add comes beside them, group by group or a few groups at a time, so that nothing larger than that ever stands in the
+// result: of few rows a product with ones has the sum of x (two fused multiply-adds a group), of many a kernel of its own, and another product brings it in.  Neither a
+// weight nor a partial sum is ever rounded to 16 bits.
 #pragma once
 
 #include "cache.hpp"

@@ -36,11 +36,13 @@ struct Plan {
     int64_t parts_bytes(const bifeat_linear_spec *s, int64_t rows) const { return split > 1 ? (split * rows * s->out_features + 3) / 4 * 16 : 0; }
     int64_t bytes(const bifeat_linear_spec *s, int64_t rows) const { return parts_bytes(s, rows) + (many ? sum_bytes(s, rows) : 0); }
 };
-// Of the ways to take the rows the one that is the fastest by what they measured (bf16, in parentheses fp32; us; 256 workgroups run at a time, for 128 rows 512):
+// Of the ways to take the rows the one that is the fastest by what they measured (bf16, in parentheses fp32; us; 256 workgroups run at a time, for 128 rows 512).
+// What the codes take from memory is the same in all of them and not in the figures, which therefore compare ways and foretell no time: one row by 8192 x 28 672
+// is 17.9 by them, 29.2 measured.
 //   16 tb rows by 16 r of the matrix a workgroup: 2.5 a call, and a round of workgroups 0.12, 0.2, 0.37, 0.55 a block of columns for tb = 1..4 (0.3, 0.6
 //     for 1, 2): 16 rows by 4096 x 4096 6.8, 64 rows 20; by 16 384 x 4096 24, 128 rows 43;
 //   128 rows by 128: 8 (what is summed first, and the beginning), 1.25 a block (3.6), 2.3 where two workgroups share a CU: 128 rows by 4096 x 4096 44,
-//     1024 51, 2048 79; fp32 128 rows 135, 2048 205 (a tile of 65 to 96 rows 0.8 of it);
+//     1024 51, 2048 80; fp32 128 rows 135, 2048 202 (a tile of 65 to 96 rows 0.8 of it);
 //   columns in parts: the parts' sums written and added, 2.5 and 8 bytes a sum and part at 4 TB/s: 40 rows by 8192 columns in one part 26, in four 15.
 Plan plan_of(const bifeat_linear_spec *s, int64_t rows, int32_t dtype) {
     const bool wide = dtype == BIFEAT_F32;
@@ -79,9 +81,12 @@ Room room_of(const bifeat_linear_spec *s, const bifeat_expert_rows *r) {
     Room o;
     const int64_t pairs = r->tokens * r->choices;
     // Tiles of up to 128 pairs where an expert has 16 on the average, and where so large ones are enough for the whole card: there 14 000 pairs times 128-row
-    // tiles of the matrix.  In tiles of 16 and of 128: 64 matrices of 1536 x 2048 with 16 pairs each 37 us and 37, with 32 57 and 44, with 48 79 and 59; 128 of
-    // 2048 x 768 with 16 44 and 43, with 32 69 and 52; 16 of 4096 x 4096 with 24 51 and 46; 200 of 512 x 1024 with 16 26 and 31, with 32 40 and 38; 8 of 1024 x 1024
-    // with 64 11 and 21, with 256 25 and 24; 32 of them with 48 21 and 23, with 96 33 and 30; 8 of 4096 x 4096 with 24 31 and 34, with 48 47 and 42.
+    // tiles of the matrix.  In tiles of 16 and of 128, of 16 bits: 64 matrices of 1536 x 2048 with 16 pairs each 37 us and 38, with 32 57 and 45, with 48 77 and 61; 128
+    // of 2048 x 768 with 16 44 and 42, with 32 71 and 52; 16 of 4096 x 4096 with 16 41 and 36, with 24 51 and 47; 200 of 512 x 1024 with 16 27 and 30, with 32 40 and 38;
+    // 8 of 1024 x 1024 with 96 15 and 22; 32 of them with 48 21 and 23, with 96 33 and 31; 8 of 4096 x 4096 with 24 31 and 36, with 48 47 and 44.  Rows of 32 bits pass
+    // over at the same numbers, though their 128 cost more: the first with 16 75 and 86, with 24 97 and 97, with 48 162 and 142; the second with 16 83 and 84, with 32 135
+    // and 104; 200 of 512 x 1024 with 24 63 and 62; 32 of 1024 x 1024 with 48 38 and 46, with 96 63 and 61; 8 of 4096 x 4096 with 48 98 and 123, with 96 179 and 162.
+    // (By the average: where pairs are is not known here, so that few pairs that crowd on few experts are taken by 16.)
     o.tile = pairs >= 16 * (int64_t)s->experts && pairs * ((s->out_features + 127) / 128) >= 14000 && s->in_features >= 8 ? bf::kManyRows : 16;
     o.most_tiles = pairs / o.tile + std::min<int64_t>(pairs, s->experts + 1);
     o.order = 16 + (o.most_tiles + 1) / 2 * 16;  // (a tile is 8 bytes)

@@ -104,8 +104,9 @@ class PackedLinear:
         """Each token by the matrices of its experts: x [tokens, in_features], or [tokens, choices, in_features] where each choice has a row of its
         own; ids int32 [tokens, choices], as ``route`` gives them (an id outside [0, experts) names none and gives zeros).  Returns
         [tokens, choices, out_features] of x's type, or with ``weights`` float32 [tokens, choices] their weighted sum,
-        [tokens, out_features].  Takes memory for the time of the call: 4 bytes a pair of a token and a choice, with weights
-        4 * out_features more.  No backward pass, and an ``out`` of its own memory, as ``multiply``."""
+        [tokens, out_features].  Takes memory for the time of the call (``bifeat_linear_experts_workspace`` has the number): 4 bytes a place of a
+        pair of a token and a choice, each expert's places filled up to a multiple of 16, or of 128 where pairs are many; there 8 bytes a group of
+        each row of x besides; with weights 4 * out_features a pair.  No backward pass, and an ``out`` of its own memory, as ``multiply``."""
         if out is None and self.experts is not None and (calls := _b._calls or _b._load_calls()):
             r = calls.linear_experts(*self._by_experts, packed, x, ids, weights)
             if r is not None:
